@@ -67,6 +67,7 @@ typedef enum {
 #define RK_DEV_TOO_LARGE     0x10  /* a window or prompt exceeded the launch's maximum   */
 #define RK_DEV_NO_CONVERGE   0x20  /* the assignment solver hit its iteration bound      */
 #define RK_DEV_BAD_PARAMS    0x40  /* an episode's policy parameters were invalid       */
+#define RK_DEV_BAD_BLOCK     0x80  /* a block number or slot lay outside the cache      */
 
 /* Static message for a status code. */
 const char* rk_status_string(int status);
@@ -477,6 +478,168 @@ int rk_poa_estimate_noalloc(int32_t n_windows, const int64_t* win_off, int32_t n
                             const int32_t* route_worker, const int32_t* overlap,
                             const int32_t* route_blocks, rk_poa_params params,
                             double* selfish_out, double* coord_out, double* poa_hat_out, void* stream);
+
+/* ------------------------------------------------------------ a worker's step
+ * What a worker does with the requests routed to it, whose cached prefixes the
+ * calls above find.  Its cache holds keys and values in blocks of
+ * RK_BLOCK_TOKENS tokens, the blocks that the chains name; row i of the block
+ * tables lists the blocks of request i's sequence.  A step of a batch:
+ *   rk_prefix_groups     requests with a common prefix, side by side
+ *   rk_block_tables      blocks and slots for the step's new tokens
+ *   rk_kv_write          the new tokens' keys and values into the cache
+ *   rk_prefix_attention  the new tokens' attention, a group's prefix read once
+ * The first two run once per step, the last two once per layer.  Sizes that
+ * only the device knows (groups, lengths) stay there: no call waits for them,
+ * and all four may be captured into a graph.  A batch has at most
+ * RK_MAX_BATCH requests (RK_EUNSUPPORTED above).
+ */
+#define RK_BLOCK_TOKENS 16
+#define RK_MAX_BATCH 4096
+#define RK_BF16 0
+#define RK_F16  1
+
+/*
+ * rk_prefix_groups -- order a batch by shared prompt prefix.
+ * A chained hash names its whole prefix, so requests i and j whose hash of
+ * block min_blocks - 1 is the same have at least min_blocks leading blocks in
+ * common and form one group; a request with fewer blocks is a group of its
+ * own.  Groups are numbered by their first request.  Group g shares
+ *   shared_g = min over its members i of (leading blocks that i's chain has in
+ *              common with the chain of the group's first request),
+ * 0 for a group of one.
+ *   B           requests, 0..RK_MAX_BATCH
+ *   chains      uint64, request i's chain is chains[chain_off[i] .. chain_off[i+1])
+ *   chain_off   int64 [B+1]
+ *   min_blocks  >= 1
+ *   order       int32 [B]     request numbers, group by group, ascending in a group
+ *   group_off   int64 [B+1]   group g is order[group_off[g] .. group_off[g+1]); B
+ *                             from the last group's end on, so that the arrays
+ *                             can be handed on without their number
+ *   shared      int32 [B]     shared_g, 0 from the last group on
+ *   n_groups    int32 [1]
+ * A hash of 0 at block min_blocks - 1 (a chain rk_hash_chains left short) names
+ * no prefix: RK_DEV_ZERO_KEY, the request is a group of its own.
+ */
+int rk_prefix_groups(int32_t B, const uint64_t* chains, const int64_t* chain_off, int32_t min_blocks,
+                     int32_t* order, int64_t* group_off, int32_t* shared, int32_t* n_groups, void* stream);
+
+/*
+ * rk_block_tables -- block tables and slot map of a step, from lengths.
+ * Request i will hold kv_len[i] tokens, the last new_len[i] of them new, in
+ * need_i = ceil(kv_len[i] / 16) blocks.  The first have[i] entries of its row
+ * are there already.  With groups, requests group_off[g] .. group_off[g+1]-1
+ * (side by side, in rk_prefix_groups' order) share their first
+ *   lead = min(shared[g], kv_len[f] / 16) blocks,  f = group_off[g].
+ * Entry p of row i becomes
+ *   p < have[i]                  unchanged
+ *   have[i] <= p < lead, i != f  the entry of row f
+ *   otherwise, p < need_i        the next of free_blocks, taken in the order of
+ *                                rows and entries
+ *   p >= need_i                  unchanged
+ * The t-th new token of request i is token q_off[i] + t of the step and
+ * position x = kv_len[i] - new_len[i] + t of its sequence; its slot is
+ *   16 * (entry x / 16 of row i) + x % 16,
+ * or -1 (not to be written) in a block that row f lends.
+ *   kv_len, new_len, have  int32 [B], new_len <= kv_len, kv_len <= 16 stride
+ *   group_off, shared      int64 [B+1], int32 [B], as of rk_prefix_groups; or both
+ *                          NULL: nothing is shared
+ *   free_blocks            int32 [n_free], block numbers
+ *   tables                 int32 [B * stride], row-major, read and written; stride < 2^20
+ *   slots                  int64 [n_slots]; -1 behind the last new token
+ *   q_off                  int64 [B+1]   tokens before request i's
+ *   taken                  int32 [1]     blocks taken from the front of free_blocks
+ * A request with lengths outside these bounds counts as one with no token and no block
+ * (RK_DEV_BAD_OFFSETS; RK_DEV_TOO_LARGE for kv_len > 16 stride), offsets that
+ * are no partition of the batch as no groups (RK_DEV_BAD_OFFSETS); new tokens
+ * past n_slots have no slot (RK_DEV_SHORT_INPUT); where free_blocks ends,
+ * entries and slots become -1 (RK_DEV_TABLE_FULL).
+ */
+int rk_block_tables(int32_t B, const int32_t* kv_len, const int32_t* new_len, const int32_t* have,
+                    const int64_t* group_off, const int32_t* shared, const int32_t* free_blocks, int32_t n_free,
+                    int32_t* tables, int32_t stride, int64_t* slots, int64_t n_slots, int64_t* q_off,
+                    int32_t* taken, void* stream);
+
+/* Strides of a block cache [block, token, head, element], in elements; the
+ * elements of a head lie side by side. */
+typedef struct {
+    int64_t block, token, head;
+} rk_cache_strides;
+
+/*
+ * rk_kv_write -- keys and values of new tokens into the block cache.
+ * Token t's Hkv heads of D 16-bit values go to token slots[t] % 16 of block
+ * slots[t] / 16; a negative slot is skipped, one past n_blocks too
+ * (RK_DEV_BAD_BLOCK).  The slots that are written must differ: of two tokens
+ * with one slot, either's values may remain, in any mixture.
+ *   T                  tokens (>= 0)
+ *   Hkv, D             key heads (1..1024), values of a head (a multiple of 8, 8..256)
+ *   k, v               [T, Hkv, D], strides k_token, k_head, v_token, v_head
+ *   k_cache, v_cache   [n_blocks, 16, Hkv, D], strides ks, vs
+ *   slots              int64 [T]
+ * All strides are multiples of 8 elements (>= 0), pointers of 16 bytes.
+ */
+int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                int64_t v_token, int64_t v_head, void* k_cache, rk_cache_strides ks, void* v_cache,
+                rk_cache_strides vs, int32_t n_blocks, const int64_t* slots, void* stream);
+
+/*
+ * rk_prefix_attention -- attention of a step's new tokens over the block cache.
+ * Query head h of token t (position x of request i, as in rk_block_tables)
+ * attends to the key head h / (Hq / Hkv) at the positions j <= x of its
+ * sequence, token j % 16 of the block at entry j / 16 of row i:
+ *   out[t, h] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q[t, h] . k_j)
+ *   lse[t, h] = log sum_j w_j
+ * with sums and softmax statistics in fp32 and the w_j of a tile rounded to the cache's type for
+ * the product with the values.  With groups, the first lead entries (as in
+ * rk_block_tables) of a group's rows are the same blocks, and where that is the faster way
+ * the group's rows attend to them together, read through the first row.
+ * No key or value past a token's position has a part in its result, whatever
+ * it holds; the tokens of q behind q_off[B] are not read, and their rows of out and lse stay
+ * as they were.
+ *   B           requests, 0..RK_MAX_BATCH;  T  tokens that q and out hold
+ *   Hq, Hkv     query and key heads, Hq a multiple of Hkv, at most 128 per key head
+ *   D           values of a head, a multiple of 8, 8..256
+ *   dtype       RK_BF16 or RK_F16, of q, caches and out
+ *   q, out      [T, Hq, D], strides q_token, q_head, out_token, out_head
+ *   k_cache, v_cache  [n_blocks, 16, Hkv, D], strides ks, vs (token stride >= D and
+ *               < 2^26)
+ *   tables      int32 [B * table_stride]
+ *   kv_len      int32 [B]    tokens of each sequence, the new ones included
+ *   q_off       int64 [B+1]  tokens of q of each request
+ *   group_off, shared        as in rk_block_tables, or both NULL
+ *   lse         float [T * Hq], or NULL
+ * Strides are multiples of 8 elements (>= 0), pointers of 16 bytes; out overlaps no input.
+ * workspace: rk_prefix_attention_workspace_size bytes, 256-byte aligned, of any content, for this
+ * call alone until it has run.
+ * A request whose tokens, length or table do not fit (RK_DEV_BAD_OFFSETS;
+ * RK_DEV_TOO_LARGE for kv_len > 16 table_stride) is skipped, its rows left as
+ * they were; the keys of a block number outside 0..n_blocks-1 are left out
+ * (RK_DEV_BAD_BLOCK), and a token that sees no key gets 0 and -infinity.
+ */
+typedef struct {
+    int32_t B, Hq, Hkv, D, dtype, n_blocks, table_stride;
+    float scale;
+    int64_t T;
+    const void* q;
+    int64_t q_token, q_head;
+    const void* k_cache;
+    rk_cache_strides ks;
+    const void* v_cache;
+    rk_cache_strides vs;
+    const int32_t* tables;
+    const int32_t* kv_len;
+    const int64_t* q_off;
+    const int64_t* group_off;
+    const int32_t* shared;
+    void* out;
+    int64_t out_token, out_head;
+    float* lse;
+} rk_attention;
+
+/* Workspace bytes for a call of these sizes on the current device (0 if they are not supported). */
+size_t rk_prefix_attention_workspace_size(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
+
+int rk_prefix_attention(const rk_attention* a /* host */, void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

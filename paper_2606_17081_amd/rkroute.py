@@ -23,13 +23,16 @@ RK_POLICY_ARGMIN, RK_POLICY_SOFTMAX, RK_POLICY_ROUND_ROBIN, RK_POLICY_RANDOM, RK
 RK_EVICT_LRU, RK_EVICT_FREQ = 0, 1
 RK_FREQ_CAP = 1 << 20
 DEV_BITS = {0x1: "bad offsets", 0x2: "short input", 0x4: "zero key", 0x8: "table full",
-            0x10: "too large", 0x20: "no convergence", 0x40: "bad policy parameters"}
+            0x10: "too large", 0x20: "no convergence", 0x40: "bad policy parameters", 0x80: "bad block"}
+RK_BLOCK_TOKENS, RK_MAX_BATCH = 16, 4096
+RK_BF16, RK_F16 = 0, 1
 
 EXPORTED = ("rk_status_string", "rk_last_error", "rk_device_status", "rk_hash_chains",
             "rk_table_build", "rk_route_score_batch", "rk_index_build", "rk_route_score_index",
             "rk_simulate_workspace_size",
             "rk_simulate_episodes", "rk_poa_workspace_size", "rk_poa_estimate",
-            "rk_poa_estimate_noalloc")
+            "rk_poa_estimate_noalloc", "rk_prefix_groups", "rk_block_tables", "rk_kv_write",
+            "rk_prefix_attention_workspace_size", "rk_prefix_attention")
 RK_POA_NOALLOC_BYTES = 64 << 20
 
 
@@ -73,6 +76,20 @@ class EpisodeOutputs(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("route_turn", "route_worker", "route_step", "route_blocks",
                                           "overlap", "cost", "evict_count", "evict_digest",
                                           "last_hash", "totals", "route_regime", "tier_overlap")]
+
+
+class CacheStrides(C.Structure):
+    _fields_ = [("block", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
+                ("n_blocks", C.c_int32), ("table_stride", C.c_int32), ("scale", C.c_float), ("T", C.c_int64),
+                ("q", C.c_void_p), ("q_token", C.c_int64), ("q_head", C.c_int64),
+                ("k_cache", C.c_void_p), ("ks", CacheStrides), ("v_cache", C.c_void_p), ("vs", CacheStrides),
+                ("tables", C.c_void_p), ("kv_len", C.c_void_p), ("q_off", C.c_void_p),
+                ("group_off", C.c_void_p), ("shared", C.c_void_p),
+                ("out", C.c_void_p), ("out_token", C.c_int64), ("out_head", C.c_int64), ("lse", C.c_void_p)]
 
 
 # rk_episode_params, 104 bytes, as a numpy record
@@ -130,6 +147,17 @@ def lib():
             L.rk_poa_estimate_noalloc.restype = C.c_int
             L.rk_poa_estimate_noalloc.argtypes = [i32, vp, i32, vp, i64, i32, i32, vp, vp, vp, PoaParams,
                                                   vp, vp, vp, vp]
+            L.rk_prefix_groups.restype = C.c_int
+            L.rk_prefix_groups.argtypes = [i32, vp, vp, i32, vp, vp, vp, vp, vp]
+            L.rk_block_tables.restype = C.c_int
+            L.rk_block_tables.argtypes = [i32, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, i64, vp, vp, vp]
+            L.rk_kv_write.restype = C.c_int
+            L.rk_kv_write.argtypes = [i64, i32, i32, vp, i64, i64, vp, i64, i64, vp, CacheStrides, vp, CacheStrides,
+                                      i32, vp, vp]
+            L.rk_prefix_attention_workspace_size.restype = sz
+            L.rk_prefix_attention_workspace_size.argtypes = [i64, i32, i32, i32, i32]
+            L.rk_prefix_attention.restype = C.c_int
+            L.rk_prefix_attention.argtypes = [C.POINTER(Attention), vp, sz, vp]
             _lib = L
     return _lib
 
@@ -352,3 +380,191 @@ def poa_estimate_noalloc(win_off, ep_win_off, n_rows: int, max_window: int, W: i
                                          _ptr(route_worker), _ptr(overlap), _ptr(route_blocks), params,
                                          _ptr(selfish), _ptr(coord), _ptr(poa_hat), _stream(stream)),
            "rk_poa_estimate_noalloc")
+
+
+# ------------------------------------------------------------------ a worker's step
+
+class _On:
+    """Where a call with tensors on `device` runs: on the given stream, or on that device's current one.  Meanwhile
+    it is the current stream, so that what the call allocates is that stream's too."""
+
+    def __init__(self, device, stream):
+        torch = _torch()
+        if stream is not None:
+            if stream.device != device:
+                raise RkError(f"the stream is on {stream.device}, the tensors are on {device}")
+            self.context = torch.cuda.stream(stream)
+        else:
+            self.context = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.context is not None:
+            self.context.__enter__()
+        return _stream()
+
+    def __exit__(self, *exc):
+        if self.context is not None:
+            self.context.__exit__(*exc)
+        return False
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise RkError(f"{name} is on {t.device}, not on {device}")
+
+
+def _size(name, t, n):
+    if t is not None and t.numel() < n:
+        raise RkError(f"{name} holds {t.numel()} elements, {n} needed")
+
+
+def prefix_groups(chains, chain_off, min_blocks: int = 1, order=None, group_off=None, shared=None, n_groups=None,
+                  stream=None):
+    """The batch ordered by shared prompt prefix (rk_prefix_groups): (order, group_off, shared, n_groups)."""
+    torch = _torch()
+    _need(chains, torch.uint64, "chains")
+    _need(chain_off, torch.int64, "chain_off")
+    if chain_off.numel() < 1:
+        raise RkError("chain_off is empty")
+    B, dev = chain_off.numel() - 1, chain_off.device
+    with _On(dev, stream) as st:
+        def out(t, n, dtype, name):
+            if t is None:
+                t = torch.empty(n, dtype=dtype, device=dev)
+            _need(t, dtype, name)
+            _size(name, t, n)
+            return t
+
+        order = out(order, B, torch.int32, "order")
+        group_off = out(group_off, B + 1, torch.int64, "group_off")
+        shared = out(shared, B, torch.int32, "shared")
+        n_groups = out(n_groups, 1, torch.int32, "n_groups")
+        _same_device(dev, chains=chains, order=order, group_off=group_off, shared=shared, n_groups=n_groups)
+        _check(lib().rk_prefix_groups(B, _ptr(chains), _ptr(chain_off), min_blocks, _ptr(order), _ptr(group_off),
+                                      _ptr(shared), _ptr(n_groups), st), "rk_prefix_groups")
+    return order, group_off, shared, n_groups
+
+
+def block_tables(tables, kv_len, new_len, have, free_blocks, n_slots: int, group_off=None, shared=None, slots=None,
+                 q_off=None, taken=None, stream=None):
+    """Block tables (in place) and slot map of a step (rk_block_tables): (tables, slots, q_off, taken).
+    tables is [B, stride]; n_slots is the number of slots wanted, the step's new tokens or more."""
+    torch = _torch()
+    for t, name in ((tables, "tables"), (kv_len, "kv_len"), (new_len, "new_len"), (have, "have"),
+                    (free_blocks, "free_blocks"), (shared, "shared")):
+        _need(t, torch.int32, name)
+    _need(group_off, torch.int64, "group_off")
+    B, dev = kv_len.numel(), kv_len.device
+    if tables.dim() != 2 or tables.shape[0] < B:
+        raise RkError("tables must be [B, stride]")
+    for t, n, name in ((new_len, B, "new_len"), (have, B, "have"), (group_off, B + 1, "group_off"), (shared, B, "shared")):
+        _size(name, t, n)
+    with _On(dev, stream) as st:
+        def out(t, n, dtype, name):
+            if t is None:
+                t = torch.empty(n, dtype=dtype, device=dev)
+            _need(t, dtype, name)
+            _size(name, t, n)
+            return t
+
+        slots = out(slots, n_slots, torch.int64, "slots")
+        q_off = out(q_off, B + 1, torch.int64, "q_off")
+        taken = out(taken, 1, torch.int32, "taken")
+        _same_device(dev, tables=tables, new_len=new_len, have=have, free_blocks=free_blocks, group_off=group_off,
+                     shared=shared, slots=slots, q_off=q_off, taken=taken)
+        _check(lib().rk_block_tables(B, _ptr(kv_len), _ptr(new_len), _ptr(have), _ptr(group_off), _ptr(shared),
+                                     _ptr(free_blocks), free_blocks.numel(), _ptr(tables), tables.shape[1], _ptr(slots),
+                                     n_slots, _ptr(q_off), _ptr(taken), st), "rk_block_tables")
+    return tables, slots, q_off, taken
+
+
+def _rows(t, name, dtype=None):
+    """A [tokens, heads, D] tensor with its heads' elements side by side: its strides of tokens and heads."""
+    torch = _torch()
+    if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float16) or (dtype is not None and t.dtype != dtype):
+        raise RkError(f"{name} must be a CUDA tensor of {dtype or 'bfloat16 or float16'}")
+    if t.dim() != 3 or (t.numel() and t.stride(2) != 1):
+        raise RkError(f"{name} must be [tokens, heads, D] with a head's elements side by side")
+    n, heads, _ = t.shape
+    return t.stride(0) if n > 1 else 0, t.stride(1) if n and heads > 1 else 0       # of one, any stride will do
+
+
+def _cache_strides(t, name, dtype, heads, D):
+    if not t.is_cuda or t.dtype != dtype:
+        raise RkError(f"{name} must be a CUDA tensor of {dtype}")
+    if t.dim() != 4 or t.shape[1:] != (RK_BLOCK_TOKENS, heads, D) or (t.numel() and t.stride(3) != 1):
+        raise RkError(f"{name} must be [blocks, {RK_BLOCK_TOKENS}, {heads}, {D}] with a head's elements side by side")
+    n = t.shape[0]
+    return CacheStrides(t.stride(0) if n > 1 else 0, t.stride(1) if n else D, t.stride(2) if n and heads > 1 else 0)
+
+
+def kv_write(k, v, k_cache, v_cache, slots, stream=None):
+    """Keys and values [T, Hkv, D] of new tokens into the block cache [blocks, 16, Hkv, D] (rk_kv_write)."""
+    torch = _torch()
+    k_token, k_head = _rows(k, "k")
+    v_token, v_head = _rows(v, "v", k.dtype)
+    _need(slots, torch.int64, "slots")
+    T, Hkv, D = k.shape
+    if tuple(v.shape) != (T, Hkv, D):
+        raise RkError("k and v differ in shape")
+    _size("slots", slots, T)
+    ks = _cache_strides(k_cache, "k_cache", k.dtype, Hkv, D)
+    vs = _cache_strides(v_cache, "v_cache", k.dtype, Hkv, D)
+    if k_cache.shape[0] != v_cache.shape[0]:
+        raise RkError("k_cache and v_cache differ in blocks")
+    _same_device(k.device, v=v, k_cache=k_cache, v_cache=v_cache, slots=slots)
+    with _On(k.device, stream) as st:
+        _check(lib().rk_kv_write(T, Hkv, D, _ptr(k), k_token, k_head, _ptr(v), v_token, v_head, _ptr(k_cache), ks,
+                                 _ptr(v_cache), vs, k_cache.shape[0], _ptr(slots), st), "rk_kv_write")
+
+
+def prefix_attention_workspace_size(T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
+    return int(lib().rk_prefix_attention_workspace_size(T, B, Hq, Hkv, D))
+
+
+def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None, shared=None, scale=None, out=None,
+                     lse=None, want_lse=False, workspace=None, stream=None):
+    """Attention of new tokens q [T, Hq, D] over the block cache (rk_prefix_attention): (out, lse or None).
+    scale defaults to D ** -0.5.  Rows behind the last request's stay as they were (in an `out` allocated here,
+    uninitialised)."""
+    torch = _torch()
+    q_token, q_head = _rows(q, "q")
+    T, Hq, D = q.shape
+    if k_cache.dim() != 4:
+        raise RkError("k_cache must be [blocks, 16, heads, D]")
+    Hkv = k_cache.shape[2]
+    ks = _cache_strides(k_cache, "k_cache", q.dtype, Hkv, D)
+    vs = _cache_strides(v_cache, "v_cache", q.dtype, Hkv, D)
+    if k_cache.shape[0] != v_cache.shape[0]:
+        raise RkError("k_cache and v_cache differ in blocks")
+    for t, name in ((tables, "tables"), (kv_len, "kv_len"), (shared, "shared")):
+        _need(t, torch.int32, name)
+    _need(q_off, torch.int64, "q_off")
+    _need(group_off, torch.int64, "group_off")
+    B, dev = kv_len.numel(), q.device
+    if tables.dim() != 2 or tables.shape[0] < B:
+        raise RkError("tables must be [B, stride]")
+    for t, n, name in ((q_off, B + 1, "q_off"), (group_off, B + 1, "group_off"), (shared, B, "shared")):
+        _size(name, t, n)
+    with _On(dev, stream) as st:
+        if out is None:
+            out = torch.empty((T, Hq, D), dtype=q.dtype, device=dev)
+        out_token, out_head = _rows(out, "out", q.dtype)
+        if tuple(out.shape) != (T, Hq, D):
+            raise RkError("out and q differ in shape")
+        if lse is None and want_lse:
+            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        _need(lse, torch.float32, "lse")
+        _size("lse", lse, T * Hq)
+        if workspace is None:
+            workspace = torch.empty(prefix_attention_workspace_size(T, B, Hq, Hkv, D), dtype=torch.uint8, device=dev)
+        _same_device(dev, k_cache=k_cache, v_cache=v_cache, tables=tables, kv_len=kv_len, q_off=q_off,
+                     group_off=group_off, shared=shared, out=out, lse=lse, workspace=workspace)
+        a = Attention(B, Hq, Hkv, D, RK_BF16 if q.dtype == torch.bfloat16 else RK_F16, k_cache.shape[0], tables.shape[1],
+                      D ** -0.5 if scale is None else scale, T, _ptr(q), q_token, q_head, _ptr(k_cache), ks,
+                      _ptr(v_cache), vs, _ptr(tables), _ptr(kv_len), _ptr(q_off), _ptr(group_off), _ptr(shared),
+                      _ptr(out), out_token, out_head, _ptr(lse))
+        _check(lib().rk_prefix_attention(C.byref(a), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                         st), "rk_prefix_attention")
+    return out, lse

@@ -1,0 +1,126 @@
+"""A worker's step: what the C ABI refuses on the host, before any launch, and what the binding refuses."""
+import ctypes as C
+
+import pytest
+
+from paper_2606_17081_amd import rkroute as rk
+
+P = C.c_void_p(4096)
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not rk.library_available():
+        pytest.skip("librkroute.so not built")
+    return rk.lib()
+
+
+def test_groups_refusals(L):
+    f = L.rk_prefix_groups
+    assert f(-1, P, P, 1, P, P, P, P, None) == rk.RK_EINVAL
+    assert f(rk.RK_MAX_BATCH + 1, P, P, 1, P, P, P, P, None) == rk.RK_EUNSUPPORTED
+    assert f(4, P, P, 0, P, P, P, P, None) == rk.RK_EINVAL and b"min_blocks" in L.rk_last_error()
+    for k in (1, 2, 4, 5, 6, 7):
+        a = [4, P, P, 1, P, P, P, P, None]
+        a[k] = None
+        assert f(*a) == rk.RK_EINVAL
+
+
+def test_tables_refusals(L):
+    f = L.rk_block_tables
+    good = [4, P, P, P, P, P, P, 9, P, 8, P, 5, P, P, None]
+
+    def rc(**at):
+        a = list(good)
+        for k, v in at.items():
+            a[int(k[1:])] = v
+        return f(*a)
+
+    for k in ("_0", "_7", "_9", "_11"):
+        assert rc(**{k: -1}) == rk.RK_EINVAL and b"negative" in L.rk_last_error()
+    assert rc(_0=rk.RK_MAX_BATCH + 1) == rk.RK_EUNSUPPORTED
+    assert rc(_9=1 << 20) == rk.RK_EUNSUPPORTED and b"stride" in L.rk_last_error()
+    for k in (1, 2, 3, 4, 5, 6, 8, 10, 12, 13):
+        assert rc(**{f"_{k}": None}) == rk.RK_EINVAL
+
+
+def test_write_refusals(L):
+    f = L.rk_kv_write
+    s = rk.CacheStrides(16 * 64, 64, 64)
+    good = [3, 1, 64, P, 64, 64, P, 64, 64, P, s, P, s, 7, P, None]
+
+    def rc(**at):
+        a = list(good)
+        for k, v in at.items():
+            a[int(k[1:])] = v
+        return f(*a)
+
+    assert rc(_0=-1) == rk.RK_EINVAL and rc(_13=-1) == rk.RK_EINVAL
+    assert rc(_0=0) == rk.RK_OK
+    assert rc(_1=0) == rc(_1=1025) == rk.RK_EUNSUPPORTED
+    assert rc(_2=0) == rc(_2=60) == rc(_2=264) == rk.RK_EUNSUPPORTED
+    for k in (4, 5, 7, 8):
+        assert rc(**{f"_{k}": 4}) == rc(**{f"_{k}": -8}) == rk.RK_EINVAL and b"stride" in L.rk_last_error()
+    for k in (10, 12):
+        for bad in (rk.CacheStrides(1, 64, 64), rk.CacheStrides(1024, -64, 64), rk.CacheStrides(1024, 64, 3)):
+            assert rc(**{f"_{k}": bad}) == rk.RK_EINVAL
+    for k in (3, 6, 9, 11, 14):
+        assert rc(**{f"_{k}": None}) == rk.RK_EINVAL
+    for k in (3, 6, 9, 11):
+        assert rc(**{f"_{k}": C.c_void_p(4104)}) == rk.RK_EINVAL and b"aligned" in L.rk_last_error()
+
+
+def _attention(**change):
+    s = rk.CacheStrides(16 * 2 * 64, 2 * 64, 64)
+    v = P.value
+    a = rk.Attention(4, 8, 2, 64, rk.RK_BF16, 50, 9, 0.125, 10, v, 8 * 64, 64, v, s, v, s, v, v, v, v, v, v, 8 * 64, 64, v)
+    for k, x in change.items():
+        setattr(a, k, x)
+    return a
+
+
+def test_attention_refusals(L):
+    def rc(ws=P, size=1 << 40, **change):
+        return L.rk_prefix_attention(C.byref(_attention(**change)), ws, size, None)
+
+    assert L.rk_prefix_attention(None, P, 1 << 30, None) == rk.RK_EINVAL
+    for k in ("B", "T", "n_blocks", "table_stride"):
+        assert rc(**{k: -1}) == rk.RK_EINVAL
+    assert rc(B=0) == rc(T=0) == rk.RK_OK
+    assert rc(Hq=7) == rc(Hq=0) == rc(Hkv=0) == rk.RK_EINVAL
+    assert rc(B=rk.RK_MAX_BATCH + 1) == rc(Hq=2 * 129) == rc(D=12) == rc(D=264) == rc(D=0) == rk.RK_EUNSUPPORTED
+    assert rc(T=1 << 40) == rc(dtype=2) == rc(dtype=-1) == rk.RK_EUNSUPPORTED
+    assert rc(scale=float("nan")) == rc(scale=float("inf")) == rk.RK_EINVAL
+    for k in ("q_token", "q_head", "out_token", "out_head"):
+        assert rc(**{k: 4}) == rc(**{k: -8}) == rk.RK_EINVAL
+    for k in ("ks", "vs"):
+        for s in (rk.CacheStrides(7, 128, 64), rk.CacheStrides(2048, 56, 64), rk.CacheStrides(2048, 1 << 26, 64),
+                  rk.CacheStrides(2048, 128, -64)):
+            assert rc(**{k: s}) == rk.RK_EINVAL
+    for k in ("q", "k_cache", "v_cache", "tables", "kv_len", "q_off", "group_off", "shared", "out"):
+        assert rc(**{k: None}) == rk.RK_EINVAL
+    for k in ("q", "k_cache", "v_cache", "out"):
+        assert rc(**{k: 4104}) == rk.RK_EINVAL and b"aligned" in L.rk_last_error()
+
+
+def test_attention_refuses_a_workspace_too_small(L):
+    need = rk.prefix_attention_workspace_size(10, 4, 8, 2, 64)
+    assert need > 0
+    a = _attention()
+    assert L.rk_prefix_attention(C.byref(a), P, need - 1, None) == rk.RK_ENOMEM
+    assert L.rk_prefix_attention(C.byref(a), None, need, None) == rk.RK_ENOMEM
+    assert L.rk_prefix_attention(C.byref(a), C.c_void_p(4096 + 16), need, None) == rk.RK_EINVAL
+
+
+def test_workspace_sizes(L):
+    size = rk.prefix_attention_workspace_size
+    assert size(1, 4097, 8, 2, 64) == size(1, 1, 7, 2, 64) == size(1, 1, 8, 2, 60) == size(-1, 1, 8, 2, 64) == 0
+    assert 0 < size(1, 1, 8, 2, 64) <= size(100, 50, 8, 2, 64) <= size(5000, 50, 8, 2, 64)
+
+
+def test_binding_needs_a_gpu_tensor():
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is there")
+    with pytest.raises(rk.RkError, match="no GPU"):
+        rk.kv_write(torch.zeros(1, 1, 8), torch.zeros(1, 1, 8), torch.zeros(1, 16, 1, 8), torch.zeros(1, 16, 1, 8), None)
