@@ -7,84 +7,1174 @@
 
 namespace rk {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kWideRows = 128, kWideKeys = 64;       // a wide step: 32 rows a wavefront, 64 keys
+constexpr int kNarrowRows = 32, kNarrowKeys = 128;   // a narrow step: 32 keys a wavefront
+constexpr uint32_t kWideCost = 2, kNarrowCost = 3;   // of a step, relative to each other
+constexpr uint32_t kLeast = 6;                       // cost that a workgroup takes at least
+constexpr int kShareBlocks = 4;                      // shorter prefixes are not worth joining their parts
+constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
+
+// A tile that more than one workgroup worked on, as the workgroup that began it noted it; n = 0: none.
+struct __align__(16) Split {
+    int32_t n, wg, token, tokens, head, pad[3];
+};
+
+// A row of tables that shares its prefix: its parts, as the workgroup that began its tile noted them.
+struct __align__(16) Parts {
+    int32_t n, wg, row, pad;                 // n = 0: one part, in the shared rows' own place
+};
+
 struct AttendArgs {
     rk_attention a;
     int32_t* status;
+    int32_t b0, n;                           // the launch's requests: n from b0 on
+    Split* split;                            // [grid]
+    int32_t* share_base;                     // [n]: first shared token of a request, -1: it shares nothing
+    Parts* parts;                            // [2][Hkv][shared tokens]
+    float *part, *part_ml;                   // [2 grid][kWideRows][DP], [..][2]: first and last tile of a workgroup
+    float *whole, *whole_ml;                 // [2][Hkv][shared rows][DP], [..][2]
+    int32_t shared_rows, shared_tokens;      // what whole and parts hold, of a head
 };
 
 template <bool Half>
-__device__ __forceinline__ float to_float(uint16_t x)
+__device__ __forceinline__ uint32_t pack16(float x, float y)
 {
-    if constexpr (Half) return (float)__builtin_bit_cast(_Float16, x);
-    else return __uint_as_float((uint32_t)x << 16);
+    if constexpr (Half) {
+        return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x) |
+               ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)y) << 16);
+    } else {
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+        bf2 v = {(__bf16)x, (__bf16)y};
+        return __builtin_bit_cast(uint32_t, v);
+    }
 }
 
-// fp32 to 16 bits, to nearest even.
 template <bool Half>
-__device__ __forceinline__ uint16_t from_float(float x)
+__device__ __forceinline__ float unpack16(uint32_t x)      // the low half
 {
-    if constexpr (Half) return __builtin_bit_cast(uint16_t, (_Float16)x);
-    else return __builtin_bit_cast(uint16_t, (__bf16)x);
+    if constexpr (Half) return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
+    else return __uint_as_float(x << 16);
 }
 
-// A workgroup of one wavefront per (token, query head): a lane per four-element
-// piece of the head, one key after another.
 template <bool Half>
-__global__ __launch_bounds__(64) void attend_plain_kernel(AttendArgs p)
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c)
+{
+    if constexpr (Half)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+
+template <bool Half>
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
+{
+    if constexpr (Half)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+
+// 16-bit values of an exponent of all ones: infinities and NaN
+template <bool Half>
+constexpr uint32_t kExponent = Half ? 0x7c007c00u : 0x7f807f80u;
+
+// x with a half of all-ones exponent replaced by 0
+template <bool Half>
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t x)
+{
+    const uint32_t e = kExponent<Half>;
+    if ((x & e & 0xffffu) == (e & 0xffffu)) x &= 0xffff0000u;
+    if ((x & e & 0xffff0000u) == (e & 0xffff0000u)) x &= 0xffffu;
+    return x;
+}
+
+template <bool Half>
+__device__ __forceinline__ bool not_finite(uint32_t x)
+{
+    const uint32_t e = kExponent<Half>;
+    return (x & e & 0xffffu) == (e & 0xffffu) || (x & e & 0xffff0000u) == (e & 0xffff0000u);
+}
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+__device__ __forceinline__ u32x4 lds_read16(uint32_t at)
+{
+    return *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>((lds_u8*)(uintptr_t)at);
+}
+__device__ __forceinline__ u32x2 lds_read8(uint32_t at)
+{
+    return *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>((lds_u8*)(uintptr_t)at);
+}
+// Four rows of 16 values, transposed: the 16 lanes of a group each name 8 bytes (lane j: row j / 4, values
+// 4 (j % 4) ..), lane j gets value j of the four rows.
+__device__ __forceinline__ u32x2 lds_read_columns(uint32_t at)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) s16x4*)(lds_u8*)(uintptr_t)at));
+}
+
+// x, in a way that what is computed from it stays where it is used: hoisted out of the loop over tiles, the
+// addresses of all three kinds of tile would be held (and spilled) at once.
+__device__ __forceinline__ int32_t afresh(int32_t x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// x, the same in all lanes, as the compiler then knows.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x)
+{
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(x >> 32)) << 32) |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)x);
+}
+
+// The workgroup's inclusive sums; tmp: 2 * kWaves words.
+__device__ __forceinline__ void incl_sums(uint64_t& x, uint32_t& y, uint64_t* tmp)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t ox = __shfl_up(x, d);
+        const uint32_t oy = __shfl_up(y, d);
+        if (lane >= d) {
+            x += ox;
+            y += oy;
+        }
+    }
+    if (lane == 63) {
+        tmp[wave] = x;
+        tmp[kWaves + wave] = y;
+    }
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) {
+        x += tmp[w];
+        y += (uint32_t)tmp[kWaves + w];
+    }
+}
+
+// One tile's work: rows of the tokens [token, token + tokens) on key head `head`, steps [s0, s1) of n_steps.
+struct Tile {
+    const int32_t* row;                      // the block table's row
+    int32_t block0;                          // first block of the segment
+    int32_t keys_end;                        // first position that no row sees
+    int32_t token, tokens, pos;              // of the first row's token
+    int32_t head;
+    int32_t s0, s1, n_steps;
+    bool mask;                               // rows see up to their own position (else up to keys_end)
+    float *part, *part_ml;                   // where the result goes; NULL: to out and lse
+};
+
+template <int DP, bool Half>
+struct Attend {
+    static constexpr int NC = DP / 8;                 // 16-byte pieces of a row
+    static constexpr int NI = NC / 4;                 // loads of 64 pieces that bring a block
+    static constexpr uint32_t kRow = DP * 2;          // bytes of a row in LDS
+    static constexpr uint32_t kTileBytes = 512 * DP;  // LDS for keys and values
+
+    const AttendArgs& p;
+    const uint32_t tile;                              // LDS address of the keys and values
+    float* const join;                                // LDS: 2 * kWaves * kNarrowRows
+    const int wave;
+    const int32_t G;                                  // query heads of a key head
+    const float c;                                    // |scale| log2(e)
+    uint32_t k_at[NI], v_at[NI];                      // byte offsets, in a block, of the pieces that the lane loads
+
+    __device__ __forceinline__ Attend(const AttendArgs& args, uint32_t lds, float* j, float scale)
+        : p(args), tile(lds), join(j), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), G(args.a.Hq / args.a.Hkv),
+          c(scale)
+    {
+        const int lane = threadIdx.x & 63;
+        // Row r of a block keeps its piece x at place x ^ (r % 8): rows of 128 bytes and more would
+        // otherwise put what a wavefront reads together into the same banks.
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int x = 64 * i + lane, r = x / NC, piece = (x % NC) ^ (r & 7);
+            const bool in = 8 * piece < p.a.D;        // pieces behind D are loaded as zeros
+            k_at[i] = in ? (uint32_t)(r * (int32_t)p.a.ks.token * 2 + 16 * piece) : 0x7ffffff0u;
+            v_at[i] = in ? (uint32_t)(r * (int32_t)p.a.vs.token * 2 + 16 * piece) : 0x7ffffff0u;
+        }
+    }
+
+    // The block's `rows` first rows from base to LDS, zeros after them.  Straight to LDS, in flight until a wait for
+    // vector memory; written as asm with no register result so that the compiler does not place that wait before
+    // every LDS read.
+    __device__ __forceinline__ void load_block(const uint16_t* base, int64_t stride, int32_t rows, const uint32_t* at,
+                                               uint32_t lds) const
+    {
+        const uint64_t b = (uint64_t)base;
+        u32x4 rsrc;
+        rsrc.x = (uint32_t)b;
+        rsrc.y = (uint32_t)(b >> 32) & 0xffffu;
+        rsrc.z = rows > 0 ? (uint32_t)((rows - 1) * (int32_t)stride * 2 + p.a.D * 2) : 0u;
+        rsrc.w = 0x00027000u;
+        rsrc.x = __builtin_amdgcn_readfirstlane(rsrc.x);
+        rsrc.y = __builtin_amdgcn_readfirstlane(rsrc.y);
+        rsrc.z = __builtin_amdgcn_readfirstlane(rsrc.z);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + 1024u * i);
+            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at[i]), "s"(rsrc)
+                         : "memory");
+        }
+    }
+
+    // Block number `b`'s block of the segment's sequence, keys to k_lds, values to v_lds (either may be left out).
+    __device__ __forceinline__ int32_t block_id(const Tile& t, int32_t b) const
+    {
+        return (int64_t)b * RK_BLOCK_TOKENS < t.keys_end ? t.row[b] : 0;
+    }
+    __device__ __forceinline__ int32_t rows_of(const Tile& t, int32_t b, int32_t id) const
+    {
+        const int32_t n = t.keys_end - b * RK_BLOCK_TOKENS;
+        return (uint32_t)id < (uint32_t)p.a.n_blocks ? (n < RK_BLOCK_TOKENS ? n : RK_BLOCK_TOKENS) : 0;
+    }
+    __device__ __forceinline__ void load_keys(const Tile& t, int32_t b, int32_t id, uint32_t lds) const
+    {
+        const int32_t rows = rows_of(t, b, id);
+        load_block((const uint16_t*)p.a.k_cache + (rows > 0 ? (int64_t)id * p.a.ks.block : 0) + t.head * p.a.ks.head,
+                   p.a.ks.token, rows, k_at, lds);
+    }
+    __device__ __forceinline__ void load_values(const Tile& t, int32_t b, int32_t id, uint32_t lds) const
+    {
+        const int32_t rows = rows_of(t, b, id);
+        load_block((const uint16_t*)p.a.v_cache + (rows > 0 ? (int64_t)id * p.a.vs.block : 0) + t.head * p.a.vs.head,
+                   p.a.vs.token, rows, v_at, lds);
+    }
+    // a block in the sequence whose number is outside the cache
+    __device__ __forceinline__ bool bad_block(const Tile& t, int32_t b, int32_t id) const
+    {
+        return (int64_t)b * RK_BLOCK_TOKENS < t.keys_end && (uint32_t)id >= (uint32_t)p.a.n_blocks;
+    }
+    __device__ __forceinline__ void report_bad() const
+    {
+        if ((threadIdx.x & 63) == 0) atomicOr(p.status, RK_DEV_BAD_BLOCK);
+    }
+
+    // piece x of the row's query, its sign turned with the scale's
+    __device__ __forceinline__ u32x4 query(const Tile& t, int32_t r, int32_t piece) const
+    {
+        u32x4 q = {0u, 0u, 0u, 0u};
+        const int32_t tok = r / G;
+        if (tok < t.tokens && 8 * piece < p.a.D) {
+            q = *reinterpret_cast<const u32x4*>((const uint16_t*)p.a.q + (t.token + (int64_t)tok) * p.a.q_token +
+                                                (t.head * G + r % G) * p.a.q_head + 8 * piece);
+            if (p.a.scale < 0.0f) q ^= 0x80008000u;
+        }
+        return q;
+    }
+
+    __device__ __forceinline__ uint16_t* out_row(const Tile& t, int32_t r) const
+    {
+        return (uint16_t*)p.a.out + (t.token + (int64_t)(r / G)) * p.a.out_token + (t.head * G + r % G) * p.a.out_head;
+    }
+    __device__ __forceinline__ void put_lse(const Tile& t, int32_t r, float m, float l) const
+    {
+        if (p.a.lse)
+            p.a.lse[(t.token + (int64_t)(r / G)) * p.a.Hq + t.head * G + r % G] =
+                l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
+    }
+
+    // ---------------------------------------------------------------- up to 128 rows, 32 a wavefront
+    //
+    // Scores are computed transposed, keys x rows: a lane then holds 32 of the 64 scores of one row (lane
+    // % 32) in registers, in the order in which the product with the values takes them: the row of
+    // the value that lane half h multiplies with its j-th weight is the key whose score it holds.
+    __device__ void wide(const Tile& t)
+    {
+        constexpr int KS = DP / 16, DT = DP / 32;
+        const int lane = afresh(threadIdx.x & 63);
+        const int hi = lane >> 5, r = 32 * wave + (lane & 31);
+        u32x4 q[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = query(t, r, 2 * ks + hi);
+        int32_t last = t.keys_end - 1;               // the last position that the row sees
+        if (t.mask) {
+            const int32_t pos = t.pos + r / G;
+            last = pos < last ? pos : last;
+        }
+        const int32_t all_see = t.mask ? (t.pos < t.keys_end - 1 ? t.pos : t.keys_end - 1) : t.keys_end - 1;
+        f32x16 o[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+        float m = -INFINITY, l = 0.0f;               // m: log2 of the weights' common divisor
+        // LDS addresses in a stage, less what the unrolled loops add
+        uint32_t k_read[4], v_read[2];
+        {
+            const uint32_t row = lane & 31;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) k_read[x] = row * kRow + (((2 * x + hi) ^ (row & 7)) << 4);
+            const uint32_t vr = 4 * hi + ((lane & 15) >> 2);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                v_read[x] = vr * kRow + (((4 * x + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ vr) << 4) + 8 * (lane & 1);
+        }
+        constexpr uint32_t kKeys = kWideKeys * kRow, kStage = 2 * kKeys;
+        auto issue = [&](int32_t s, uint32_t stage) {
+            const int32_t b = t.block0 + 4 * s + wave;
+            const int32_t id = __builtin_amdgcn_readfirstlane(block_id(t, b));
+            const uint32_t to = tile + stage * kStage + wave * (RK_BLOCK_TOKENS * kRow);
+            load_keys(t, b, id, to);
+            load_values(t, b, id, to + kKeys);
+        };
+        __syncthreads();                             // the LDS is the last tile's until here
+        issue(t.s0, 0);
+        for (int32_t s = t.s0; s < t.s1; ++s) {
+            const uint32_t at = tile + ((s - t.s0) & 1) * kStage;
+            __builtin_amdgcn_s_waitcnt(0);           // this step's keys and values are there, this wavefront's part
+            __builtin_amdgcn_s_barrier();            // ... everyone's, and the other stage has been read
+            asm volatile("" ::: "memory");
+            if (s + 1 < t.s1) issue(s + 1, (s + 1 - t.s0) & 1);
+            f32x16 sc[2];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                sc[kt] = f32x16{};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    sc[kt] = mfma32<Half>(lds_read16(at + k_read[ks & 3] + (uint32_t)(kt * 32 * kRow + (ks >> 2) * 128)),
+                                          q[ks], sc[kt]);
+            }
+            const int32_t key0 = (t.block0 + 4 * s) * RK_BLOCK_TOKENS;
+            uint32_t bad = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int32_t x = t.block0 + 4 * s + b;
+                if (bad_block(t, x, block_id(t, x))) bad |= 1u << b;
+            }
+            const bool masked = key0 + kWideKeys - 1 > all_see || bad;
+            if (masked) {
+                if (bad) report_bad();
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int x = 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3);
+                        if (key0 + x > last || ((bad >> (x >> 4)) & 1)) sc[kt][i] = -INFINITY;
+                    }
+            }
+            float top = sc[0][0];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kt][i]);
+            // The weights' divisor follows the largest score only when that has left it behind by 2^8: sums
+            // and weights stay far from fp32's and fp16's ends, and the results are seldom rescaled.
+            if (__any(top * c > m + 8.0f)) {
+                top = fmaxf(top, __shfl_xor(top, 32)) * c;
+                const float nm = fmaxf(m, top);
+                const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - nm);
+                m = nm;
+                l *= keep;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= keep;
+            }
+            const float base = m == -INFINITY ? 0.0f : -m;
+            u32x4 w[4];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][i], c, base));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][i + 1], c, base));
+                    sum += x + y;
+                    w[2 * kt + (i >> 3)][(i & 7) >> 1] = pack16<Half>(x, y);
+                }
+                l += sum;
+            }
+            auto values = [&](int d, int kk) {
+                const uint32_t x = at + kKeys + v_read[d & 1] + (uint32_t)((d >> 1) * 128 + 16 * kk * kRow);
+                const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 8 * kRow);
+                return u32x4{lo.x, lo.y, up.x, up.y};
+            };
+            bool odd = false;                        // a value that is not finite where some row does not see it
+            if (masked && t.mask) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) {
+                        const u32x4 v = values(d, kk);
+                        odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
+                    }
+                odd = __any(odd);
+                asm volatile("" ::: "memory");       // (read again below, not kept)
+            }
+            if (!odd) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) o[d] = mfma32<Half>(values(d, kk), w[kk], o[d]);
+            } else {
+                // the finite values by the product, the others one by one, to the rows that see them
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) {
+                        u32x4 v = values(d, kk);
+                        v.x = finite_or_zero<Half>(v.x);
+                        v.y = finite_or_zero<Half>(v.y);
+                        v.z = finite_or_zero<Half>(v.z);
+                        v.w = finite_or_zero<Half>(v.w);
+                        o[d] = mfma32<Half>(v, w[kk], o[d]);
+                    }
+                for (int x = 0; x < kWideKeys; ++x) {
+                    if (key0 + x > last) continue;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const uint32_t piece = (uint32_t)(4 * d + g) ^ (x & 7);
+                            const u32x2 v = lds_read8(at + kKeys + x * kRow + (piece << 4) + 8 * hi);
+                            if (not_finite<Half>(v.x & 0xffffu)) o[d][4 * g] += unpack16<Half>(v.x & 0xffffu);
+                            if (not_finite<Half>(v.x >> 16)) o[d][4 * g + 1] += unpack16<Half>(v.x >> 16);
+                            if (not_finite<Half>(v.y & 0xffffu)) o[d][4 * g + 2] += unpack16<Half>(v.y & 0xffffu);
+                            if (not_finite<Half>(v.y >> 16)) o[d][4 * g + 3] += unpack16<Half>(v.y >> 16);
+                        }
+                }
+            }
+        }
+        l += __shfl_xor(l, 32);
+        if (r >= t.tokens * G) return;
+        if (t.part) {
+            float* to = t.part + (int64_t)r * DP + 4 * hi;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4*>(to + 32 * d + 8 * g) =
+                        f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+            if (hi == 0) {
+                t.part_ml[2 * r] = m;
+                t.part_ml[2 * r + 1] = l;
+            }
+        } else {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            uint16_t* to = out_row(t, r) + 4 * hi;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (32 * d + 8 * g < p.a.D)
+                        *reinterpret_cast<u32x2*>(to + 32 * d + 8 * g) =
+                            u32x2{pack16<Half>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv),
+                                  pack16<Half>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv)};
+            if (hi == 0) put_lse(t, r, m, l);
+        }
+    }
+
+    // ---------------------------------------------------------------- up to 16 NQ rows, 32 keys a wavefront
+    //
+    // What bounds few rows is the reading of keys and values, so each wavefront takes keys of its own, with no
+    // barrier: while it computes on the keys of a step its values are still under way, and the next step's keys
+    // follow as soon as this step's are in registers.  The wavefronts' results are joined through LDS.
+    template <int NQ>
+    __device__ void narrow(const Tile& t)
+    {
+        constexpr int KS = DP / 32, DT = DP / 16;
+        const int lane = afresh(threadIdx.x & 63);
+        const int g = lane >> 4, col = lane & 15;
+        u32x4 q[NQ][KS];
+        int32_t last[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int32_t r = 16 * n + col;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query(t, r, 4 * ks + g);
+            last[n] = t.keys_end - 1;
+            if (t.mask) {
+                const int32_t pos = t.pos + r / G;
+                last[n] = pos < last[n] ? pos : last[n];
+            }
+        }
+        const int32_t all_see = t.mask ? (t.pos < t.keys_end - 1 ? t.pos : t.keys_end - 1) : t.keys_end - 1;
+        f32x4 o[NQ][DT];
+        float m[NQ], l[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[n][d] = f32x4{};
+            m[n] = -INFINITY;
+            l[n] = 0.0f;
+        }
+        uint32_t k_read[2], v_read[4];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) k_read[x] = col * kRow + (((4 * x + g) ^ (col & 7)) << 4);
+        {
+            const uint32_t vr = 4 * g + (col >> 2);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                v_read[x] = vr * kRow + (((2 * x + ((lane & 3) >> 1)) ^ (vr & 7)) << 4) + 8 * (lane & 1);
+        }
+        const uint32_t keys = tile + wave * (64 * kRow), vals = keys + 32 * kRow;
+        // this wavefront's steps: 32 keys at 128 s + 32 wave
+        const int32_t first_block = t.block0 + 2 * wave;
+        int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kNarrowKeys - 1) / kNarrowKeys;
+        s1 = s1 < t.s1 ? s1 : t.s1;
+        int32_t s = t.s0;
+        __syncthreads();                             // the LDS is the last tile's until here
+        int32_t id[2] = {0, 0};
+        auto ids = [&](int32_t x) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) id[b] = __builtin_amdgcn_readfirstlane(block_id(t, first_block + 8 * x + b));
+        };
+        if (s < s1) {
+            ids(s);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) load_keys(t, first_block + 8 * s + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
+#pragma unroll
+            for (int b = 0; b < 2; ++b) load_values(t, first_block + 8 * s + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+        }
+        for (; s < s1; ++s) {
+            const int32_t b0 = first_block + 8 * s, key0 = b0 * RK_BLOCK_TOKENS;
+            const uint32_t bad = (bad_block(t, b0, id[0]) ? 1u : 0u) | (bad_block(t, b0 + 1, id[1]) ? 2u : 0u);
+            const bool more = s + 1 < s1;
+            if (more) ids(s + 1);
+            // (vector memory operations end in the order of their issue: all but the values' loads)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
+            f32x4 sc[NQ][2];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) sc[n][kt] = f32x4{};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const u32x4 k = lds_read16(keys + k_read[ks & 1] + (uint32_t)(kt * 16 * kRow + (ks >> 1) * 128));
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) sc[n][kt] = mfma16<Half>(k, q[n][ks], sc[n][kt]);
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the keys are in registers
+            if (more)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) load_keys(t, b0 + 8 + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
+            const bool masked = key0 + 31 > all_see || bad;
+            u32x4 w[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                if (masked) {
+                    if (bad && n == 0) report_bad();
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
+                }
+                float top = sc[n][0][0];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[n][kt][i]);
+                if (__any(top * c > m[n] + 8.0f)) {
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32)) * c;
+                    const float nm = fmaxf(m[n], top);
+                    const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[n] - nm);
+                    m[n] = nm;
+                    l[n] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+                }
+                const float base = m[n] == -INFINITY ? 0.0f : -m[n];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i], c, base));
+                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i + 1], c, base));
+                        l[n] += x + y;
+                        w[n][2 * kt + (i >> 1)] = pack16<Half>(x, y);
+                    }
+            }
+            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            auto values = [&](int d) {
+                const uint32_t x = vals + v_read[d & 3] + (uint32_t)((d >> 2) * 128);
+                const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
+                return u32x4{lo.x, lo.y, up.x, up.y};
+            };
+            bool odd = false;
+            if (masked && t.mask && t.tokens > 1) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const u32x4 v = values(d);
+                    odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
+                }
+                odd = __any(odd);
+                asm volatile("" ::: "memory");       // (read again below, not kept)
+            }
+            if (!odd) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const u32x4 v = values(d);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    u32x4 v = values(d);
+                    v.x = finite_or_zero<Half>(v.x);
+                    v.y = finite_or_zero<Half>(v.y);
+                    v.z = finite_or_zero<Half>(v.z);
+                    v.w = finite_or_zero<Half>(v.w);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
+                }
+                for (int x = 0; x < 32; ++x)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ (x & 7);
+                        const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) {
+                            if (key0 + x > last[n]) continue;
+                            if (not_finite<Half>(v.x & 0xffffu)) o[n][d][0] += unpack16<Half>(v.x & 0xffffu);
+                            if (not_finite<Half>(v.x >> 16)) o[n][d][1] += unpack16<Half>(v.x >> 16);
+                            if (not_finite<Half>(v.y & 0xffffu)) o[n][d][2] += unpack16<Half>(v.y & 0xffffu);
+                            if (not_finite<Half>(v.y >> 16)) o[n][d][3] += unpack16<Half>(v.y >> 16);
+                        }
+                    }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the values are in registers
+            if (more)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) load_values(t, b0 + 8 + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+        }
+        // the four wavefronts' results: rows of DP floats in LDS, wavefront after wavefront
+        __syncthreads();
+        constexpr int kRows = 16 * NQ;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+            if (g == 0) {
+                join[2 * (wave * kRows + 16 * n + col)] = m[n];
+                join[2 * (wave * kRows + 16 * n + col) + 1] = l[n];
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(
+                    (lds_u8*)(uintptr_t)(tile + 4 * ((wave * kRows + 16 * n + col) * DP + 16 * d + 4 * g))) = o[n][d];
+        }
+        __syncthreads();
+        const int32_t rows = t.tokens * G;
+        for (int x = 64 * wave + lane; x < kRows * (DP / 8); x += kThreads) {
+            const int r = x / (DP / 8), piece = x % (DP / 8);
+            if (r >= rows) continue;
+            float mm[kWaves], nm = -INFINITY, total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) nm = fmaxf(nm, mm[w] = join[2 * (w * kRows + r)]);
+            f32x4 a = {}, b = {};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = mm[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mm[w] - nm);
+                total += f * join[2 * (w * kRows + r) + 1];
+                const uint32_t at = tile + 4 * ((w * kRows + r) * DP + 8 * piece);
+                if (f != 0.0f) {
+                    a += f * *reinterpret_cast<__attribute__((address_space(3))) f32x4*>((lds_u8*)(uintptr_t)at);
+                    b += f * *reinterpret_cast<__attribute__((address_space(3))) f32x4*>((lds_u8*)(uintptr_t)(at + 16));
+                }
+            }
+            if (t.part) {
+                *reinterpret_cast<f32x4*>(t.part + (int64_t)r * DP + 8 * piece) = a;
+                *reinterpret_cast<f32x4*>(t.part + (int64_t)r * DP + 8 * piece + 4) = b;
+                if (piece == 0) {
+                    t.part_ml[2 * r] = nm;
+                    t.part_ml[2 * r + 1] = total;
+                }
+            } else {
+                const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+                if (8 * piece < p.a.D)
+                    *reinterpret_cast<u32x4*>(out_row(t, r) + 8 * piece) =
+                        u32x4{pack16<Half>(a.x * inv, a.y * inv), pack16<Half>(a.z * inv, a.w * inv),
+                              pack16<Half>(b.x * inv, b.y * inv), pack16<Half>(b.z * inv, b.w * inv)};
+                if (piece == 0) put_lse(t, r, nm, total);
+            }
+        }
+    }
+};
+
+// What a workgroup keeps of each request, in LDS.
+struct Request {
+    int32_t kv, q0, tokens;                  // tokens = 0: nothing to do
+    int32_t shared;                          // blocks of the prefix that its group attends to together; 0: none
+    int32_t end;                             // of the first that shares: the group's end; else 0
+    int32_t base;                            // shared tokens before its own
+};
+
+// A segment's extent along the line of work: the tokens of one request over its own keys, or those of a group over
+// its prefix, for one key head.  Wide segments of a request run over tiles whose keys grow with the position,
+// paired first with last so that every pair takes the same.
+struct Segment {
+    int32_t tokens, rows, tiles, per;        // tokens in all, rows in all, tiles, tokens of a tile
+    int32_t steps0, block0;                  // steps of a tile (of the first, where they grow)
+    bool wide, grows;
+    uint64_t pair, cost;                     // cost of a pair (or tile), and in all
+};
+
+__device__ __forceinline__ int32_t steps_for(int64_t keys, int32_t per_step)
+{
+    return keys > 0 ? (int32_t)((keys + per_step - 1) / per_step) : 1;
+}
+
+__device__ __forceinline__ Segment own_segment(const Request& r, int32_t G)
+{
+    Segment s{};
+    s.tokens = r.tokens;
+    s.rows = r.tokens * G;
+    s.block0 = r.shared;
+    s.wide = s.rows > kNarrowRows;
+    s.per = s.wide ? kWideRows / G : s.tokens;
+    if (s.tokens == 0) return s;
+    const int64_t own = (int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS;
+    s.tiles = (s.tokens + s.per - 1) / s.per;
+    if (!s.wide) {
+        s.steps0 = steps_for(own, kNarrowKeys);
+        s.pair = s.cost = (uint64_t)s.steps0 * kNarrowCost;
+    } else if (s.tiles == 1) {
+        s.steps0 = steps_for(own, kWideKeys);
+        s.pair = s.cost = (uint64_t)s.steps0 * kWideCost;
+    } else {
+        s.grows = true;
+        s.steps0 = steps_for(own - s.tokens + s.per, kWideKeys);
+        const int32_t last = steps_for(own - s.tokens + (int64_t)s.tiles * s.per, kWideKeys);
+        s.pair = ((uint64_t)s.steps0 + last + 2) * kWideCost;
+        s.cost = s.pair * ((s.tiles + 1) / 2);
+    }
+    return s;
+}
+
+__device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks, int32_t G)
+{
+    Segment s{};
+    s.tokens = tokens;
+    s.rows = tokens * G;
+    s.wide = s.rows > kNarrowRows;
+    s.per = s.wide ? kWideRows / G : s.tokens;
+    s.tiles = (s.tokens + s.per - 1) / s.per;
+    s.steps0 = steps_for((int64_t)blocks * RK_BLOCK_TOKENS, s.wide ? kWideKeys : kNarrowKeys);
+    s.pair = (uint64_t)s.steps0 * (s.wide ? kWideCost : kNarrowCost);
+    s.cost = s.pair * s.tiles;
+    return s;
+}
+
+__device__ __forceinline__ int32_t last_group(const int32_t* off, int32_t n, int32_t v)
+{
+    int32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (off[mid] <= v) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// One launch over a line of work: request after request (a group's prefix before its first member's own keys), key head
+// after key head, tile after tile, step after step.  The line is cut into equal pieces, a workgroup each, whatever the
+// lengths are; a tile that is cut is joined by the next kernel.
+template <int DP, bool Half>
+__global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs p)
+{
+    extern __shared__ __align__(1024) uint8_t lds[];
+    __shared__ float s_join[2 * kWaves * kNarrowRows];
+    __shared__ uint64_t s_tmp[2 * kWaves], s_off;
+    __shared__ int32_t s_i, s_bad;
+    using A = Attend<DP, Half>;
+    const rk_attention& a = p.a;
+    const int tid = threadIdx.x;
+    const int32_t B = p.n, G = a.Hq / a.Hkv;
+    Request* req = reinterpret_cast<Request*>(lds + A::kTileBytes);
+    int32_t* goff = reinterpret_cast<int32_t*>(lds);                 // until the keys and values come
+    const bool tell = blockIdx.x == 0;
+    if (tid == 0) {
+        s_bad = 0;
+        s_i = B;
+        s_off = 0;
+    }
+    __syncthreads();
+    for (int32_t i = tid; i < B; i += kThreads) {
+        Request r{};
+        const int64_t q0 = a.q_off[p.b0 + i], q1 = a.q_off[p.b0 + i + 1];
+        const int32_t kv = a.kv_len[p.b0 + i];
+        const bool large = (int64_t)kv > (int64_t)a.table_stride * RK_BLOCK_TOKENS;
+        if (q0 < 0 || q1 < q0 || q1 > a.T || q1 - q0 > kv || large) {
+            if (tell) atomicOr(p.status, large ? RK_DEV_TOO_LARGE : RK_DEV_BAD_OFFSETS);
+            r.tokens = -1;
+        } else {
+            r.kv = kv;
+            r.q0 = (int32_t)q0;
+            r.tokens = (int32_t)(q1 - q0);
+        }
+        req[i] = r;
+    }
+    if (a.group_off)
+        for (int32_t g = tid; g < a.B; g += kThreads) {
+            const int64_t x = a.group_off[g], y = a.group_off[g + 1];
+            if (x > y || x < 0 || y > a.B || (g == 0 && x != 0) || (g == a.B - 1 && y != a.B)) s_bad = 1;
+            goff[g] = (int32_t)x;
+            if (g == a.B - 1) goff[a.B] = (int32_t)y;
+        }
+    __syncthreads();
+    const bool groups = a.group_off && !s_bad;
+    if (tell && tid == 0 && s_bad) atomicOr(p.status, RK_DEV_BAD_OFFSETS);
+    if (groups) {
+        // A group attends to its prefix together where every member sees all of it; if only the first
+        // does not (it brings the prefix), the others do.  (Members in another launch are a group of their own.)
+        struct Members {
+            int32_t lent, first, end;
+            bool whole;                      // the group's first request is among them
+        };
+        auto members = [&](int32_t i) {
+            const int32_t g = last_group(goff, a.B, p.b0 + i), f = goff[g];
+            Members m;
+            m.whole = f >= p.b0;
+            m.first = m.whole ? f - p.b0 : 0;
+            m.end = goff[g + 1] - p.b0 < B ? goff[g + 1] - p.b0 : B;
+            m.lent = 0;
+            if (m.end - m.first >= 2) {
+                const int32_t most = a.kv_len[f] / RK_BLOCK_TOKENS, sh = a.shared[g];
+                m.lent = sh < most ? sh : most;
+            }
+            return m;
+        };
+        for (int32_t i = tid; i < B; i += kThreads) {
+            const Members m = members(i);
+            const int32_t tokens = req[i].tokens;
+            if (m.lent > 0 && (tokens < 0 || (tokens > 0 && req[i].kv - tokens < m.lent * RK_BLOCK_TOKENS - 1)))
+                atomicOr(&req[m.first].base, i == m.first && m.whole ? 1 : 2);       // (base is not needed yet)
+        }
+        __syncthreads();
+        for (int32_t i = tid; i < B; i += kThreads) {
+            const Members m = members(i);
+            if (m.lent < kShareBlocks) continue;
+            const int32_t broken = req[m.first].base, f = m.first + (broken & 1);
+            if (m.end - f < 2 || (broken & 2) || i < f) continue;
+            // together where most members have fewer rows than a wide tile
+            const int64_t rows = (int64_t)(req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0) * G;
+            if (rows == 0 || rows >= (int64_t)kWideRows * (m.end - f)) continue;
+            req[i].shared = m.lent;
+            if (i == f) req[i].end = m.end;
+        }
+        __syncthreads();
+    }
+    // the line of work: per thread's requests, then over the threads
+    const int32_t per = (B + kThreads - 1) / kThreads;
+    const int32_t i0 = tid * per, i1 = i0 + per < B ? i0 + per : B;
+    uint64_t mine = 0;
+    uint32_t together = 0;
+    auto prefix_of = [&](int32_t i) {
+        const Request& l = req[req[i].end - 1];
+        return prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G);
+    };
+    for (int32_t i = i0; i < i1; ++i) {
+        if (req[i].tokens < 0) req[i].tokens = 0;
+        if (req[i].shared) together += req[i].tokens;
+    }
+    __syncthreads();
+    for (int32_t i = i0; i < i1; ++i) {
+        mine += own_segment(req[i], G).cost;
+        if (req[i].end) mine += prefix_of(i).cost;
+    }
+    mine *= (uint64_t)a.Hkv;
+    uint64_t upto = mine;
+    uint32_t tokens_upto = together;
+    incl_sums(upto, tokens_upto, s_tmp);
+    uint64_t total = 0;
+    for (int w = 0; w < kWaves; ++w) total += s_tmp[w];
+    // (sums of the wavefronts)
+    const uint64_t grid = gridDim.x;
+    total = uniform(total);
+    uint64_t each = (total + grid - 1) / grid;
+    if (each < kLeast) each = kLeast;
+    const uint32_t active = (uint32_t)((total + each - 1) / each);
+    // workgroups go to the 8 XCDs in turn: each XCD takes a stretch of the line
+    const uint32_t wg = (blockIdx.x & 7u) * ((active + 7) / 8) + (blockIdx.x >> 3);
+    const bool idle = (blockIdx.x >> 3) >= (active + 7) / 8 || wg >= active;
+    const uint64_t from = (uint64_t)wg * each, to = from + each < total ? from + each : total;
+    {
+        uint32_t tok = tokens_upto - together;
+        uint64_t x = upto - mine;
+        for (int32_t i = i0; i < i1; ++i) {
+            req[i].base = (int32_t)tok;
+            if (req[i].shared) tok += req[i].tokens;
+            if (tell) p.share_base[i] = req[i].shared && req[i].tokens ? req[i].base : -1;
+            uint64_t w = own_segment(req[i], G).cost;
+            if (req[i].end) w += prefix_of(i).cost;
+            w *= (uint64_t)a.Hkv;
+            if (!idle && from >= x && from < x + w) {
+                s_i = i;
+                s_off = from - x;
+            }
+            x += w;
+        }
+    }
+    __syncthreads();
+    if (tid == 0) p.split[blockIdx.x].n = 0;
+    if (idle) return;
+    float c = fabsf(a.scale) * kLog2e;
+    if (c < 1e-30f) c = 1e-30f;              // scores of 0, and -infinity stays what it is
+    A work(p, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds, s_join, c);
+    int32_t i = uniform(s_i);
+    uint64_t x = from;
+    uint64_t off = uniform(s_off);           // x's place in request i's part of the line
+    while (x < to && i < B) {
+        Request r = req[i];
+        r.kv = uniform(r.kv);
+        r.q0 = uniform(r.q0);
+        r.tokens = uniform(r.tokens);
+        r.shared = uniform(r.shared);
+        r.end = uniform(r.end);
+        r.base = uniform(r.base);
+        Segment sg;
+        bool prefix = false;
+        uint64_t before = 0;
+        if (r.end) {
+            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, G);
+            before = sg.cost * (uint64_t)a.Hkv;
+            prefix = off < before;
+        }
+        if (!prefix) {
+            sg = own_segment(r, G);
+            off -= before;
+            if (sg.cost == 0 || off >= sg.cost * (uint64_t)a.Hkv) {        // on to the next request
+                off -= sg.cost * (uint64_t)a.Hkv;
+                ++i;
+                continue;
+            }
+        }
+        const int32_t head = (int32_t)(off / sg.cost);
+        uint64_t in = off - (uint64_t)head * sg.cost;              // place in the head's part
+        int32_t j = (int32_t)(in / sg.pair);
+        in -= (uint64_t)j * sg.pair;
+        int32_t steps = sg.steps0;
+        uint64_t left = sg.pair;             // cost from the tile's start to the next tile's
+        const uint32_t cost = sg.wide ? kWideCost : kNarrowCost;
+        bool nothing = false;
+        if (sg.grows) {
+            auto steps_of = [&](int32_t k) {
+                const int64_t seen = (int64_t)(k + 1) * sg.per < sg.tokens ? (int64_t)(k + 1) * sg.per : sg.tokens;
+                return steps_for((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWideKeys);
+            };
+            const int32_t k = sg.tiles - 1 - j;
+            const uint64_t head_cost = (uint64_t)steps_of(j) * cost;
+            steps = steps_of(j);
+            left = head_cost;
+            if (in >= head_cost) {           // the pair's other tile
+                in -= head_cost;
+                left = sg.pair - head_cost;
+                nothing = k == j;
+                j = k;
+                steps = steps_of(k);
+            }
+        }
+        // the steps of the tile that begin in [from, to)
+        const uint64_t room = to - x + in;
+        int32_t s0 = (int32_t)((in + cost - 1) / cost), s1 = (int32_t)((room + cost - 1) / cost < (uint64_t)steps ? (room + cost - 1) / cost : steps);
+        if (!nothing && s0 < s1) {
+            Tile t;
+            t.token = r.q0 + j * sg.per;
+            t.tokens = sg.tokens - j * sg.per < sg.per ? sg.tokens - j * sg.per : sg.per;
+            t.head = head;
+            t.s0 = s0;
+            t.s1 = s1;
+            t.n_steps = steps;
+            t.mask = !prefix;
+            t.row = a.tables + (int64_t)(p.b0 + i) * a.table_stride;
+            if (prefix) {
+                t.block0 = 0;
+                t.keys_end = r.shared * RK_BLOCK_TOKENS;
+                t.pos = 0;
+            } else {
+                t.block0 = r.shared;
+                t.pos = r.kv - r.tokens + j * sg.per;
+                t.keys_end = t.pos + t.tokens;
+            }
+            const bool whole = s0 == 0 && s1 == steps, joined = r.shared != 0;
+            // workgroups that the tile's steps fall to: its last step begins at cost (steps - 1) behind its start
+            const uint64_t start = x - in;
+            const int32_t n = (int32_t)((start + (uint64_t)(steps - 1) * cost) / each) - (int32_t)wg + 1;
+            t.part = t.part_ml = nullptr;
+            const int kind = prefix ? 0 : 1;
+            if (!whole) {
+                const int64_t slot = 2 * (int64_t)wg + (s0 == 0 ? 1 : 0);
+                t.part = p.part + slot * kWideRows * DP;
+                t.part_ml = p.part_ml + slot * kWideRows * 2;
+            } else if (joined) {
+                const int64_t row = ((int64_t)kind * a.Hkv + head) * p.shared_rows + (int64_t)(r.base + j * sg.per) * G;
+                t.part = p.whole + row * DP;
+                t.part_ml = p.whole_ml + row * 2;
+            }
+            if (s0 == 0) {
+                if (joined) {
+                    for (int32_t k = tid; k < t.tokens; k += kThreads)
+                        p.parts[((int64_t)kind * a.Hkv + head) * p.shared_tokens + r.base + j * sg.per + k] =
+                            Parts{whole ? 0 : n, (int32_t)wg, k * G, 0};
+                } else if (!whole && tid == 0) {
+                    p.split[blockIdx.x] = Split{n, (int32_t)wg, t.token, t.tokens, head, {0, 0, 0}};
+                }
+            }
+            if (sg.wide) work.wide(t);
+            else if (sg.rows <= 16) work.template narrow<1>(t);
+            else work.template narrow<2>(t);
+        }
+        x += left - in;
+        off += left - in + (prefix ? 0 : before);
+    }
+}
+
+// The parts of rows that more than one workgroup worked on, joined: a wavefront a row, a lane every 64th value.
+template <int DP, bool Half>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks)
 {
     const rk_attention& a = p.a;
-    const int lane = threadIdx.x;
-    const int32_t h = (int32_t)blockIdx.y, hk = h / (a.Hq / a.Hkv);
-    const int64_t t = blockIdx.x;
-    int32_t i = -1;
-    for (int32_t x = lane; x < a.B; x += 64) {
-        const int64_t x0 = a.q_off[x], x1 = a.q_off[x + 1];
-        if (x0 < 0 || x1 < x0 || x1 > a.T) atomicOr(p.status, RK_DEV_BAD_OFFSETS);
-        else if (x0 <= t && t < x1) i = x;
-    }
-    if (a.group_off && t == 0 && h == 0)
-        for (int32_t x = lane; x < a.B; x += 64)
-            if (a.group_off[x] < 0 || a.group_off[x] > a.group_off[x + 1] || (x == 0 && a.group_off[x] != 0) ||
-                (x == a.B - 1 && a.group_off[x + 1] != a.B))
-                atomicOr(p.status, RK_DEV_BAD_OFFSETS);
-    const uint64_t m = __ballot(i >= 0);
-    if (m == 0ull) return;
-    i = __builtin_amdgcn_readlane(i, __ffsll((unsigned long long)m) - 1);
-    const int64_t q0 = a.q_off[i], q1 = a.q_off[i + 1];
-    const int32_t kv = a.kv_len[i];
-    const bool large = kv > (int64_t)a.table_stride * RK_BLOCK_TOKENS;
-    if (q1 - q0 > kv || large) {
-        if (lane == 0) atomicOr(p.status, large ? RK_DEV_TOO_LARGE : RK_DEV_BAD_OFFSETS);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int32_t G = a.Hq / a.Hkv;
+    constexpr int N = DP / 64;
+    auto put = [&](int64_t token, int32_t h, const float* o, float m, float l) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t* to = (uint16_t*)a.out + token * a.out_token + h * a.out_head;
+#pragma unroll
+        for (int x = 0; x < N; ++x)
+            if (64 * x + lane < a.D) to[64 * x + lane] = (uint16_t)pack16<Half>(o[x] * inv, 0.0f);
+        if (lane == 0 && a.lse) a.lse[token * a.Hq + h] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
+    };
+    // n parts of a row: the tail of workgroup wg's work, then the heads of those after it
+    auto slot = [&](int32_t wg, int32_t k) { return 2 * (int64_t)(wg + k) + (k == 0 ? 1 : 0); };
+    auto add = [&](float* o, float& m, float& l, const float* part, const float* ml) {
+        const float pm = ml[0], nm = fmaxf(m, pm);
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - nm);
+        const float g = pm == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(pm - nm);
+        l = l * f + ml[1] * g;
+#pragma unroll
+        for (int x = 0; x < N; ++x) o[x] = (f == 0.0f ? 0.0f : o[x] * f) + (g == 0.0f ? 0.0f : part[64 * x + lane] * g);
+        m = nm;
+    };
+    if ((int32_t)blockIdx.x < grid * chunks) {
+        const Split s = p.split[blockIdx.x / chunks];
+        const int32_t rows = s.tokens * G;
+        if (s.n == 0) return;
+        for (int32_t r = (int32_t)(blockIdx.x % chunks) * kWaves + wave; r < rows; r += chunks * kWaves) {
+            float o[N] = {}, m = -INFINITY, l = 0.0f;
+            for (int32_t k = 0; k < s.n; ++k) {
+                const int64_t row = slot(s.wg, k) * kWideRows + r;
+                add(o, m, l, p.part + row * DP, p.part_ml + row * 2);
+            }
+            put(s.token + (int64_t)(r / G), s.head * G + r % G, o, m, l);
+        }
         return;
     }
-    const int32_t pos = kv - (int32_t)(q1 - q0) + (int32_t)(t - q0);
-    const uint16_t* q = (const uint16_t*)a.q + t * a.q_token + h * a.q_head;
-    float qf[4] = {}, o[4] = {}, mx = -INFINITY, l = 0.0f;
-    for (int c = 0; c < 4; ++c)
-        if (4 * lane + c < a.D) qf[c] = to_float<Half>(q[4 * lane + c]);
-    for (int32_t j = 0; j <= pos; ++j) {
-        const int32_t b = a.tables[(int64_t)i * a.table_stride + j / RK_BLOCK_TOKENS];
-        if (b < 0 || b >= a.n_blocks) {
-            if (lane == 0) atomicOr(p.status, RK_DEV_BAD_BLOCK);
-            continue;
+    // a request whose group attends to its prefix together
+    const int32_t b = (int32_t)blockIdx.x - grid * chunks, i = b / a.Hkv, head = b % a.Hkv;
+    const int32_t base = p.share_base[i];
+    if (base < 0) return;
+    const int64_t q0 = a.q_off[p.b0 + i];
+    const int32_t rows = (int32_t)(a.q_off[p.b0 + i + 1] - q0) * G;
+    for (int32_t r = wave; r < rows; r += kWaves) {
+        const int32_t tok = r / G, h = r % G;
+        float o[N] = {}, m = -INFINITY, l = 0.0f;
+        for (int kind = 0; kind < 2; ++kind) {
+            const int64_t at = (int64_t)kind * a.Hkv + head;
+            const Parts s = p.parts[at * p.shared_tokens + base + tok];
+            if (s.n == 0) {
+                const int64_t row = at * p.shared_rows + (int64_t)base * G + r;
+                add(o, m, l, p.whole + row * DP, p.whole_ml + row * 2);
+            }
+            for (int32_t k = 0; k < s.n; ++k) {
+                const int64_t row = slot(s.wg, k) * kWideRows + s.row + h;
+                add(o, m, l, p.part + row * DP, p.part_ml + row * 2);
+            }
         }
-        const uint16_t* k = (const uint16_t*)a.k_cache + b * a.ks.block + (j % RK_BLOCK_TOKENS) * a.ks.token + hk * a.ks.head;
-        const uint16_t* v = (const uint16_t*)a.v_cache + b * a.vs.block + (j % RK_BLOCK_TOKENS) * a.vs.token + hk * a.vs.head;
-        float s = 0.0f;
-        for (int c = 0; c < 4; ++c)
-            if (4 * lane + c < a.D) s += qf[c] * to_float<Half>(k[4 * lane + c]);
-        for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
-        s *= a.scale;
-        const float nm = fmaxf(mx, s), w = expf(s - nm), keep = expf(mx - nm);
-        l = l * keep + w;
-        for (int c = 0; c < 4; ++c)
-            if (4 * lane + c < a.D) o[c] = o[c] * keep + w * to_float<Half>(v[4 * lane + c]);
-        mx = nm;
+        put(q0 + tok, head * G + h, o, m, l);
     }
-    uint16_t* out = (uint16_t*)a.out + t * a.out_token + h * a.out_head;
-    for (int c = 0; c < 4; ++c)
-        if (4 * lane + c < a.D) out[4 * lane + c] = from_float<Half>(l > 0.0f ? o[c] / l : 0.0f);
-    if (a.lse && lane == 0) a.lse[t * a.Hq + h] = l > 0.0f ? mx + logf(l) : -INFINITY;
+}
+
+// ---------------------------------------------------------------- host
+
+inline int head_size(int32_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 192 ? 192 : 256; }
+
+// requests of a launch: their places along the line of work are kept in LDS
+constexpr int32_t kLaunch = 1024;
+inline int32_t launch_size(int32_t B) { return B < kLaunch ? B : kLaunch; }
+
+inline size_t lds_bytes(int dp, int32_t n) { return (size_t)512 * dp + sizeof(Request) * (size_t)n; }
+
+// Workgroups that the device holds at once.
+inline int32_t grid_for(int dp, int32_t n)
+{
+    const int32_t cus = compute_units();
+    const int fit = dp <= 128 && lds_bytes(dp, n) + 4096 <= (160u << 10) / 2 ? 2 : 1;
+    return ((cus > 0 ? cus : 256) * fit + 7) / 8 * 8;
+}
+
+struct AttendLayout {
+    size_t split, share_base, parts, part, part_ml, whole, whole_ml, bytes;
+    int32_t grid, shared_rows, shared_tokens;
+};
+
+inline AttendLayout attend_layout(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D)
+{
+    AttendLayout L;
+    const int dp = head_size(D);
+    const int32_t G = Hq / Hkv, n = launch_size(B);
+    L.grid = grid_for(dp, n);
+    // rows of groups that attend together: fewer than a wide tile's for each member
+    const int64_t most = (int64_t)kWideRows * n / G, tokens = T < most ? T : most;
+    L.shared_tokens = (int32_t)tokens;
+    L.shared_rows = (int32_t)(tokens * G);
+    size_t o = 0;
+    auto take = [&](size_t n) {
+        const size_t at = o;
+        o = align_up(o + n, 256);
+        return at;
+    };
+    L.split = take(sizeof(Split) * (size_t)L.grid);
+    L.share_base = take(4 * (size_t)n);
+    L.parts = take(sizeof(Parts) * 2 * (size_t)Hkv * L.shared_tokens);
+    L.part_ml = take(4 * 2 * (size_t)kWideRows * 2 * L.grid);
+    L.part = take(4 * (size_t)dp * kWideRows * 2 * L.grid);
+    L.whole_ml = take(4 * 2 * 2 * (size_t)Hkv * L.shared_rows);
+    L.whole = take(4 * (size_t)dp * 2 * (size_t)Hkv * L.shared_rows);
+    L.bytes = o;
+    return L;
+}
+
+template <int DP, bool Half>
+static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
+{
+    const int64_t rows = p.a.T * (p.a.Hq / p.a.Hkv);
+    const int32_t chunks = rows <= 4 ? 1 : rows <= 32 ? 4 : 8;
+    for (p.b0 = 0; p.b0 < p.a.B; p.b0 += p.n) {
+        p.n = launch_size(p.a.B - p.b0);
+        hipLaunchKernelGGL((attend_kernel<DP, Half>), dim3((unsigned)grid), dim3(kThreads), lds_bytes(DP, p.n), s, p);
+        int rc = hip_check(hipGetLastError(), "rk_prefix_attention launch");
+        if (rc) return rc;
+        const int64_t blocks = (int64_t)grid * chunks + (p.a.group_off ? (int64_t)p.n * p.a.Hkv : 0);
+        hipLaunchKernelGGL((join_kernel<DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, grid, chunks);
+        rc = hip_check(hipGetLastError(), "rk_prefix_attention join launch");
+        if (rc) return rc;
+    }
+    return RK_OK;
+}
+
+template <bool Half>
+static int launch_of(AttendArgs& p, int32_t grid, hipStream_t s)
+{
+    switch (head_size(p.a.D)) {
+    case 64: return launch<64, Half>(p, grid, s);
+    case 128: return launch<128, Half>(p, grid, s);
+    case 192: return launch<192, Half>(p, grid, s);
+    default: return launch<256, Half>(p, grid, s);
+    }
 }
 
 }  // namespace rk
@@ -112,7 +1202,7 @@ size_t rk_prefix_attention_workspace_size(int64_t T, int32_t B, int32_t Hq, int3
 {
     int rc;
     if (attention_sizes(T, B, Hq, Hkv, D, &rc)) return 0;
-    return 256;
+    return attend_layout(T, B, Hq, Hkv, D).bytes;
 }
 
 int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes, void* stream)
@@ -123,7 +1213,7 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
         return fail(rc, "rk_prefix_attention: %s", what);
     if (a->dtype != RK_BF16 && a->dtype != RK_F16) return fail(RK_EUNSUPPORTED, "rk_prefix_attention: dtype %d", a->dtype);
     if (a->n_blocks < 0 || a->table_stride < 0) return fail(RK_EINVAL, "rk_prefix_attention: a negative size");
-    if (!(fabsf(a->scale) <= 3.0e38f)) return fail(RK_EINVAL, "rk_prefix_attention: scale is not finite");
+    if (!(fabsf(a->scale) <= 1e18f)) return fail(RK_EINVAL, "rk_prefix_attention: scale outside -1e18..1e18");
     const int64_t strides[] = {a->q_token, a->q_head, a->out_token, a->out_head, a->ks.block, a->ks.token, a->ks.head,
                                a->vs.block, a->vs.token, a->vs.head};
     for (int64_t x : strides)
@@ -138,18 +1228,25 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
         return fail(RK_EINVAL, "rk_prefix_attention: NULL array");
     if (((uintptr_t)a->q | (uintptr_t)a->out | (uintptr_t)a->k_cache | (uintptr_t)a->v_cache) % 16)
         return fail(RK_EINVAL, "rk_prefix_attention: an array is not aligned to 16 bytes");
-    const size_t need = rk_prefix_attention_workspace_size(a->T, a->B, a->Hq, a->Hkv, a->D);
-    if (!workspace || ws_bytes < need)
-        return fail(RK_ENOMEM, "rk_prefix_attention: workspace of %zu bytes, %zu needed", workspace ? ws_bytes : (size_t)0, need);
+    const AttendLayout L = attend_layout(a->T, a->B, a->Hq, a->Hkv, a->D);
+    if (!workspace || ws_bytes < L.bytes)
+        return fail(RK_ENOMEM, "rk_prefix_attention: workspace of %zu bytes, %zu needed", workspace ? ws_bytes : (size_t)0, L.bytes);
     if ((uintptr_t)workspace % 256) return fail(RK_EINVAL, "rk_prefix_attention: workspace is not aligned to 256 bytes");
+    uint8_t* ws = (uint8_t*)workspace;
     AttendArgs p;
     p.a = *a;
     p.status = status_word();
     if (!p.status) return fail(RK_EHIP, "rk_prefix_attention: no status word");
-    const dim3 grid((unsigned)a->T, (unsigned)a->Hq);
-    if (a->dtype == RK_F16) hipLaunchKernelGGL(attend_plain_kernel<true>, grid, dim3(64), 0, (hipStream_t)stream, p);
-    else hipLaunchKernelGGL(attend_plain_kernel<false>, grid, dim3(64), 0, (hipStream_t)stream, p);
-    return hip_check(hipGetLastError(), "rk_prefix_attention launch");
+    p.split = (Split*)(ws + L.split);
+    p.share_base = (int32_t*)(ws + L.share_base);
+    p.parts = (Parts*)(ws + L.parts);
+    p.part = (float*)(ws + L.part);
+    p.part_ml = (float*)(ws + L.part_ml);
+    p.whole = (float*)(ws + L.whole);
+    p.whole_ml = (float*)(ws + L.whole_ml);
+    p.shared_rows = L.shared_rows;
+    p.shared_tokens = L.shared_tokens;
+    return a->dtype == RK_F16 ? launch_of<true>(p, L.grid, (hipStream_t)stream) : launch_of<false>(p, L.grid, (hipStream_t)stream);
 }
 
 }  // extern "C"
