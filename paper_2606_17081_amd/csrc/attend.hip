@@ -137,44 +137,55 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x)
            (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)x);
 }
 
-// The workgroup's inclusive sums; tmp: 2 * kWaves words.
-__device__ __forceinline__ void incl_sums(uint64_t& x, uint32_t& y, uint64_t* tmp)
+// The workgroup's inclusive sums; tmp: 3 * kWaves words, the wavefronts' sums afterwards.
+__device__ __forceinline__ void incl_sums(uint64_t& x, uint64_t& y, uint32_t& z, uint64_t* tmp)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t ox = __shfl_up(x, d);
-        const uint32_t oy = __shfl_up(y, d);
+        const uint64_t ox = __shfl_up(x, d), oy = __shfl_up(y, d);
+        const uint32_t oz = __shfl_up(z, d);
         if (lane >= d) {
             x += ox;
             y += oy;
+            z += oz;
         }
     }
     if (lane == 63) {
         tmp[wave] = x;
         tmp[kWaves + wave] = y;
+        tmp[2 * kWaves + wave] = z;
     }
     __syncthreads();
     for (int w = 0; w < wave; ++w) {
         x += tmp[w];
-        y += (uint32_t)tmp[kWaves + w];
+        y += tmp[kWaves + w];
+        z += (uint32_t)tmp[2 * kWaves + w];
     }
 }
 
+// a / b, mostly of numbers below 2^32
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b)
+{
+    return ((a | b) >> 32) == 0 ? (uint64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+__device__ __forceinline__ uint64_t quotient_up(uint64_t a, uint64_t b) { return quotient(a + b - 1, b); }
+
 // One tile's work: rows of the tokens [token, token + tokens) on key head `head`, steps [s0, s1) of n_steps.
 struct Tile {
-    const int32_t* row;                      // the block table's row
+    const __attribute__((address_space(4))) int32_t* row;        // the block table's row
     int32_t block0;                          // first block of the segment
     int32_t keys_end;                        // first position that no row sees
     int32_t token, tokens, pos;              // of the first row's token
     int32_t head;
-    int32_t s0, s1, n_steps;
+    int32_t s0, s1;
     bool mask;                               // rows see up to their own position (else up to keys_end)
     float *part, *part_ml;                   // where the result goes; NULL: to out and lse
 };
 
 template <int DP, bool Half>
 struct Attend {
+    static constexpr int kHead = DP;
     static constexpr int NC = DP / 8;                 // 16-byte pieces of a row
     static constexpr int NI = NC / 4;                 // loads of 64 pieces that bring a block
     static constexpr uint32_t kRow = DP * 2;          // bytes of a row in LDS
@@ -228,9 +239,11 @@ struct Attend {
     }
 
     // Block number `b`'s block of the segment's sequence, keys to k_lds, values to v_lds (either may be left out).
+    // (read by scalar loads, whose wait is not the one of the keys and values under way)
     __device__ __forceinline__ int32_t block_id(const Tile& t, int32_t b) const
     {
-        return (int64_t)b * RK_BLOCK_TOKENS < t.keys_end ? t.row[b] : 0;
+        const int32_t last = (t.keys_end - 1) / RK_BLOCK_TOKENS;
+        return t.row[b < last ? b : last];
     }
     __device__ __forceinline__ int32_t rows_of(const Tile& t, int32_t b, int32_t id) const
     {
@@ -318,22 +331,8 @@ struct Attend {
                 v_read[x] = vr * kRow + (((4 * x + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ vr) << 4) + 8 * (lane & 1);
         }
         constexpr uint32_t kKeys = kWideKeys * kRow, kStage = 2 * kKeys;
-        auto issue = [&](int32_t s, uint32_t stage) {
-            const int32_t b = t.block0 + 4 * s + wave;
-            const int32_t id = __builtin_amdgcn_readfirstlane(block_id(t, b));
-            const uint32_t to = tile + stage * kStage + wave * (RK_BLOCK_TOKENS * kRow);
-            load_keys(t, b, id, to);
-            load_values(t, b, id, to + kKeys);
-        };
-        __syncthreads();                             // the LDS is the last tile's until here
-        issue(t.s0, 0);
-        for (int32_t s = t.s0; s < t.s1; ++s) {
-            const uint32_t at = tile + ((s - t.s0) & 1) * kStage;
-            __builtin_amdgcn_s_waitcnt(0);           // this step's keys and values are there, this wavefront's part
-            __builtin_amdgcn_s_barrier();            // ... everyone's, and the other stage has been read
-            asm volatile("" ::: "memory");
-            if (s + 1 < t.s1) issue(s + 1, (s + 1 - t.s0) & 1);
-            f32x16 sc[2];
+        // One step: keys and values of step s in the stage at `at`.
+        auto scores = [&](uint32_t at, f32x16* sc) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
                 sc[kt] = f32x16{};
@@ -342,24 +341,8 @@ struct Attend {
                     sc[kt] = mfma32<Half>(lds_read16(at + k_read[ks & 3] + (uint32_t)(kt * 32 * kRow + (ks >> 2) * 128)),
                                           q[ks], sc[kt]);
             }
-            const int32_t key0 = (t.block0 + 4 * s) * RK_BLOCK_TOKENS;
-            uint32_t bad = 0;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int32_t x = t.block0 + 4 * s + b;
-                if (bad_block(t, x, block_id(t, x))) bad |= 1u << b;
-            }
-            const bool masked = key0 + kWideKeys - 1 > all_see || bad;
-            if (masked) {
-                if (bad) report_bad();
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int x = 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3);
-                        if (key0 + x > last || ((bad >> (x >> 4)) & 1)) sc[kt][i] = -INFINITY;
-                    }
-            }
+        };
+        auto weights = [&](const f32x16* sc, u32x4* w) {
             float top = sc[0][0];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
@@ -379,7 +362,6 @@ struct Attend {
                     for (int i = 0; i < 16; ++i) o[d][i] *= keep;
             }
             const float base = m == -INFINITY ? 0.0f : -m;
-            u32x4 w[4];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
                 float sum = 0.0f;
@@ -392,55 +374,111 @@ struct Attend {
                 }
                 l += sum;
             }
-            auto values = [&](int d, int kk) {
-                const uint32_t x = at + kKeys + v_read[d & 1] + (uint32_t)((d >> 1) * 128 + 16 * kk * kRow);
-                const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 8 * kRow);
-                return u32x4{lo.x, lo.y, up.x, up.y};
-            };
-            bool odd = false;                        // a value that is not finite where some row does not see it
-            if (masked && t.mask) {
+        };
+        auto values = [&](uint32_t at, int d, int kk) {
+            const uint32_t x = at + kKeys + v_read[d & 1] + (uint32_t)((d >> 1) * 128 + 16 * kk * kRow);
+            const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 8 * kRow);
+            return u32x4{lo.x, lo.y, up.x, up.y};
+        };
+        int32_t s = t.s0, id[4];
+        auto ids = [&](int32_t x) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) id[b] = block_id(t, t.block0 + 4 * x + b);
+        };
+        uint32_t bad, next_bad = 0;                  // of the step's four blocks, those outside the cache
+        auto issue = [&](int32_t x) {
+            const int32_t b = t.block0 + 4 * x + wave;
+            const int32_t mine = wave == 0 ? id[0] : wave == 1 ? id[1] : wave == 2 ? id[2] : id[3];
+            const uint32_t to = tile + ((x - t.s0) & 1) * kStage + wave * (RK_BLOCK_TOKENS * kRow);
+            load_keys(t, b, mine, to);
+            load_values(t, b, mine, to + kKeys);
+            next_bad = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (bad_block(t, t.block0 + 4 * x + k, id[k])) next_bad |= 1u << k;
+        };
+        auto arrive = [&]() {                        // step s is there; the next one's loads begin
+            bad = next_bad;
+            __builtin_amdgcn_s_waitcnt(0);           // this wavefront's part of the step has come
+            __builtin_amdgcn_s_barrier();            // ... everyone's, and everyone has read the other stage
+            asm volatile("" ::: "memory");
+            if (s + 1 < t.s1) {
+                issue(s + 1);
+                ids(s + 2);
+            }
+            return tile + ((s - t.s0) & 1) * kStage;
+        };
+        __syncthreads();                             // the LDS is the last tile's until here
+        ids(s);
+        issue(s);
+        ids(s + 1);
+        // the steps whose keys every row sees, if their blocks are good
+        const int32_t open = (all_see + 1 - t.block0 * RK_BLOCK_TOKENS) / kWideKeys, s_open = open < t.s1 ? open : t.s1;
+        for (; s < s_open && !next_bad; ++s) {
+            const uint32_t at = arrive();
+            f32x16 sc[2];
+            u32x4 w[4];
+            scores(at, sc);
+            weights(sc, w);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) o[d] = mfma32<Half>(values(at, d, kk), w[kk], o[d]);
+        }
+        for (; s < t.s1; ++s) {
+            const uint32_t at = arrive();
+            const int32_t key0 = (t.block0 + 4 * s) * RK_BLOCK_TOKENS;
+            f32x16 sc[2];
+            u32x4 w[4];
+            scores(at, sc);
+            if (bad) report_bad();
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int x = 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3);
+                    if (key0 + x > last || ((bad >> (x >> 4)) & 1)) sc[kt][i] = -INFINITY;
+                }
+            weights(sc, w);
+            // A value that is not finite, where some row does not see it, must not meet that row's weight of 0: the
+            // finite values go through the product, the others one by one to the rows that see them.
+            bool odd = false;
+            if (t.mask)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) {
-                        const u32x4 v = values(d, kk);
+                        const u32x4 v = values(at, d, kk);
                         odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
                     }
-                odd = __any(odd);
-                asm volatile("" ::: "memory");       // (read again below, not kept)
-            }
-            if (!odd) {
+            odd = __any(odd);
+            asm volatile("" ::: "memory");           // (read again below, not kept)
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) o[d] = mfma32<Half>(values(d, kk), w[kk], o[d]);
-            } else {
-                // the finite values by the product, the others one by one, to the rows that see them
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        u32x4 v = values(d, kk);
+                for (int kk = 0; kk < 4; ++kk) {
+                    u32x4 v = values(at, d, kk);
+                    if (odd) {
                         v.x = finite_or_zero<Half>(v.x);
                         v.y = finite_or_zero<Half>(v.y);
                         v.z = finite_or_zero<Half>(v.z);
                         v.w = finite_or_zero<Half>(v.w);
-                        o[d] = mfma32<Half>(v, w[kk], o[d]);
                     }
-                for (int x = 0; x < kWideKeys; ++x) {
-                    if (key0 + x > last) continue;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const uint32_t piece = (uint32_t)(4 * d + g) ^ (x & 7);
-                            const u32x2 v = lds_read8(at + kKeys + x * kRow + (piece << 4) + 8 * hi);
-                            if (not_finite<Half>(v.x & 0xffffu)) o[d][4 * g] += unpack16<Half>(v.x & 0xffffu);
-                            if (not_finite<Half>(v.x >> 16)) o[d][4 * g + 1] += unpack16<Half>(v.x >> 16);
-                            if (not_finite<Half>(v.y & 0xffffu)) o[d][4 * g + 2] += unpack16<Half>(v.y & 0xffffu);
-                            if (not_finite<Half>(v.y >> 16)) o[d][4 * g + 3] += unpack16<Half>(v.y >> 16);
-                        }
+                    o[d] = mfma32<Half>(v, w[kk], o[d]);
                 }
+            for (int x = 0; odd && x < kWideKeys; ++x) {
+                const bool sees = key0 + x <= last;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const uint32_t piece = (uint32_t)(4 * d + g) ^ (x & 7);
+                        const u32x2 v = lds_read8(at + kKeys + x * kRow + (piece << 4) + 8 * hi);
+                        o[d][4 * g] += sees && not_finite<Half>(v.x & 0xffffu) ? unpack16<Half>(v.x & 0xffffu) : 0.0f;
+                        o[d][4 * g + 1] += sees && not_finite<Half>(v.x >> 16) ? unpack16<Half>(v.x >> 16) : 0.0f;
+                        o[d][4 * g + 2] += sees && not_finite<Half>(v.y & 0xffffu) ? unpack16<Half>(v.y & 0xffffu) : 0.0f;
+                        o[d][4 * g + 3] += sees && not_finite<Half>(v.y >> 16) ? unpack16<Half>(v.y >> 16) : 0.0f;
+                    }
             }
         }
         l += __shfl_xor(l, 32);
@@ -520,28 +558,26 @@ struct Attend {
         const int32_t first_block = t.block0 + 2 * wave;
         int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kNarrowKeys - 1) / kNarrowKeys;
         s1 = s1 < t.s1 ? s1 : t.s1;
-        int32_t s = t.s0;
-        __syncthreads();                             // the LDS is the last tile's until here
-        int32_t id[2] = {0, 0};
-        auto ids = [&](int32_t x) {
+        int32_t s = t.s0, id[2], later[2];
+        auto ids = [&](int32_t* to, int32_t x) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) id[b] = __builtin_amdgcn_readfirstlane(block_id(t, first_block + 8 * x + b));
+            for (int b = 0; b < 2; ++b) to[b] = block_id(t, first_block + 8 * x + b);
         };
-        if (s < s1) {
-            ids(s);
+        uint32_t bad = 0, next_bad = 0;
+        auto issue_keys = [&](int32_t x) {
+            next_bad = 0;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) load_keys(t, first_block + 8 * s + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
+            for (int b = 0; b < 2; ++b) {
+                load_keys(t, first_block + 8 * x + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
+                if (bad_block(t, first_block + 8 * x + b, id[b])) next_bad |= 1u << b;
+            }
+        };
+        auto issue_values = [&](int32_t x) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) load_values(t, first_block + 8 * s + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
-        }
-        for (; s < s1; ++s) {
-            const int32_t b0 = first_block + 8 * s, key0 = b0 * RK_BLOCK_TOKENS;
-            const uint32_t bad = (bad_block(t, b0, id[0]) ? 1u : 0u) | (bad_block(t, b0 + 1, id[1]) ? 2u : 0u);
-            const bool more = s + 1 < s1;
-            if (more) ids(s + 1);
-            // (vector memory operations end in the order of their issue: all but the values' loads)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
-            f32x4 sc[NQ][2];
+            for (int b = 0; b < 2; ++b)
+                load_values(t, first_block + 8 * x + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+        };
+        auto scores = [&](f32x4 (*sc)[2]) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
@@ -553,28 +589,16 @@ struct Attend {
                     for (int n = 0; n < NQ; ++n) sc[n][kt] = mfma16<Half>(k, q[n][ks], sc[n][kt]);
                 }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the keys are in registers
-            if (more)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) load_keys(t, b0 + 8 + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
-            const bool masked = key0 + 31 > all_see || bad;
-            u32x4 w[NQ];
+        };
+        auto weights = [&](f32x4 (*sc)[2], u32x4* w) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                if (masked) {
-                    if (bad && n == 0) report_bad();
-#pragma unroll
-                    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
-                }
                 float top = sc[n][0][0];
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[n][kt][i]);
-                if (__any(top * c > m[n] + 8.0f)) {
+                if (__any(top * c > m[n] + 8.0f)) {                      // (as for wide tiles)
                     top = fmaxf(top, __shfl_xor(top, 16));
                     top = fmaxf(top, __shfl_xor(top, 32)) * c;
                     const float nm = fmaxf(m[n], top);
@@ -595,60 +619,111 @@ struct Attend {
                         w[n][2 * kt + (i >> 1)] = pack16<Half>(x, y);
                     }
             }
-            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
+        };
+        auto values = [&](int d) {
+            const uint32_t x = vals + v_read[d & 3] + (uint32_t)((d >> 2) * 128);
+            const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
+            return u32x4{lo.x, lo.y, up.x, up.y};
+        };
+        // (vector memory operations end in the order of their issue: the step's keys are there when only its values'
+        // loads are under way, its values when only the next keys' are)
+        auto wait_keys = [&]() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory"); };
+        auto keys_read = [&]() {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the keys are in registers
+            bad = next_bad;
+            if (s + 1 < s1) {
+                id[0] = later[0];
+                id[1] = later[1];
+                issue_keys(s + 1);
+                ids(later, s + 2);
+            }
+        };
+        auto wait_values = [&]() {
+            if (s + 1 < s1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            auto values = [&](int d) {
-                const uint32_t x = vals + v_read[d & 3] + (uint32_t)((d >> 2) * 128);
-                const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
-                return u32x4{lo.x, lo.y, up.x, up.y};
-            };
-            bool odd = false;
-            if (masked && t.mask && t.tokens > 1) {
+        };
+        auto values_read = [&]() {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the values are in registers
+            if (s + 1 < s1) issue_values(s + 1);
+        };
+        __syncthreads();                             // the LDS is the last tile's until here
+        if (s < s1) {
+            ids(id, s);
+            issue_keys(s);
+            issue_values(s);
+            ids(later, s + 1);
+        }
+        const int32_t seen = all_see + 1 - first_block * RK_BLOCK_TOKENS - 32;       // the last step's first key that all see
+        const int32_t open = seen < 0 ? 0 : seen / kNarrowKeys + 1, s_open = open < s1 ? open : s1;
+        for (; s < s_open && !next_bad; ++s) {
+            f32x4 sc[NQ][2];
+            u32x4 w[NQ];
+            wait_keys();
+            scores(sc);
+            keys_read();
+            weights(sc, w);
+            wait_values();
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const u32x4 v = values(d);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
+            }
+            values_read();
+        }
+        for (; s < s1; ++s) {
+            const int32_t key0 = (first_block + 8 * s) * RK_BLOCK_TOKENS;
+            f32x4 sc[NQ][2];
+            u32x4 w[NQ];
+            wait_keys();
+            scores(sc);
+            keys_read();
+            if (bad) report_bad();
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
+            weights(sc, w);
+            wait_values();
+            bool odd = false;                        // (as for wide tiles)
+            if (t.mask && t.tokens > 1)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const u32x4 v = values(d);
                     odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
                 }
-                odd = __any(odd);
-                asm volatile("" ::: "memory");       // (read again below, not kept)
-            }
-            if (!odd) {
+            odd = __any(odd);
+            asm volatile("" ::: "memory");
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const u32x4 v = values(d);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
-                }
-            } else {
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    u32x4 v = values(d);
+            for (int d = 0; d < DT; ++d) {
+                u32x4 v = values(d);
+                if (odd) {
                     v.x = finite_or_zero<Half>(v.x);
                     v.y = finite_or_zero<Half>(v.y);
                     v.z = finite_or_zero<Half>(v.z);
                     v.w = finite_or_zero<Half>(v.w);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
                 }
-                for (int x = 0; x < 32; ++x)
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ (x & 7);
-                        const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) {
-                            if (key0 + x > last[n]) continue;
-                            if (not_finite<Half>(v.x & 0xffffu)) o[n][d][0] += unpack16<Half>(v.x & 0xffffu);
-                            if (not_finite<Half>(v.x >> 16)) o[n][d][1] += unpack16<Half>(v.x >> 16);
-                            if (not_finite<Half>(v.y & 0xffffu)) o[n][d][2] += unpack16<Half>(v.y & 0xffffu);
-                            if (not_finite<Half>(v.y >> 16)) o[n][d][3] += unpack16<Half>(v.y >> 16);
-                        }
-                    }
+                for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the values are in registers
-            if (more)
+            for (int x = 0; odd && x < 32; ++x)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) load_values(t, b0 + 8 + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+                for (int d = 0; d < DT; ++d) {
+                    const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ (x & 7);
+                    const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) {
+                        const bool sees = key0 + x <= last[n];
+                        o[n][d][0] += sees && not_finite<Half>(v.x & 0xffffu) ? unpack16<Half>(v.x & 0xffffu) : 0.0f;
+                        o[n][d][1] += sees && not_finite<Half>(v.x >> 16) ? unpack16<Half>(v.x >> 16) : 0.0f;
+                        o[n][d][2] += sees && not_finite<Half>(v.y & 0xffffu) ? unpack16<Half>(v.y & 0xffffu) : 0.0f;
+                        o[n][d][3] += sees && not_finite<Half>(v.y >> 16) ? unpack16<Half>(v.y >> 16) : 0.0f;
+                    }
+                }
+            values_read();
         }
         // the four wavefronts' results: rows of DP floats in LDS, wavefront after wavefront
         __syncthreads();
@@ -779,6 +854,122 @@ __device__ __forceinline__ int32_t last_group(const int32_t* off, int32_t n, int
     return lo;
 }
 
+// A workgroup's piece [from, to) of the line of its kind of tiles, from place `off` of request i's part on; wg: its
+// place among the workgroups.
+template <bool Wide, class A>
+__device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uint64_t off, uint64_t from, uint64_t to,
+                                     uint64_t each, int32_t wg)
+{
+    const AttendArgs& p = work.p;
+    const rk_attention& a = p.a;
+    const int32_t G = work.G, B = p.n, tid = threadIdx.x;
+    constexpr int DP = A::kHead;
+    constexpr uint32_t cost = Wide ? kWideCost : kNarrowCost;
+    uint64_t x = from;
+    while (x < to && i < B) {
+        Request r = req[i];
+        r.kv = uniform(r.kv);
+        r.q0 = uniform(r.q0);
+        r.tokens = uniform(r.tokens);
+        r.shared = uniform(r.shared);
+        r.end = uniform(r.end);
+        r.base = uniform(r.base);
+        Segment sg;
+        bool prefix = false;
+        uint64_t before = 0;
+        if (r.end) {
+            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, G);
+            before = sg.wide == Wide ? sg.cost * (uint64_t)a.Hkv : 0;
+            prefix = off < before;
+        }
+        if (!prefix) {
+            sg = own_segment(r, G);
+            const uint64_t own = sg.wide == Wide ? sg.cost * (uint64_t)a.Hkv : 0;
+            off -= before;
+            if (off >= own) {                // on to the next request
+                off -= own;
+                ++i;
+                continue;
+            }
+        }
+        const int32_t head = (int32_t)quotient(off, sg.cost);
+        uint64_t in = off - (uint64_t)head * sg.cost;              // place in the head's part
+        int32_t j = (int32_t)quotient(in, sg.pair);
+        in -= (uint64_t)j * sg.pair;
+        int32_t steps = sg.steps0;
+        uint64_t left = sg.pair;             // cost from the tile's start to the next tile's
+        bool nothing = false;
+        if (Wide && sg.grows) {
+            auto steps_of = [&](int32_t k) {
+                const int64_t seen = (int64_t)(k + 1) * sg.per < sg.tokens ? (int64_t)(k + 1) * sg.per : sg.tokens;
+                return steps_for((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWideKeys);
+            };
+            const int32_t k = sg.tiles - 1 - j;
+            const uint64_t first = (uint64_t)steps_of(j) * cost;
+            steps = steps_of(j);
+            left = first;
+            if (in >= first) {               // the pair's other tile
+                in -= first;
+                left = sg.pair - first;
+                nothing = k == j;
+                j = k;
+                steps = steps_of(k);
+            }
+        }
+        // the steps of the tile that begin in [from, to)
+        const uint64_t s_end = quotient_up(to - x + in, cost);
+        const int32_t s0 = (int32_t)quotient_up(in, cost), s1 = s_end < (uint64_t)steps ? (int32_t)s_end : steps;
+        if (!nothing && s0 < s1) {
+            Tile t;
+            t.token = r.q0 + j * sg.per;
+            t.tokens = sg.tokens - j * sg.per < sg.per ? sg.tokens - j * sg.per : sg.per;
+            t.head = head;
+            t.s0 = s0;
+            t.s1 = s1;
+            t.mask = !prefix;
+            t.row = (const __attribute__((address_space(4))) int32_t*)(a.tables + (int64_t)(p.b0 + i) * a.table_stride);
+            if (prefix) {
+                t.block0 = 0;
+                t.keys_end = r.shared * RK_BLOCK_TOKENS;
+                t.pos = 0;
+            } else {
+                t.block0 = r.shared;
+                t.pos = r.kv - r.tokens + j * sg.per;
+                t.keys_end = t.pos + t.tokens;
+            }
+            const bool whole = s0 == 0 && s1 == steps, joined = r.shared != 0;
+            t.part = t.part_ml = nullptr;
+            const int kind = prefix ? 0 : 1;
+            if (!whole) {
+                const int64_t slot = 2 * (int64_t)wg + (s0 == 0 ? 1 : 0);
+                t.part = p.part + slot * kWideRows * DP;
+                t.part_ml = p.part_ml + slot * kWideRows * 2;
+            } else if (joined) {
+                const int64_t row = ((int64_t)kind * a.Hkv + head) * p.shared_rows + (int64_t)(r.base + j * sg.per) * G;
+                t.part = p.whole + row * DP;
+                t.part_ml = p.whole_ml + row * 2;
+            }
+            if (s0 == 0 && (joined || !whole)) {
+                // workgroups that the tile's steps fall to: the last step begins (steps - 1) costs behind its start
+                const uint64_t of_mine = x - in - from + (uint64_t)(steps - 1) * cost;
+                const int32_t n = (int32_t)quotient(of_mine, each) + 1;
+                if (joined) {
+                    for (int32_t k = tid; k < t.tokens; k += kThreads)
+                        p.parts[((int64_t)kind * a.Hkv + head) * p.shared_tokens + r.base + j * sg.per + k] =
+                            Parts{whole ? 0 : n, wg, k * G, 0};
+                } else if (tid == 0) {
+                    p.split[blockIdx.x] = Split{n, wg, t.token, t.tokens, head, {0, 0, 0}};
+                }
+            }
+            if constexpr (Wide) work.wide(t);
+            else if (sg.rows <= 16) work.template narrow<1>(t);
+            else work.template narrow<2>(t);
+        }
+        x += left - in;
+        off += left - in + (prefix ? 0 : before);
+    }
+}
+
 // One launch over a line of work: request after request (a group's prefix before its first member's own keys), key head
 // after key head, tile after tile, step after step.  The line is cut into equal pieces, a workgroup each, whatever the
 // lengths are; a tile that is cut is joined by the next kernel.
@@ -787,7 +978,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 {
     extern __shared__ __align__(1024) uint8_t lds[];
     __shared__ float s_join[2 * kWaves * kNarrowRows];
-    __shared__ uint64_t s_tmp[2 * kWaves], s_off;
+    __shared__ uint64_t s_tmp[3 * kWaves], s_off;
     __shared__ int32_t s_i, s_bad;
     using A = Attend<DP, Half>;
     const rk_attention& a = p.a;
@@ -867,51 +1058,69 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
         }
         __syncthreads();
     }
-    // the line of work: per thread's requests, then over the threads
+    // the line of work: per thread's requests, then over the threads; wide tiles first, then narrow ones
     const int32_t per = (B + kThreads - 1) / kThreads;
     const int32_t i0 = tid * per, i1 = i0 + per < B ? i0 + per : B;
-    uint64_t mine = 0;
-    uint32_t together = 0;
-    auto prefix_of = [&](int32_t i) {
-        const Request& l = req[req[i].end - 1];
-        return prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G);
+    struct Cost {
+        uint64_t wide, narrow;
     };
+    auto cost_of = [&](int32_t i) {
+        Cost x{0, 0};
+        const Segment own = own_segment(req[i], G);
+        (own.wide ? x.wide : x.narrow) += own.cost;
+        if (req[i].end) {
+            const Request& l = req[req[i].end - 1];
+            const Segment prefix = prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G);
+            (prefix.wide ? x.wide : x.narrow) += prefix.cost;
+        }
+        return x;
+    };
+    uint32_t together = 0;
     for (int32_t i = i0; i < i1; ++i) {
         if (req[i].tokens < 0) req[i].tokens = 0;
         if (req[i].shared) together += req[i].tokens;
     }
     __syncthreads();
+    Cost mine{0, 0};
     for (int32_t i = i0; i < i1; ++i) {
-        mine += own_segment(req[i], G).cost;
-        if (req[i].end) mine += prefix_of(i).cost;
+        const Cost x = cost_of(i);
+        mine.wide += x.wide;
+        mine.narrow += x.narrow;
     }
-    mine *= (uint64_t)a.Hkv;
-    uint64_t upto = mine;
+    mine.wide *= (uint64_t)a.Hkv;
+    mine.narrow *= (uint64_t)a.Hkv;
+    uint64_t wide_upto = mine.wide, narrow_upto = mine.narrow;
     uint32_t tokens_upto = together;
-    incl_sums(upto, tokens_upto, s_tmp);
-    uint64_t total = 0;
-    for (int w = 0; w < kWaves; ++w) total += s_tmp[w];
-    // (sums of the wavefronts)
-    const uint64_t grid = gridDim.x;
-    total = uniform(total);
-    uint64_t each = (total + grid - 1) / grid;
+    incl_sums(wide_upto, narrow_upto, tokens_upto, s_tmp);
+    Cost all{0, 0};
+    for (int w = 0; w < kWaves; ++w) {
+        all.wide += s_tmp[w];
+        all.narrow += s_tmp[kWaves + w];
+    }
+    all.wide = uniform(all.wide);
+    all.narrow = uniform(all.narrow);
+    // pieces for at most gridDim.x workgroups (each kind's last may be short)
+    uint64_t each = quotient_up(all.wide + all.narrow, gridDim.x - 1);
     if (each < kLeast) each = kLeast;
-    const uint32_t active = (uint32_t)((total + each - 1) / each);
+    const uint32_t n_wide = (uint32_t)quotient_up(all.wide, each);
+    const uint32_t active = n_wide + (uint32_t)quotient_up(all.narrow, each);
     // workgroups go to the 8 XCDs in turn: each XCD takes a stretch of the line
     const uint32_t wg = (blockIdx.x & 7u) * ((active + 7) / 8) + (blockIdx.x >> 3);
-    const bool idle = (blockIdx.x >> 3) >= (active + 7) / 8 || wg >= active;
-    const uint64_t from = (uint64_t)wg * each, to = from + each < total ? from + each : total;
+    const bool idle = (blockIdx.x >> 3) >= (active + 7) / 8 || wg >= active, wide = wg < n_wide;
+    const uint64_t from = (uint64_t)(wide ? wg : wg - n_wide) * each, end = wide ? all.wide : all.narrow;
+    const uint64_t to = from + each < end ? from + each : end;
     {
         uint32_t tok = tokens_upto - together;
-        uint64_t x = upto - mine;
+        uint64_t x = wide ? wide_upto - mine.wide : narrow_upto - mine.narrow;
+        const bool here = !idle && from >= x && from < (wide ? wide_upto : narrow_upto);
         for (int32_t i = i0; i < i1; ++i) {
             req[i].base = (int32_t)tok;
             if (req[i].shared) tok += req[i].tokens;
             if (tell) p.share_base[i] = req[i].shared && req[i].tokens ? req[i].base : -1;
-            uint64_t w = own_segment(req[i], G).cost;
-            if (req[i].end) w += prefix_of(i).cost;
-            w *= (uint64_t)a.Hkv;
-            if (!idle && from >= x && from < x + w) {
+            if (!here) continue;
+            const Cost k = cost_of(i);
+            const uint64_t w = (wide ? k.wide : k.narrow) * (uint64_t)a.Hkv;
+            if (from >= x && from < x + w) {
                 s_i = i;
                 s_off = from - x;
             }
@@ -924,112 +1133,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
     float c = fabsf(a.scale) * kLog2e;
     if (c < 1e-30f) c = 1e-30f;              // scores of 0, and -infinity stays what it is
     A work(p, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds, s_join, c);
-    int32_t i = uniform(s_i);
-    uint64_t x = from;
-    uint64_t off = uniform(s_off);           // x's place in request i's part of the line
-    while (x < to && i < B) {
-        Request r = req[i];
-        r.kv = uniform(r.kv);
-        r.q0 = uniform(r.q0);
-        r.tokens = uniform(r.tokens);
-        r.shared = uniform(r.shared);
-        r.end = uniform(r.end);
-        r.base = uniform(r.base);
-        Segment sg;
-        bool prefix = false;
-        uint64_t before = 0;
-        if (r.end) {
-            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, G);
-            before = sg.cost * (uint64_t)a.Hkv;
-            prefix = off < before;
-        }
-        if (!prefix) {
-            sg = own_segment(r, G);
-            off -= before;
-            if (sg.cost == 0 || off >= sg.cost * (uint64_t)a.Hkv) {        // on to the next request
-                off -= sg.cost * (uint64_t)a.Hkv;
-                ++i;
-                continue;
-            }
-        }
-        const int32_t head = (int32_t)(off / sg.cost);
-        uint64_t in = off - (uint64_t)head * sg.cost;              // place in the head's part
-        int32_t j = (int32_t)(in / sg.pair);
-        in -= (uint64_t)j * sg.pair;
-        int32_t steps = sg.steps0;
-        uint64_t left = sg.pair;             // cost from the tile's start to the next tile's
-        const uint32_t cost = sg.wide ? kWideCost : kNarrowCost;
-        bool nothing = false;
-        if (sg.grows) {
-            auto steps_of = [&](int32_t k) {
-                const int64_t seen = (int64_t)(k + 1) * sg.per < sg.tokens ? (int64_t)(k + 1) * sg.per : sg.tokens;
-                return steps_for((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWideKeys);
-            };
-            const int32_t k = sg.tiles - 1 - j;
-            const uint64_t head_cost = (uint64_t)steps_of(j) * cost;
-            steps = steps_of(j);
-            left = head_cost;
-            if (in >= head_cost) {           // the pair's other tile
-                in -= head_cost;
-                left = sg.pair - head_cost;
-                nothing = k == j;
-                j = k;
-                steps = steps_of(k);
-            }
-        }
-        // the steps of the tile that begin in [from, to)
-        const uint64_t room = to - x + in;
-        int32_t s0 = (int32_t)((in + cost - 1) / cost), s1 = (int32_t)((room + cost - 1) / cost < (uint64_t)steps ? (room + cost - 1) / cost : steps);
-        if (!nothing && s0 < s1) {
-            Tile t;
-            t.token = r.q0 + j * sg.per;
-            t.tokens = sg.tokens - j * sg.per < sg.per ? sg.tokens - j * sg.per : sg.per;
-            t.head = head;
-            t.s0 = s0;
-            t.s1 = s1;
-            t.n_steps = steps;
-            t.mask = !prefix;
-            t.row = a.tables + (int64_t)(p.b0 + i) * a.table_stride;
-            if (prefix) {
-                t.block0 = 0;
-                t.keys_end = r.shared * RK_BLOCK_TOKENS;
-                t.pos = 0;
-            } else {
-                t.block0 = r.shared;
-                t.pos = r.kv - r.tokens + j * sg.per;
-                t.keys_end = t.pos + t.tokens;
-            }
-            const bool whole = s0 == 0 && s1 == steps, joined = r.shared != 0;
-            // workgroups that the tile's steps fall to: its last step begins at cost (steps - 1) behind its start
-            const uint64_t start = x - in;
-            const int32_t n = (int32_t)((start + (uint64_t)(steps - 1) * cost) / each) - (int32_t)wg + 1;
-            t.part = t.part_ml = nullptr;
-            const int kind = prefix ? 0 : 1;
-            if (!whole) {
-                const int64_t slot = 2 * (int64_t)wg + (s0 == 0 ? 1 : 0);
-                t.part = p.part + slot * kWideRows * DP;
-                t.part_ml = p.part_ml + slot * kWideRows * 2;
-            } else if (joined) {
-                const int64_t row = ((int64_t)kind * a.Hkv + head) * p.shared_rows + (int64_t)(r.base + j * sg.per) * G;
-                t.part = p.whole + row * DP;
-                t.part_ml = p.whole_ml + row * 2;
-            }
-            if (s0 == 0) {
-                if (joined) {
-                    for (int32_t k = tid; k < t.tokens; k += kThreads)
-                        p.parts[((int64_t)kind * a.Hkv + head) * p.shared_tokens + r.base + j * sg.per + k] =
-                            Parts{whole ? 0 : n, (int32_t)wg, k * G, 0};
-                } else if (!whole && tid == 0) {
-                    p.split[blockIdx.x] = Split{n, (int32_t)wg, t.token, t.tokens, head, {0, 0, 0}};
-                }
-            }
-            if (sg.wide) work.wide(t);
-            else if (sg.rows <= 16) work.template narrow<1>(t);
-            else work.template narrow<2>(t);
-        }
-        x += left - in;
-        off += left - in + (prefix ? 0 : before);
-    }
+    const int32_t i = uniform(s_i);
+    const uint64_t off = uniform(s_off);
+    if (wide) walk<true>(work, req, i, off, from, to, each, (int32_t)wg);
+    else walk<false>(work, req, i, off, from, to, each, (int32_t)wg);
 }
 
 // The parts of rows that more than one workgroup worked on, joined: a wavefront a row, a lane every 64th value.
