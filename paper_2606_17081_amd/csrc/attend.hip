@@ -18,7 +18,7 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kWideRows = 128, kWideKeys = 64;       // a wide step: 32 rows a wavefront, 64 keys
 constexpr int kNarrowRows = 32, kNarrowKeys = 128;   // a narrow step: 32 keys a wavefront
 constexpr uint32_t kWideCost = 2, kNarrowCost = 3;   // of a step, relative to each other
-constexpr uint32_t kLeast = 6;                       // cost that a workgroup takes at least
+constexpr uint32_t kLeast = 3;                       // cost that a workgroup takes at least: a step
 constexpr int kShareBlocks = 4;                      // shorter prefixes are not worth joining their parts
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 
@@ -1139,69 +1139,112 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
     else walk<false>(work, req, i, off, from, to, each, (int32_t)wg);
 }
 
-// The parts of rows that more than one workgroup worked on, joined: a wavefront a row, a lane every 64th value.
+// The parts of rows that more than one workgroup worked on, joined: a wavefront a row, DP / 64 neighbouring values a
+// lane.  The parts' weights come first, a lane each; then their values, several loads under way at a time.
 template <int DP, bool Half>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks)
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks, int32_t shared_chunks)
 {
     const rk_attention& a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int32_t G = a.Hq / a.Hkv;
     constexpr int N = DP / 64;
-    auto put = [&](int64_t token, int32_t h, const float* o, float m, float l) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        uint16_t* to = (uint16_t*)a.out + token * a.out_token + h * a.out_head;
-#pragma unroll
-        for (int x = 0; x < N; ++x)
-            if (64 * x + lane < a.D) to[64 * x + lane] = (uint16_t)pack16<Half>(o[x] * inv, 0.0f);
-        if (lane == 0 && a.lse) a.lse[token * a.Hq + h] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
+    struct Sum {
+        float o[N], m, l;
     };
-    // n parts of a row: the tail of workgroup wg's work, then the heads of those after it
-    auto slot = [&](int32_t wg, int32_t k) { return 2 * (int64_t)(wg + k) + (k == 0 ? 1 : 0); };
-    auto add = [&](float* o, float& m, float& l, const float* part, const float* ml) {
-        const float pm = ml[0], nm = fmaxf(m, pm);
-        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - nm);
-        const float g = pm == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(pm - nm);
-        l = l * f + ml[1] * g;
-#pragma unroll
-        for (int x = 0; x < N; ++x) o[x] = (f == 0.0f ? 0.0f : o[x] * f) + (g == 0.0f ? 0.0f : part[64 * x + lane] * g);
-        m = nm;
-    };
-    if ((int32_t)blockIdx.x < grid * chunks) {
-        const Split s = p.split[blockIdx.x / chunks];
-        const int32_t rows = s.tokens * G;
-        if (s.n == 0) return;
-        for (int32_t r = (int32_t)(blockIdx.x % chunks) * kWaves + wave; r < rows; r += chunks * kWaves) {
-            float o[N] = {}, m = -INFINITY, l = 0.0f;
-            for (int32_t k = 0; k < s.n; ++k) {
-                const int64_t row = slot(s.wg, k) * kWideRows + r;
-                add(o, m, l, p.part + row * DP, p.part_ml + row * 2);
+    // n parts of a row: the first the last that workgroup wg began, the others the first of the workgroups
+    // after it; rows of kWideRows a place
+    auto add = [&](Sum& s, int32_t n, const float* part, const float* ml, int64_t first, int64_t next) {
+        for (int32_t k0 = 0; k0 < n; k0 += 64) {
+            const int32_t k = k0 + lane;
+            float pm = -INFINITY, pl = 0.0f;
+            if (k < n) {
+                const int64_t row = k == 0 ? first : next + (int64_t)(k - 1) * (2 * kWideRows);
+                pm = ml[2 * row];
+                pl = ml[2 * row + 1];
             }
-            put(s.token + (int64_t)(r / G), s.head * G + r % G, o, m, l);
+            float top = pm;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+            const float nm = fmaxf(s.m, top);
+            if (nm == -INFINITY) continue;
+            const float old = __builtin_amdgcn_exp2f(s.m - nm), w = __builtin_amdgcn_exp2f(pm - nm);
+            float sum = w * pl;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+            s.l = s.l * old + sum;
+            s.m = nm;
+#pragma unroll
+            for (int x = 0; x < N; ++x) s.o[x] = old == 0.0f ? 0.0f : s.o[x] * old;
+            const int32_t here = n - k0 < 64 ? n - k0 : 64;
+            constexpr int kAtOnce = 8;
+            for (int32_t q = 0; q < here; q += kAtOnce) {
+                float v[kAtOnce][N];
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int32_t at = k0 + (q + u < here ? q + u : here - 1);
+                    const int64_t row = at == 0 ? first : next + (int64_t)(at - 1) * (2 * kWideRows);
+#pragma unroll
+                    for (int x = 0; x < N; ++x) v[u][x] = part[row * DP + N * lane + x];
+                }
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const float f = q + u < here ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), q + u)) : 0.0f;
+                    if (f != 0.0f)
+#pragma unroll
+                        for (int x = 0; x < N; ++x) s.o[x] += f * v[u][x];
+                }
+            }
+        }
+    };
+    auto put = [&](const Sum& s, int64_t token, int32_t h) {
+        const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
+        uint16_t* to = (uint16_t*)a.out + token * a.out_token + h * a.out_head + N * lane;
+        if (N * lane < a.D) {
+            if constexpr (N % 2 == 0) {
+#pragma unroll
+                for (int x = 0; x < N; x += 2)
+                    if (N * lane + x < a.D) *reinterpret_cast<uint32_t*>(to + x) = pack16<Half>(s.o[x] * inv, s.o[x + 1] * inv);
+            } else {
+#pragma unroll
+                for (int x = 0; x < N; ++x)
+                    if (N * lane + x < a.D) to[x] = (uint16_t)pack16<Half>(s.o[x] * inv, 0.0f);
+            }
+        }
+        if (lane == 0 && a.lse) a.lse[token * a.Hq + h] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_log2f(s.l)) * kLn2;
+    };
+    auto tail = [&](int32_t wg, int32_t r) { return (2 * (int64_t)wg + 1) * kWideRows + r; };
+    auto heads = [&](int32_t wg, int32_t r) { return 2 * (int64_t)(wg + 1) * kWideRows + r; };
+    if ((int32_t)blockIdx.x < grid * chunks) {
+        const Split t = p.split[blockIdx.x / chunks];
+        const int32_t rows = t.tokens * G;
+        if (t.n == 0) return;
+        for (int32_t r = (int32_t)(blockIdx.x % chunks) * kWaves + wave; r < rows; r += chunks * kWaves) {
+            Sum s{{}, -INFINITY, 0.0f};
+            add(s, t.n, p.part, p.part_ml, tail(t.wg, r), heads(t.wg, r));
+            put(s, t.token + (int64_t)(r / G), t.head * G + r % G);
         }
         return;
     }
     // a request whose group attends to its prefix together
-    const int32_t b = (int32_t)blockIdx.x - grid * chunks, i = b / a.Hkv, head = b % a.Hkv;
+    const int32_t b = (int32_t)blockIdx.x - grid * chunks, u = b / shared_chunks, i = u / a.Hkv, head = u % a.Hkv;
     const int32_t base = p.share_base[i];
+    const int64_t q0 = a.q_off[p.b0 + i], q1 = a.q_off[p.b0 + i + 1];
     if (base < 0) return;
-    const int64_t q0 = a.q_off[p.b0 + i];
-    const int32_t rows = (int32_t)(a.q_off[p.b0 + i + 1] - q0) * G;
-    for (int32_t r = wave; r < rows; r += kWaves) {
+    const int32_t rows = (int32_t)(q1 - q0) * G;
+    for (int32_t r = (b % shared_chunks) * kWaves + wave; r < rows; r += shared_chunks * kWaves) {
         const int32_t tok = r / G, h = r % G;
-        float o[N] = {}, m = -INFINITY, l = 0.0f;
+        Parts t[2];
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind)
+            t[kind] = p.parts[((int64_t)kind * a.Hkv + head) * p.shared_tokens + base + tok];
+        Sum s{{}, -INFINITY, 0.0f};
+#pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
-            const int64_t at = (int64_t)kind * a.Hkv + head;
-            const Parts s = p.parts[at * p.shared_tokens + base + tok];
-            if (s.n == 0) {
-                const int64_t row = at * p.shared_rows + (int64_t)base * G + r;
-                add(o, m, l, p.whole + row * DP, p.whole_ml + row * 2);
-            }
-            for (int32_t k = 0; k < s.n; ++k) {
-                const int64_t row = slot(s.wg, k) * kWideRows + s.row + h;
-                add(o, m, l, p.part + row * DP, p.part_ml + row * 2);
-            }
+            const int32_t n = uniform(t[kind].n), wg = uniform(t[kind].wg), row = uniform(t[kind].row) + h;
+            if (n == 0) add(s, 1, p.whole, p.whole_ml, ((int64_t)kind * a.Hkv + head) * p.shared_rows + (int64_t)base * G + r, 0);
+            else add(s, n, p.part, p.part_ml, tail(wg, row), heads(wg, row));
         }
-        put(q0 + tok, head * G + h, o, m, l);
+        put(s, q0 + tok, head * G + h);
     }
 }
 
@@ -1260,13 +1303,15 @@ static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
 {
     const int64_t rows = p.a.T * (p.a.Hq / p.a.Hkv);
     const int32_t chunks = rows <= 4 ? 1 : rows <= 32 ? 4 : 8;
+    const int32_t shared_chunks = (p.a.Hq / p.a.Hkv + kWaves - 1) / kWaves;       // a row a wavefront, of one new token
     for (p.b0 = 0; p.b0 < p.a.B; p.b0 += p.n) {
         p.n = launch_size(p.a.B - p.b0);
         hipLaunchKernelGGL((attend_kernel<DP, Half>), dim3((unsigned)grid), dim3(kThreads), lds_bytes(DP, p.n), s, p);
         int rc = hip_check(hipGetLastError(), "rk_prefix_attention launch");
         if (rc) return rc;
-        const int64_t blocks = (int64_t)grid * chunks + (p.a.group_off ? (int64_t)p.n * p.a.Hkv : 0);
-        hipLaunchKernelGGL((join_kernel<DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, grid, chunks);
+        const int64_t blocks = (int64_t)grid * chunks + (p.a.group_off ? (int64_t)p.n * p.a.Hkv * shared_chunks : 0);
+        hipLaunchKernelGGL((join_kernel<DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, grid, chunks,
+                           shared_chunks);
         rc = hip_check(hipGetLastError(), "rk_prefix_attention join launch");
         if (rc) return rc;
     }
