@@ -129,6 +129,9 @@ __device__ __forceinline__ int32_t afresh(int32_t x)
     return x;
 }
 
+// The larger number; NaN gives way to a number (and shows in the weights).
+__device__ __forceinline__ float larger(float x, float y) { return fmaxf(x, y); }
+
 // x, the same in all lanes, as the compiler then knows.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint64_t uniform(uint64_t x)
@@ -191,6 +194,16 @@ struct Attend {
     static constexpr uint32_t kRow = DP * 2;          // bytes of a row in LDS
     static constexpr uint32_t kTileBytes = 512 * DP;  // LDS for keys and values
 
+    // Row r of a block keeps its piece x at place x ^ turn(r), so that what a wavefront reads together lies in all of the
+    // 256 bytes of banks: one piece of 16 rows (keys), two or four neighbouring ones of 8 or 4 rows (values).  The
+    // rows' lengths turn rows of 128 or 384 bytes by half of that already.
+    static constexpr int kTurn = NC % 16 == 0 ? 16 : 8;
+    static __device__ __forceinline__ uint32_t turn(uint32_t r)
+    {
+        const uint32_t t = (r >> 1 & 1) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1);
+        return kTurn == 16 ? (r & 1) << 3 | t : t;
+    }
+
     const AttendArgs& p;
     const uint32_t tile;                              // LDS address of the keys and values
     float* const join;                                // LDS: 2 * kWaves * kNarrowRows
@@ -204,11 +217,9 @@ struct Attend {
           c(scale)
     {
         const int lane = threadIdx.x & 63;
-        // Row r of a block keeps its piece x at place x ^ (r % 8): rows of 128 bytes and more would
-        // otherwise put what a wavefront reads together into the same banks.
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int x = 64 * i + lane, r = x / NC, piece = (x % NC) ^ (r & 7);
+            const int x = 64 * i + lane, r = x / NC, piece = (x % NC) ^ turn(r);
             const bool in = 8 * piece < p.a.D;        // pieces behind D are loaded as zeros
             k_at[i] = in ? (uint32_t)(r * (int32_t)p.a.ks.token * 2 + 16 * piece) : 0x7ffffff0u;
             v_at[i] = in ? (uint32_t)(r * (int32_t)p.a.vs.token * 2 + 16 * piece) : 0x7ffffff0u;
@@ -262,11 +273,8 @@ struct Attend {
         load_block((const uint16_t*)p.a.v_cache + (rows > 0 ? (int64_t)id * p.a.vs.block : 0) + t.head * p.a.vs.head,
                    p.a.vs.token, rows, v_at, lds);
     }
-    // a block in the sequence whose number is outside the cache
-    __device__ __forceinline__ bool bad_block(const Tile& t, int32_t b, int32_t id) const
-    {
-        return (int64_t)b * RK_BLOCK_TOKENS < t.keys_end && (uint32_t)id >= (uint32_t)p.a.n_blocks;
-    }
+    // a block whose number is outside the cache
+    __device__ __forceinline__ bool bad_block(int32_t id) const { return (uint32_t)id >= (uint32_t)p.a.n_blocks; }
     __device__ __forceinline__ void report_bad() const
     {
         if ((threadIdx.x & 63) == 0) atomicOr(p.status, RK_DEV_BAD_BLOCK);
@@ -320,39 +328,77 @@ struct Attend {
         for (int d = 0; d < DT; ++d) o[d] = f32x16{};
         float m = -INFINITY, l = 0.0f;               // m: log2 of the weights' common divisor
         // LDS addresses in a stage, less what the unrolled loops add
-        uint32_t k_read[4], v_read[2];
+        uint32_t k_read[kTurn / 2], v_read[kTurn / 4], v_read8[kTurn / 4];       // (of rows 8 further)
         {
-            const uint32_t row = lane & 31;
+            const uint32_t row = lane & 31, vr = 4 * hi + ((lane & 15) >> 2), vp = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) k_read[x] = row * kRow + (((2 * x + hi) ^ (row & 7)) << 4);
-            const uint32_t vr = 4 * hi + ((lane & 15) >> 2);
+            for (int x = 0; x < kTurn / 2; ++x) k_read[x] = row * kRow + (((2 * x + hi) ^ turn(row & 15)) << 4);
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                v_read[x] = vr * kRow + (((4 * x + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ vr) << 4) + 8 * (lane & 1);
+            for (int x = 0; x < kTurn / 4; ++x) {
+                v_read[x] = vr * kRow + (((4 * x + vp) ^ turn(vr)) << 4) + 8 * (lane & 1);
+                v_read8[x] = (vr + 8) * kRow + (((4 * x + vp) ^ turn(vr + 8)) << 4) + 8 * (lane & 1);
+            }
         }
-        constexpr uint32_t kKeys = kWideKeys * kRow, kStage = 2 * kKeys;
-        // One step: keys and values of step s in the stage at `at`.
+        constexpr uint32_t kKeys = kWideKeys * kRow;   // bytes of a step's keys; two of them, then two steps' values
+        // Keys come two steps ahead, values one: while a step's weights are computed, the products of the next step's
+        // scores run beside them.  Pieces are read from LDS kAhead products before the one that takes them.
+        constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
+        struct Step {
+            int32_t own;                             // this wavefront's block
+            uint32_t bad;                            // of the four blocks, those outside the cache
+        };
+        auto look = [&](int32_t x) {
+            const int32_t b = t.block0 + 4 * x;
+            const int32_t b0 = block_id(t, b), b1 = block_id(t, b + 1), b2 = block_id(t, b + 2), b3 = block_id(t, b + 3);
+            Step e;
+            e.own = uniform(wave < 2 ? (wave == 0 ? b0 : b1) : (wave == 2 ? b2 : b3));
+            e.bad = (bad_block(b0) ? 1u : 0u) | (bad_block(b1) ? 2u : 0u) | (bad_block(b2) ? 4u : 0u) | (bad_block(b3) ? 8u : 0u);
+            return e;
+        };
+        auto keys_at = [&](int32_t x) { return tile + ((x - t.s0) & 1) * kKeys; };
+        auto values_at = [&](int32_t x) { return tile + 2 * kKeys + ((x - t.s0) & 1) * kKeys; };
+        auto issue_keys = [&](int32_t x, const Step& e) {
+            load_keys(t, t.block0 + 4 * x + wave, e.own, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow));
+        };
+        auto issue_values = [&](int32_t x, const Step& e) {
+            load_values(t, t.block0 + 4 * x + wave, e.own, values_at(x) + wave * (RK_BLOCK_TOKENS * kRow));
+        };
+        auto key_piece = [&](uint32_t at, int x) {   // of the x-th product
+            const int kt = x & 1, ks = x >> 1;
+            return lds_read16(at + k_read[ks % (kTurn / 2)] + (uint32_t)(kt * 32 * kRow + ks / (kTurn / 2) * (16 * kTurn)));
+        };
+        auto value_piece = [&](uint32_t at, int x) {
+            constexpr int n = kTurn / 4;
+            const int d = x % DT, kk = x / DT;
+            const uint32_t y = at + (uint32_t)(d / n * (16 * kTurn) + 16 * kk * kRow);
+            const u32x2 lo = lds_read_columns(y + v_read[d % n]), up = lds_read_columns(y + v_read8[d % n]);
+            return u32x4{lo.x, lo.y, up.x, up.y};
+        };
         auto scores = [&](uint32_t at, f32x16* sc) {
+            u32x4 k[kAhead];
+            sc[0] = sc[1] = f32x16{};
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                sc[kt] = f32x16{};
+            for (int x = 0; x < kAhead; ++x) k[x] = key_piece(at, x);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    sc[kt] = mfma32<Half>(lds_read16(at + k_read[ks & 3] + (uint32_t)(kt * 32 * kRow + (ks >> 2) * 128)),
-                                          q[ks], sc[kt]);
+            for (int x = 0; x < 2 * KS; ++x) {
+                sc[x & 1] = mfma32<Half>(k[x % kAhead], q[x >> 1], sc[x & 1]);
+                if (x + kAhead < 2 * KS) k[x % kAhead] = key_piece(at, x + kAhead);
             }
         };
-        auto weights = [&](const f32x16* sc, u32x4* w) {
+        auto highest = [&](const f32x16* sc) {
             float top = sc[0][0];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kt][i]);
-            // The weights' divisor follows the largest score only when that has left it behind by 2^8: sums
-            // and weights stay far from fp32's and fp16's ends, and the results are seldom rescaled.
+                for (int i = 0; i < 16; ++i) top = larger(top, sc[kt][i]);
+            return top;
+        };
+        // The weights' divisor follows the largest score only when that has left it behind by 2^8: sums
+        // and weights stay far from fp32's and fp16's ends, and the results are seldom rescaled.
+        auto follow = [&](float top) {
             if (__any(top * c > m + 8.0f)) {
-                top = fmaxf(top, __shfl_xor(top, 32)) * c;
-                const float nm = fmaxf(m, top);
+                top = larger(top, __shfl_xor(top, 32)) * c;
+                const float nm = larger(m, top);
                 const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - nm);
                 m = nm;
                 l *= keep;
@@ -361,125 +407,157 @@ struct Attend {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[d][i] *= keep;
             }
-            const float base = m == -INFINITY ? 0.0f : -m;
+            return m == -INFINITY ? 0.0f : -m;
+        };
+        auto exponent = [&](const f32x16* sc, int x, int e, float base) {
+            return __builtin_fmaf(sc[x >> 3][2 * (x & 7) + e], c, base);
+        };
+        auto weight = [&](u32x4* w, int x, float a, float b) {
+            l += a + b;
+            w[x >> 2][x & 3] = pack16<Half>(a, b);
+        };
+        // A step whose keys every row sees: sc its scores, top their largest; the next step's into nx.
+        auto open_step = [&](int32_t x, const f32x16* sc, f32x16* nx, float& top) {
+            const float base = follow(top);
+            const uint32_t ka = keys_at(x + 1), va = values_at(x);
+            constexpr int n = 2 * KS;
+            u32x4 k[kAhead], w[4];
+            nx[0] = nx[1] = f32x16{};
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                float sum = 0.0f;
+            for (int u = 0; u < kAhead; ++u) k[u] = key_piece(ka, u);
+            float fa = exponent(sc, 0, 0, base), fb = exponent(sc, 0, 1, base), ea = 0.0f, eb = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][i], c, base));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][i + 1], c, base));
-                    sum += x + y;
-                    w[2 * kt + (i >> 3)][(i & 7) >> 1] = pack16<Half>(x, y);
+            for (int u = 0; u < n; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                nx[u & 1] = mfma32<Half>(k[u % kAhead], q[u >> 1], nx[u & 1]);
+                if (u + kAhead < n) k[u % kAhead] = key_piece(ka, u + kAhead);
+#pragma unroll
+                for (int y = u * kPairs / n; y < (u + 1) * kPairs / n; ++y) {
+                    const float na = __builtin_amdgcn_exp2f(fa), nb = __builtin_amdgcn_exp2f(fb);
+                    if (y + 1 < kPairs) {
+                        fa = exponent(sc, y + 1, 0, base);
+                        fb = exponent(sc, y + 1, 1, base);
+                    }
+                    if (y > 0) weight(w, y - 1, ea, eb);
+                    ea = na;
+                    eb = nb;
                 }
-                l += sum;
+            }
+            u32x4 v[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
+            weight(w, kPairs - 1, ea, eb);
+            top = nx[0][0];
+#pragma unroll
+            for (int u = 0; u < 4 * DT; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                o[u % DT] = mfma32<Half>(v[u % kAhead], w[u / DT], o[u % DT]);
+                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(va, u + kAhead);
+#pragma unroll
+                for (int y = u * 32 / (4 * DT); y < (u + 1) * 32 / (4 * DT); ++y) top = larger(top, nx[y >> 4][y & 15]);
             }
         };
-        auto values = [&](uint32_t at, int d, int kk) {
-            const uint32_t x = at + kKeys + v_read[d & 1] + (uint32_t)((d >> 1) * 128 + 16 * kk * kRow);
-            const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 8 * kRow);
-            return u32x4{lo.x, lo.y, up.x, up.y};
-        };
-        int32_t s = t.s0, id[4];
-        auto ids = [&](int32_t x) {
-#pragma unroll
-            for (int b = 0; b < 4; ++b) id[b] = block_id(t, t.block0 + 4 * x + b);
-        };
-        uint32_t bad, next_bad = 0;                  // of the step's four blocks, those outside the cache
-        auto issue = [&](int32_t x) {
-            const int32_t b = t.block0 + 4 * x + wave;
-            const int32_t mine = wave == 0 ? id[0] : wave == 1 ? id[1] : wave == 2 ? id[2] : id[3];
-            const uint32_t to = tile + ((x - t.s0) & 1) * kStage + wave * (RK_BLOCK_TOKENS * kRow);
-            load_keys(t, b, mine, to);
-            load_values(t, b, mine, to + kKeys);
-            next_bad = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (bad_block(t, t.block0 + 4 * x + k, id[k])) next_bad |= 1u << k;
-        };
-        auto arrive = [&]() {                        // step s is there; the next one's loads begin
-            bad = next_bad;
-            __builtin_amdgcn_s_waitcnt(0);           // this wavefront's part of the step has come
-            __builtin_amdgcn_s_barrier();            // ... everyone's, and everyone has read the other stage
+        int32_t s = t.s0;
+        Step now, next, then;
+        // Step s + 1's keys and step s's values are there, and everyone has read what came before; the loads of those
+        // after them begin.
+        auto arrive = [&]() {
+            __builtin_amdgcn_s_waitcnt(0);
+            __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (s + 1 < t.s1) {
-                issue(s + 1);
-                ids(s + 2);
+                issue_values(s + 1, next);
+                if (s + 2 < t.s1) issue_keys(s + 2, then);
             }
-            return tile + ((s - t.s0) & 1) * kStage;
+        };
+        auto advance = [&]() {
+            ++s;
+            now = next;
+            next = then;
+            then = look(s + 2);
         };
         __syncthreads();                             // the LDS is the last tile's until here
-        ids(s);
-        issue(s);
-        ids(s + 1);
-        // the steps whose keys every row sees, if their blocks are good
-        const int32_t open = (all_see + 1 - t.block0 * RK_BLOCK_TOKENS) / kWideKeys, s_open = open < t.s1 ? open : t.s1;
-        for (; s < s_open && !next_bad; ++s) {
-            const uint32_t at = arrive();
-            f32x16 sc[2];
-            u32x4 w[4];
-            scores(at, sc);
-            weights(sc, w);
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk) o[d] = mfma32<Half>(values(at, d, kk), w[kk], o[d]);
+        now = look(s);
+        next = look(s + 1);
+        then = look(s + 2);
+        issue_keys(s, now);
+        issue_values(s, now);
+        if (s + 1 < t.s1) issue_keys(s + 1, next);
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        f32x16 sa[2], sb[2];
+        scores(keys_at(s), sa);
+        // the steps whose keys every row sees, if their blocks are good, but the last
+        const int32_t open = (all_see + 1 - t.block0 * RK_BLOCK_TOKENS) / kWideKeys, s_open = open < t.s1 - 1 ? open : t.s1 - 1;
+        float top = highest(sa);
+        while (s + 1 < s_open && !(now.bad | next.bad)) {
+            arrive();
+            open_step(s, sa, sb, top);
+            advance();
+            arrive();
+            open_step(s, sb, sa, top);
+            advance();
         }
-        for (; s < t.s1; ++s) {
-            const uint32_t at = arrive();
+        for (;;) {
+            arrive();
             const int32_t key0 = (t.block0 + 4 * s) * RK_BLOCK_TOKENS;
-            f32x16 sc[2];
+            const bool masked = key0 + kWideKeys - 1 > all_see;
+            if (masked || now.bad) {
+                if (now.bad) report_bad();
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int x = 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3);
+                        if (key0 + x > last || ((now.bad >> (x >> 4)) & 1)) sa[kt][i] = -INFINITY;
+                    }
+            }
+            const float base = follow(highest(sa));
             u32x4 w[4];
-            scores(at, sc);
-            if (bad) report_bad();
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int x = 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3);
-                    if (key0 + x > last || ((bad >> (x >> 4)) & 1)) sc[kt][i] = -INFINITY;
-                }
-            weights(sc, w);
+            for (int x = 0; x < kPairs; ++x)
+                weight(w, x, __builtin_amdgcn_exp2f(exponent(sa, x, 0, base)), __builtin_amdgcn_exp2f(exponent(sa, x, 1, base)));
             // A value that is not finite, where some row does not see it, must not meet that row's weight of 0: the
             // finite values go through the product, the others one by one to the rows that see them.
+            const uint32_t va = values_at(s);
             bool odd = false;
-            if (t.mask)
+            if (masked && t.mask)
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        const u32x4 v = values(at, d, kk);
-                        odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
-                    }
+                for (int x = 0; x < 4 * DT; ++x) {
+                    const u32x4 v = value_piece(va, x);
+                    odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
+                }
             odd = __any(odd);
             asm volatile("" ::: "memory");           // (read again below, not kept)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    u32x4 v = values(at, d, kk);
-                    if (odd) {
-                        v.x = finite_or_zero<Half>(v.x);
-                        v.y = finite_or_zero<Half>(v.y);
-                        v.z = finite_or_zero<Half>(v.z);
-                        v.w = finite_or_zero<Half>(v.w);
-                    }
-                    o[d] = mfma32<Half>(v, w[kk], o[d]);
+            for (int x = 0; x < 4 * DT; ++x) {
+                u32x4 v = value_piece(va, x);
+                if (odd) {
+                    v.x = finite_or_zero<Half>(v.x);
+                    v.y = finite_or_zero<Half>(v.y);
+                    v.z = finite_or_zero<Half>(v.z);
+                    v.w = finite_or_zero<Half>(v.w);
                 }
+                o[x % DT] = mfma32<Half>(v, w[x / DT], o[x % DT]);
+            }
             for (int x = 0; odd && x < kWideKeys; ++x) {
                 const bool sees = key0 + x <= last;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const uint32_t piece = (uint32_t)(4 * d + g) ^ (x & 7);
-                        const u32x2 v = lds_read8(at + kKeys + x * kRow + (piece << 4) + 8 * hi);
+                        const uint32_t piece = (uint32_t)(4 * d + g) ^ turn(x & 15);
+                        const u32x2 v = lds_read8(va + x * kRow + (piece << 4) + 8 * hi);
                         o[d][4 * g] += sees && not_finite<Half>(v.x & 0xffffu) ? unpack16<Half>(v.x & 0xffffu) : 0.0f;
                         o[d][4 * g + 1] += sees && not_finite<Half>(v.x >> 16) ? unpack16<Half>(v.x >> 16) : 0.0f;
                         o[d][4 * g + 2] += sees && not_finite<Half>(v.y & 0xffffu) ? unpack16<Half>(v.y & 0xffffu) : 0.0f;
                         o[d][4 * g + 3] += sees && not_finite<Half>(v.y >> 16) ? unpack16<Half>(v.y >> 16) : 0.0f;
                     }
             }
+            if (s + 1 >= t.s1) break;
+            scores(keys_at(s + 1), sa);
+            advance();
         }
         l += __shfl_xor(l, 32);
         if (r >= t.tokens * G) return;
@@ -544,14 +622,14 @@ struct Attend {
             m[n] = -INFINITY;
             l[n] = 0.0f;
         }
-        uint32_t k_read[2], v_read[4];
+        uint32_t k_read[kTurn / 4], v_read[kTurn / 2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) k_read[x] = col * kRow + (((4 * x + g) ^ (col & 7)) << 4);
+        for (int x = 0; x < kTurn / 4; ++x) k_read[x] = col * kRow + (((4 * x + g) ^ turn(col)) << 4);
         {
             const uint32_t vr = 4 * g + (col >> 2);
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                v_read[x] = vr * kRow + (((2 * x + ((lane & 3) >> 1)) ^ (vr & 7)) << 4) + 8 * (lane & 1);
+            for (int x = 0; x < kTurn / 2; ++x)
+                v_read[x] = vr * kRow + (((2 * x + ((lane & 3) >> 1)) ^ turn(vr)) << 4) + 8 * (lane & 1);
         }
         const uint32_t keys = tile + wave * (64 * kRow), vals = keys + 32 * kRow;
         // this wavefront's steps: 32 keys at 128 s + 32 wave
@@ -569,7 +647,7 @@ struct Attend {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 load_keys(t, first_block + 8 * x + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
-                if (bad_block(t, first_block + 8 * x + b, id[b])) next_bad |= 1u << b;
+                next_bad |= (bad_block(id[b]) ? 1u : 0u) << b;
             }
         };
         auto issue_values = [&](int32_t x) {
@@ -584,7 +662,8 @@ struct Attend {
                 for (int n = 0; n < NQ; ++n) sc[n][kt] = f32x4{};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const u32x4 k = lds_read16(keys + k_read[ks & 1] + (uint32_t)(kt * 16 * kRow + (ks >> 1) * 128));
+                    const u32x4 k = lds_read16(keys + k_read[ks % (kTurn / 4)] +
+                                               (uint32_t)(kt * 16 * kRow + ks / (kTurn / 4) * (16 * kTurn)));
 #pragma unroll
                     for (int n = 0; n < NQ; ++n) sc[n][kt] = mfma16<Half>(k, q[n][ks], sc[n][kt]);
                 }
@@ -621,7 +700,7 @@ struct Attend {
             }
         };
         auto values = [&](int d) {
-            const uint32_t x = vals + v_read[d & 3] + (uint32_t)((d >> 2) * 128);
+            const uint32_t x = vals + v_read[d % (kTurn / 2)] + (uint32_t)(d / (kTurn / 2) * (16 * kTurn));
             const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
             return u32x4{lo.x, lo.y, up.x, up.y};
         };
@@ -712,7 +791,7 @@ struct Attend {
             for (int x = 0; odd && x < 32; ++x)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ (x & 7);
+                    const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ turn(x & 15);
                     const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
 #pragma unroll
                     for (int n = 0; n < NQ; ++n) {
