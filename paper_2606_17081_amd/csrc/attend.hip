@@ -17,8 +17,11 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kWideRows = 128, kWideKeys = 64;       // a wide step: 32 rows a wavefront, 64 keys
 constexpr int kNarrowRows = 32, kNarrowKeys = 128;   // a narrow step: 32 keys a wavefront
-constexpr uint32_t kWideCost = 2, kNarrowCost = 3;   // of a step, relative to each other
-constexpr uint32_t kLeast = 3;                       // cost that a workgroup takes at least: a step
+// What a step of a tile costs, and its beginning and end, relative to each other; a workgroup takes at least one
+// of both, so that a tile's parts follow each other without a gap.
+constexpr uint32_t kWideCost = 2, kNarrowCost = 2, kWideEnds = 6, kNarrowEnds = 6;
+constexpr uint32_t kLeast = 8;
+static_assert(kLeast >= kWideCost + kWideEnds && kLeast >= kNarrowCost + kNarrowEnds, "a step begins in every piece");
 constexpr int kShareBlocks = 4;                      // shorter prefixes are not worth joining their parts
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 
@@ -103,6 +106,23 @@ __device__ __forceinline__ bool not_finite(uint32_t x)
     return (x & e & 0xffffu) == (e & 0xffffu) || (x & e & 0xffff0000u) == (e & 0xffff0000u);
 }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// The larger, half by half, of x and v's values without their signs: not finite if one of them is not.
+__device__ __forceinline__ u16x2 without_sign(u16x2 x, u32x4 v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x = __builtin_elementwise_max(x, __builtin_bit_cast(u16x2, v[i] & 0x7fff7fffu));
+    return x;
+}
+
+// The 16-bit value x if it is not finite and its row sees it, else 0.
+template <bool Half>
+__device__ __forceinline__ float only_odd(bool sees, uint32_t x)
+{
+    return sees && not_finite<Half>(x) ? unpack16<Half>(x) : 0.0f;
+}
+
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 
 __device__ __forceinline__ u32x4 lds_read16(uint32_t at)
@@ -112,6 +132,14 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t at)
 __device__ __forceinline__ u32x2 lds_read8(uint32_t at)
 {
     return *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>((lds_u8*)(uintptr_t)at);
+}
+__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x)
+{
+    *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((lds_u8*)(uintptr_t)at) = x;
+}
+__device__ __forceinline__ void lds_write8(uint32_t at, u32x2 x)
+{
+    *reinterpret_cast<__attribute__((address_space(3))) u32x2*>((lds_u8*)(uintptr_t)at) = x;
 }
 // Four rows of 16 values, transposed: the 16 lanes of a group each name 8 bytes (lane j: row j / 4, values
 // 4 (j % 4) ..), lane j gets value j of the four rows.
@@ -209,20 +237,43 @@ struct Attend {
     float* const join;                                // LDS: 2 * kWaves * kNarrowRows
     const int wave;
     const int32_t G;                                  // query heads of a key head
+    const uint32_t g_inverse;                         // 2^16 / G, rounded up: exact quotients of rows of a tile
     const float c;                                    // |scale| log2(e)
-    uint32_t k_at[NI], v_at[NI];                      // byte offsets, in a block, of the pieces that the lane loads
+    const uint32_t last_piece;                        // of a row: the bytes before it
+    // the pieces of a block that the lane loads: whole rows a load, or not
+    static constexpr bool kEven = 64 % NC == 0;
+    uint32_t k_at[kEven ? 2 : NI], v_at[kEven ? 2 : NI];
 
     __device__ __forceinline__ Attend(const AttendArgs& args, uint32_t lds, float* j, float scale)
         : p(args), tile(lds), join(j), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), G(args.a.Hq / args.a.Hkv),
-          c(scale)
+          g_inverse((65535 + args.a.Hq / args.a.Hkv) / (args.a.Hq / args.a.Hkv)), c(scale),
+          last_piece(2 * args.a.D - 16)
     {
         const int lane = threadIdx.x & 63;
+        if constexpr (kEven) {
+            const uint32_t r = lane / NC;
+            k_at[0] = r * (uint32_t)p.a.ks.token * 2;
+            v_at[0] = r * (uint32_t)p.a.vs.token * 2;
+            k_at[1] = v_at[1] = 16 * ((uint32_t)(lane % NC) ^ turn(r));
+        } else {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int x = 64 * i + lane, r = x / NC, piece = (x % NC) ^ turn(r);
-            const bool in = 8 * piece < p.a.D;        // pieces behind D are loaded as zeros
-            k_at[i] = in ? (uint32_t)(r * (int32_t)p.a.ks.token * 2 + 16 * piece) : 0x7ffffff0u;
-            v_at[i] = in ? (uint32_t)(r * (int32_t)p.a.vs.token * 2 + 16 * piece) : 0x7ffffff0u;
+            for (int i = 0; i < NI; ++i) {
+                const uint32_t x = 64 * i + lane, r = x / NC, piece = 16 * ((x % NC) ^ turn(r));
+                k_at[i] = r * (uint32_t)p.a.ks.token * 2 + (piece < last_piece ? piece : last_piece);
+                v_at[i] = r * (uint32_t)p.a.vs.token * 2 + (piece < last_piece ? piece : last_piece);
+            }
+        }
+    }
+
+    // The byte offset in a block of the piece that the lane loads i-th.  Pieces behind D, of rows that D does not fill, are
+    // the last one again: the query's are 0, and the results of such values are not written.
+    __device__ __forceinline__ uint32_t offset(const uint32_t* at, int i, int64_t token) const
+    {
+        if constexpr (!kEven) {
+            return at[i];
+        } else {
+            const uint32_t piece = at[1] ^ (16 * turn((uint32_t)i * (64 / NC)));
+            return at[0] + (uint32_t)(i * (64 / NC)) * (uint32_t)token * 2 + (piece < last_piece ? piece : last_piece);
         }
     }
 
@@ -244,7 +295,7 @@ struct Attend {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const uint32_t to = __builtin_amdgcn_readfirstlane(lds + 1024u * i);
-            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at[i]), "s"(rsrc)
+            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset(at, i, stride)), "s"(rsrc)
                          : "memory");
         }
     }
@@ -280,14 +331,16 @@ struct Attend {
         if ((threadIdx.x & 63) == 0) atomicOr(p.status, RK_DEV_BAD_BLOCK);
     }
 
+    __device__ __forceinline__ int32_t token_of(int32_t r) const { return (int32_t)((uint32_t)r * g_inverse >> 16); }
+
     // piece x of the row's query, its sign turned with the scale's
     __device__ __forceinline__ u32x4 query(const Tile& t, int32_t r, int32_t piece) const
     {
         u32x4 q = {0u, 0u, 0u, 0u};
-        const int32_t tok = r / G;
+        const int32_t tok = token_of(r);
         if (tok < t.tokens && 8 * piece < p.a.D) {
             q = *reinterpret_cast<const u32x4*>((const uint16_t*)p.a.q + (t.token + (int64_t)tok) * p.a.q_token +
-                                                (t.head * G + r % G) * p.a.q_head + 8 * piece);
+                                                (t.head * G + r - tok * G) * p.a.q_head + 8 * piece);
             if (p.a.scale < 0.0f) q ^= 0x80008000u;
         }
         return q;
@@ -295,12 +348,14 @@ struct Attend {
 
     __device__ __forceinline__ uint16_t* out_row(const Tile& t, int32_t r) const
     {
-        return (uint16_t*)p.a.out + (t.token + (int64_t)(r / G)) * p.a.out_token + (t.head * G + r % G) * p.a.out_head;
+        const int32_t tok = token_of(r);
+        return (uint16_t*)p.a.out + (t.token + (int64_t)tok) * p.a.out_token + (t.head * G + r - tok * G) * p.a.out_head;
     }
     __device__ __forceinline__ void put_lse(const Tile& t, int32_t r, float m, float l) const
     {
+        const int32_t tok = token_of(r);
         if (p.a.lse)
-            p.a.lse[(t.token + (int64_t)(r / G)) * p.a.Hq + t.head * G + r % G] =
+            p.a.lse[(t.token + (int64_t)tok) * p.a.Hq + t.head * G + r - tok * G] =
                 l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
     }
 
@@ -314,12 +369,9 @@ struct Attend {
         constexpr int KS = DP / 16, DT = DP / 32;
         const int lane = afresh(threadIdx.x & 63);
         const int hi = lane >> 5, r = 32 * wave + (lane & 31);
-        u32x4 q[KS];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = query(t, r, 2 * ks + hi);
         int32_t last = t.keys_end - 1;               // the last position that the row sees
         if (t.mask) {
-            const int32_t pos = t.pos + r / G;
+            const int32_t pos = t.pos + token_of(r);
             last = pos < last ? pos : last;
         }
         const int32_t all_see = t.mask ? (t.pos < t.keys_end - 1 ? t.pos : t.keys_end - 1) : t.keys_end - 1;
@@ -328,16 +380,13 @@ struct Attend {
         for (int d = 0; d < DT; ++d) o[d] = f32x16{};
         float m = -INFINITY, l = 0.0f;               // m: log2 of the weights' common divisor
         // LDS addresses in a stage, less what the unrolled loops add
-        uint32_t k_read[kTurn / 2], v_read[kTurn / 4], v_read8[kTurn / 4];       // (of rows 8 further)
+        uint32_t k_read[kTurn / 2], v_read[kTurn / 4];
         {
             const uint32_t row = lane & 31, vr = 4 * hi + ((lane & 15) >> 2), vp = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 #pragma unroll
             for (int x = 0; x < kTurn / 2; ++x) k_read[x] = row * kRow + (((2 * x + hi) ^ turn(row & 15)) << 4);
 #pragma unroll
-            for (int x = 0; x < kTurn / 4; ++x) {
-                v_read[x] = vr * kRow + (((4 * x + vp) ^ turn(vr)) << 4) + 8 * (lane & 1);
-                v_read8[x] = (vr + 8) * kRow + (((4 * x + vp) ^ turn(vr + 8)) << 4) + 8 * (lane & 1);
-            }
+            for (int x = 0; x < kTurn / 4; ++x) v_read[x] = vr * kRow + (((4 * x + vp) ^ turn(vr)) << 4) + 8 * (lane & 1);
         }
         constexpr uint32_t kKeys = kWideKeys * kRow;   // bytes of a step's keys; two of them, then two steps' values
         // Keys come two steps ahead, values one: while a step's weights are computed, the products of the next step's
@@ -370,10 +419,11 @@ struct Attend {
         auto value_piece = [&](uint32_t at, int x) {
             constexpr int n = kTurn / 4;
             const int d = x % DT, kk = x / DT;
-            const uint32_t y = at + (uint32_t)(d / n * (16 * kTurn) + 16 * kk * kRow);
-            const u32x2 lo = lds_read_columns(y + v_read[d % n]), up = lds_read_columns(y + v_read8[d % n]);
+            const uint32_t y = at + v_read[d % n] + (uint32_t)(d / n * (16 * kTurn) + 16 * kk * kRow);
+            const u32x2 lo = lds_read_columns(y), up = lds_read_columns((y ^ 16 * turn(8)) + 8 * kRow);
             return u32x4{lo.x, lo.y, up.x, up.y};
         };
+        u32x4 q[KS];
         auto scores = [&](uint32_t at, f32x16* sc) {
             u32x4 k[kAhead];
             sc[0] = sc[1] = f32x16{};
@@ -476,13 +526,15 @@ struct Attend {
             next = then;
             then = look(s + 2);
         };
-        __syncthreads();                             // the LDS is the last tile's until here
         now = look(s);
         next = look(s + 1);
         then = look(s + 2);
+        __syncthreads();                             // the LDS is the last tile's until here
         issue_keys(s, now);
         issue_values(s, now);
         if (s + 1 < t.s1) issue_keys(s + 1, next);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = query(t, r, 2 * ks + hi);
         __builtin_amdgcn_s_waitcnt(0);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -518,73 +570,104 @@ struct Attend {
 #pragma unroll
             for (int x = 0; x < kPairs; ++x)
                 weight(w, x, __builtin_amdgcn_exp2f(exponent(sa, x, 0, base)), __builtin_amdgcn_exp2f(exponent(sa, x, 1, base)));
-            // A value that is not finite, where some row does not see it, must not meet that row's weight of 0: the
-            // finite values go through the product, the others one by one to the rows that see them.
             const uint32_t va = values_at(s);
-            bool odd = false;
-            if (masked && t.mask)
+            if (masked && t.mask) {
+                // A value that is not finite must not meet the weight of 0 of a row that does not see it: such values
+                // are added to the rows that do, and are 0 in the product.  (All wavefronts decide alike.)
+                u16x2 most = {0, 0};
+#pragma unroll 4
+                for (int x = lane; x < kWideKeys * NC; x += 64) most = without_sign(most, lds_read16(va + 16 * x));
+                if (__any(not_finite<Half>(__builtin_bit_cast(uint32_t, most)))) {
+#pragma unroll 1
+                    for (int x = 0; x < kWideKeys; ++x) {
+                        const bool sees = key0 + x <= last;
 #pragma unroll
-                for (int x = 0; x < 4 * DT; ++x) {
-                    const u32x4 v = value_piece(va, x);
-                    odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
-                }
-            odd = __any(odd);
-            asm volatile("" ::: "memory");           // (read again below, not kept)
+                        for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int x = 0; x < 4 * DT; ++x) {
-                u32x4 v = value_piece(va, x);
-                if (odd) {
-                    v.x = finite_or_zero<Half>(v.x);
-                    v.y = finite_or_zero<Half>(v.y);
-                    v.z = finite_or_zero<Half>(v.z);
-                    v.w = finite_or_zero<Half>(v.w);
-                }
-                o[x % DT] = mfma32<Half>(v, w[x / DT], o[x % DT]);
-            }
-            for (int x = 0; odd && x < kWideKeys; ++x) {
-                const bool sees = key0 + x <= last;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const uint32_t piece = (uint32_t)(4 * d + g) ^ turn(x & 15);
-                        const u32x2 v = lds_read8(va + x * kRow + (piece << 4) + 8 * hi);
-                        o[d][4 * g] += sees && not_finite<Half>(v.x & 0xffffu) ? unpack16<Half>(v.x & 0xffffu) : 0.0f;
-                        o[d][4 * g + 1] += sees && not_finite<Half>(v.x >> 16) ? unpack16<Half>(v.x >> 16) : 0.0f;
-                        o[d][4 * g + 2] += sees && not_finite<Half>(v.y & 0xffffu) ? unpack16<Half>(v.y & 0xffffu) : 0.0f;
-                        o[d][4 * g + 3] += sees && not_finite<Half>(v.y >> 16) ? unpack16<Half>(v.y >> 16) : 0.0f;
+                            for (int g = 0; g < 4; ++g) {
+                                __builtin_amdgcn_sched_barrier(0);
+                                const uint32_t piece = (uint32_t)(4 * d + g) ^ turn(x & 15);
+                                const u32x2 v = lds_read8(va + x * kRow + (piece << 4) + 8 * hi);
+                                o[d][4 * g] += only_odd<Half>(sees, v.x & 0xffffu);
+                                o[d][4 * g + 1] += only_odd<Half>(sees, v.x >> 16);
+                                o[d][4 * g + 2] += only_odd<Half>(sees, v.y & 0xffffu);
+                                o[d][4 * g + 3] += only_odd<Half>(sees, v.y >> 16);
+                            }
                     }
+                    __builtin_amdgcn_s_waitcnt(0xc07f);              // (lgkmcnt 0: loads to LDS stay under way)
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    for (int x = 64 * wave + lane; x < kWideKeys * NC; x += kThreads) {
+                        const u32x4 v = lds_read16(va + 16 * x);
+                        lds_write16(va + 16 * x, u32x4{finite_or_zero<Half>(v.x), finite_or_zero<Half>(v.y),
+                                                       finite_or_zero<Half>(v.z), finite_or_zero<Half>(v.w)});
+                    }
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                }
+            }
+            u32x4 v[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
+#pragma unroll
+            for (int u = 0; u < 4 * DT; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                o[u % DT] = mfma32<Half>(v[u % kAhead], w[u / DT], o[u % DT]);
+                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(va, u + kAhead);
             }
             if (s + 1 >= t.s1) break;
             scores(keys_at(s + 1), sa);
             advance();
         }
         l += __shfl_xor(l, 32);
-        if (r >= t.tokens * G) return;
+        // Out through LDS, so that whole rows are written: a lane's own pieces of a row are 8 or 16 bytes each, and writing those
+        // took 20 us a tile.  The keys' stages are free: everyone has read the last keys.
+        const uint32_t mine = tile + wave * (32 * kRow);
+        const int32_t rows = t.tokens * G - 32 * wave;
+        const int late = afresh(lane);
+        auto written = [&](auto&& put) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < NC / 2; ++i) {
+                const int x = 64 * i + late, row = x / NC, piece = x % NC;
+                const u32x4 v = lds_read16(mine + row * kRow + ((piece ^ turn(row & 15)) << 4));
+                if (row < rows) put(row, piece, v);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        };
+        const uint32_t row_at = mine + (late & 31) * kRow, turned = turn(late & 15);
         if (t.part) {
-            float* to = t.part + (int64_t)r * DP + 4 * hi;
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<f32x4*>(to + 32 * d + 8 * g) =
-                        f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
-            if (hi == 0) {
+                for (int d = 0; d < DT / 2; ++d)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x16& y = o[half * (DT / 2) + d];
+                        lds_write16(row_at + (((8 * d + 2 * g + hi) ^ turned) << 4),
+                                    __builtin_bit_cast(u32x4, f32x4{y[4 * g], y[4 * g + 1], y[4 * g + 2], y[4 * g + 3]}));
+                    }
+                float* to = t.part + (int64_t)(32 * wave) * DP + half * (DP / 2);
+                written([&](int row, int piece, u32x4 v) { *reinterpret_cast<u32x4*>(to + row * DP + 4 * piece) = v; });
+            }
+            if (hi == 0 && (lane & 31) < rows) {
                 t.part_ml[2 * r] = m;
                 t.part_ml[2 * r + 1] = l;
             }
         } else {
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            uint16_t* to = out_row(t, r) + 4 * hi;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                    if (32 * d + 8 * g < p.a.D)
-                        *reinterpret_cast<u32x2*>(to + 32 * d + 8 * g) =
-                            u32x2{pack16<Half>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv),
-                                  pack16<Half>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv)};
-            if (hi == 0) put_lse(t, r, m, l);
+                    lds_write8(row_at + (((4 * d + g) ^ turned) << 4) + 8 * hi,
+                               u32x2{pack16<Half>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv),
+                                     pack16<Half>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv)});
+            written([&](int row, int piece, u32x4 v) {
+                if (8 * piece < p.a.D) *reinterpret_cast<u32x4*>(out_row(t, 32 * wave + row) + 8 * piece) = v;
+            });
+            if (hi == 0 && (lane & 31) < rows) put_lse(t, r, m, l);
         }
     }
 
@@ -608,7 +691,7 @@ struct Attend {
             for (int ks = 0; ks < KS; ++ks) q[n][ks] = query(t, r, 4 * ks + g);
             last[n] = t.keys_end - 1;
             if (t.mask) {
-                const int32_t pos = t.pos + r / G;
+                const int32_t pos = t.pos + token_of(r);
                 last[n] = pos < last[n] ? pos : last[n];
             }
         }
@@ -752,6 +835,7 @@ struct Attend {
         }
         for (; s < s1; ++s) {
             const int32_t key0 = (first_block + 8 * s) * RK_BLOCK_TOKENS;
+            const bool masked = key0 + 31 > all_see;
             f32x4 sc[NQ][2];
             u32x4 w[NQ];
             wait_keys();
@@ -767,41 +851,41 @@ struct Attend {
                         if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
             weights(sc, w);
             wait_values();
-            bool odd = false;                        // (as for wide tiles)
-            if (t.mask && t.tokens > 1)
+            if (masked && t.mask && t.tokens > 1) {                      // (as for wide tiles, of values of the wavefront's own)
+                u16x2 most = {0, 0};
+#pragma unroll 4
+                for (int x = lane; x < 32 * NC; x += 64) most = without_sign(most, lds_read16(vals + 16 * x));
+                if (__any(not_finite<Half>(__builtin_bit_cast(uint32_t, most)))) {
+#pragma unroll 1
+                    for (int x = 0; x < 32; ++x)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const u32x4 v = values(d);
-                    odd = odd || not_finite<Half>(v.x) || not_finite<Half>(v.y) || not_finite<Half>(v.z) || not_finite<Half>(v.w);
+                        for (int d = 0; d < DT; ++d) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ turn(x & 15);
+                            const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n) {
+                                const bool sees = key0 + x <= last[n];
+                                o[n][d][0] += only_odd<Half>(sees, v.x & 0xffffu);
+                                o[n][d][1] += only_odd<Half>(sees, v.x >> 16);
+                                o[n][d][2] += only_odd<Half>(sees, v.y & 0xffffu);
+                                o[n][d][3] += only_odd<Half>(sees, v.y >> 16);
+                            }
+                        }
+                    for (int x = lane; x < 32 * NC; x += 64) {
+                        const u32x4 v = lds_read16(vals + 16 * x);
+                        lds_write16(vals + 16 * x, u32x4{finite_or_zero<Half>(v.x), finite_or_zero<Half>(v.y),
+                                                         finite_or_zero<Half>(v.z), finite_or_zero<Half>(v.w)});
+                    }
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 }
-            odd = __any(odd);
-            asm volatile("" ::: "memory");
+            }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                u32x4 v = values(d);
-                if (odd) {
-                    v.x = finite_or_zero<Half>(v.x);
-                    v.y = finite_or_zero<Half>(v.y);
-                    v.z = finite_or_zero<Half>(v.z);
-                    v.w = finite_or_zero<Half>(v.w);
-                }
+                const u32x4 v = values(d);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
             }
-            for (int x = 0; odd && x < 32; ++x)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ turn(x & 15);
-                    const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) {
-                        const bool sees = key0 + x <= last[n];
-                        o[n][d][0] += sees && not_finite<Half>(v.x & 0xffffu) ? unpack16<Half>(v.x & 0xffffu) : 0.0f;
-                        o[n][d][1] += sees && not_finite<Half>(v.x >> 16) ? unpack16<Half>(v.x >> 16) : 0.0f;
-                        o[n][d][2] += sees && not_finite<Half>(v.y & 0xffffu) ? unpack16<Half>(v.y & 0xffffu) : 0.0f;
-                        o[n][d][3] += sees && not_finite<Half>(v.y >> 16) ? unpack16<Half>(v.y >> 16) : 0.0f;
-                    }
-                }
             values_read();
         }
         // the four wavefronts' results: rows of DP floats in LDS, wavefront after wavefront
@@ -881,6 +965,20 @@ __device__ __forceinline__ int32_t steps_for(int64_t keys, int32_t per_step)
     return keys > 0 ? (int32_t)((keys + per_step - 1) / per_step) : 1;
 }
 
+// A tile's extent along the line, and the steps of it that begin in its first `length`: the first at its start, the
+// s-th behind the ends' cost and s steps.
+template <bool Wide>
+__device__ __forceinline__ uint64_t extent(int32_t steps)
+{
+    return (Wide ? kWideEnds : kNarrowEnds) + (uint64_t)steps * (Wide ? kWideCost : kNarrowCost);
+}
+template <bool Wide>
+__device__ __forceinline__ uint64_t steps_before(uint64_t length)
+{
+    constexpr uint32_t ends = Wide ? kWideEnds : kNarrowEnds, cost = Wide ? kWideCost : kNarrowCost;
+    return length == 0 ? 0 : length <= ends ? 1 : quotient(length - 1 - ends, cost) + 1;
+}
+
 __device__ __forceinline__ Segment own_segment(const Request& r, int32_t G)
 {
     Segment s{};
@@ -894,15 +992,15 @@ __device__ __forceinline__ Segment own_segment(const Request& r, int32_t G)
     s.tiles = (s.tokens + s.per - 1) / s.per;
     if (!s.wide) {
         s.steps0 = steps_for(own, kNarrowKeys);
-        s.pair = s.cost = (uint64_t)s.steps0 * kNarrowCost;
+        s.pair = s.cost = extent<false>(s.steps0);
     } else if (s.tiles == 1) {
         s.steps0 = steps_for(own, kWideKeys);
-        s.pair = s.cost = (uint64_t)s.steps0 * kWideCost;
+        s.pair = s.cost = extent<true>(s.steps0);
     } else {
         s.grows = true;
         s.steps0 = steps_for(own - s.tokens + s.per, kWideKeys);
         const int32_t last = steps_for(own - s.tokens + (int64_t)s.tiles * s.per, kWideKeys);
-        s.pair = ((uint64_t)s.steps0 + last + 2) * kWideCost;
+        s.pair = extent<true>(s.steps0) + extent<true>(last) + 2 * kWideCost;
         s.cost = s.pair * ((s.tiles + 1) / 2);
     }
     return s;
@@ -917,7 +1015,7 @@ __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks
     s.per = s.wide ? kWideRows / G : s.tokens;
     s.tiles = (s.tokens + s.per - 1) / s.per;
     s.steps0 = steps_for((int64_t)blocks * RK_BLOCK_TOKENS, s.wide ? kWideKeys : kNarrowKeys);
-    s.pair = (uint64_t)s.steps0 * (s.wide ? kWideCost : kNarrowCost);
+    s.pair = s.wide ? extent<true>(s.steps0) : extent<false>(s.steps0);
     s.cost = s.pair * s.tiles;
     return s;
 }
@@ -943,7 +1041,6 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
     const rk_attention& a = p.a;
     const int32_t G = work.G, B = p.n, tid = threadIdx.x;
     constexpr int DP = A::kHead;
-    constexpr uint32_t cost = Wide ? kWideCost : kNarrowCost;
     uint64_t x = from;
     while (x < to && i < B) {
         Request r = req[i];
@@ -984,7 +1081,7 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
                 return steps_for((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWideKeys);
             };
             const int32_t k = sg.tiles - 1 - j;
-            const uint64_t first = (uint64_t)steps_of(j) * cost;
+            const uint64_t first = extent<true>(steps_of(j));
             steps = steps_of(j);
             left = first;
             if (in >= first) {               // the pair's other tile
@@ -996,8 +1093,8 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
             }
         }
         // the steps of the tile that begin in [from, to)
-        const uint64_t s_end = quotient_up(to - x + in, cost);
-        const int32_t s0 = (int32_t)quotient_up(in, cost), s1 = s_end < (uint64_t)steps ? (int32_t)s_end : steps;
+        const uint64_t s_end = steps_before<Wide>(to - x + in);
+        const int32_t s0 = (int32_t)steps_before<Wide>(in), s1 = s_end < (uint64_t)steps ? (int32_t)s_end : steps;
         if (!nothing && s0 < s1) {
             Tile t;
             t.token = r.q0 + j * sg.per;
@@ -1029,8 +1126,8 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
                 t.part_ml = p.whole_ml + row * 2;
             }
             if (s0 == 0 && (joined || !whole)) {
-                // workgroups that the tile's steps fall to: the last step begins (steps - 1) costs behind its start
-                const uint64_t of_mine = x - in - from + (uint64_t)(steps - 1) * cost;
+                // workgroups that the tile's steps fall to, up to the one in whose piece the last begins
+                const uint64_t of_mine = x - in - from + (steps > 1 ? extent<Wide>(steps - 1) : 0);
                 const int32_t n = (int32_t)quotient(of_mine, each) + 1;
                 if (joined) {
                     for (int32_t k = tid; k < t.tokens; k += kThreads)
