@@ -36,6 +36,7 @@ __device__ __forceinline__ int64_t group_incl_sum(int64_t v, int64_t* tmp)
 // the groups, by a population count over 64-request masks; a counting sort by
 // group number, 6 bits a pass, gives the stable order.
 constexpr int kGroupSlots = 2 * kBatchMax;
+constexpr int kFewGroups = 128;              // batches up to this are done in one launch
 
 struct GroupLds {
     uint64_t key[kGroupSlots];
@@ -82,6 +83,36 @@ __device__ __forceinline__ void sort_pass(const int32_t* el, const int32_t* key,
     for (int u = 0; u < kPer; ++u)
         if (64 * (kPer * wave + u) + lane < B) out[hist[digit[u] * 16 + wave] + rank[u]] = el[u];
     __syncthreads();
+}
+
+// Leading blocks that request i's chain has in common with request f's, by a team of 16 lanes (sub: the lane's place,
+// shift: its first lane); 0 for lanes with pair = false, which take part all the same.  Chained hashes agree up to the first block that
+// differs and nowhere after it, so each round tests 16 positions and keeps a sixteenth of the interval.
+__device__ __forceinline__ int32_t common_blocks(const uint64_t* __restrict__ chains, const int64_t* __restrict__ chain_off,
+                                                 int32_t i, int32_t f, bool pair, int sub, int shift)
+{
+    int64_t a = 0, b = 0;
+    int32_t have = 0, most = 0;              // `have` blocks agree; at most `most` do
+    if (pair) {
+        a = chain_off[i];
+        b = chain_off[f];
+        const int64_t la = chain_off[i + 1] - a, lb = chain_off[f + 1] - b, l = la < lb ? la : lb;
+        most = l > 0 ? (int32_t)(l < 0x7ffffffe ? l : 0x7ffffffe) : 0;
+    }
+    while (__any(have < most)) {
+        const int64_t w = most - have;
+        const int32_t x = have + (int32_t)((int64_t)(sub + 1) * w / 16);       // a count of blocks, <= most
+        bool same = false;
+        if (have < most) same = x == have || chains[a + x - 1] == chains[b + x - 1];
+        const uint32_t m = (uint32_t)(__ballot(same) >> shift) & 0xffffu;
+        if (have < most) {
+            const int k = __popc(m);         // the first k samples agree
+            const int32_t agreed = have + (int32_t)((int64_t)k * w / 16);
+            if (k < 16) most = have + (int32_t)((int64_t)(k + 1) * w / 16) - 1;
+            have = agreed;
+        }
+    }
+    return have;
 }
 
 __global__ __launch_bounds__(kBatchThreads) void group_kernel(int32_t B, const uint64_t* __restrict__ chains,
@@ -163,7 +194,9 @@ __global__ __launch_bounds__(kBatchThreads) void group_kernel(int32_t B, const u
             const int32_t g = kPer * tid + u;
             if (g < B) {
                 group_off[g] = at;
-                shared[g] = n[u] > 1 ? 0x7fffffff : 0;       // the next kernel's minimum
+                const int32_t least = n[u] > 1 ? 0x7fffffff : 0;
+                if (B <= kFewGroups) s.off[g] = least;       // (a thread's own places are read)
+                else shared[g] = least;                      // the next kernel's minimum
             }
             at += n[u];
         }
@@ -171,6 +204,28 @@ __global__ __launch_bounds__(kBatchThreads) void group_kernel(int32_t B, const u
     if (tid == 0) {
         group_off[B] = B;
         *n_groups = G;
+    }
+    if (B <= kFewGroups) {
+        // the groups' common blocks, by the teams of this workgroup
+        int32_t* first_of = reinterpret_cast<int32_t*>(s.key) + 2 * kBatchThreads;
+        int32_t* group_of = first_of + kFewGroups;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int32_t i = 64 * (kPer * wave + u) + lane;
+            if (i < B) {
+                first_of[i] = first[u];
+                group_of[i] = group[u];
+            }
+        }
+        __syncthreads();
+        for (int32_t i0 = 0; i0 < B; i0 += kBatchThreads / 16) {
+            const int32_t i = i0 + (tid >> 4), f = i < B ? first_of[i] : i;
+            const int32_t n = common_blocks(chains, chain_off, i, f, f != i, tid & 15, tid & 48);
+            if (f != i && (tid & 15) == 0) atomicMin(&s.off[group_of[i]], n);
+        }
+        __syncthreads();
+        if (tid < B) shared[tid] = s.off[tid];
     }
     // the order; the hash table's memory is free by now
     int32_t* hist = reinterpret_cast<int32_t*>(s.key);
@@ -197,10 +252,8 @@ __global__ __launch_bounds__(kBatchThreads) void group_kernel(int32_t B, const u
     }
 }
 
-// shared_g: the least number of leading blocks that a member has in common with its group's first
-// request.  A group of 16 lanes per member: chained hashes agree up to the first block that
-// differs and nowhere after it, so each round tests 16 positions and keeps a seventeenth of the
-// interval.
+// shared_g: the least number of leading blocks that a member has in common with its group's first request; a team of
+// 16 lanes per place in the order.
 __global__ __launch_bounds__(256) void common_kernel(int32_t B, const uint64_t* __restrict__ chains,
                                                      const int64_t* __restrict__ chain_off,
                                                      const int32_t* __restrict__ order,
@@ -219,36 +272,11 @@ __global__ __launch_bounds__(256) void common_kernel(int32_t B, const uint64_t* 
         const int32_t w = hi - lo;
         if (k < 16) hi = lo + (int32_t)((int64_t)(k + 1) * w / 17);
         if (k > 0) lo = lo + (int32_t)((int64_t)k * w / 17);
-        if (hi <= lo) hi = lo + 1;
     }
-    if (!in) lo = 0;
     const int32_t f = in ? order[group_off[lo]] : 0, i = in ? order[r] : 0;
     const bool pair = in && f != i;
-    int64_t a = 0, b = 0;
-    int32_t n = 0;                           // common blocks lie in [n_lo, n_hi]
-    if (pair) {
-        a = chain_off[i];
-        b = chain_off[f];
-        const int64_t la = chain_off[i + 1] - a, lb = chain_off[f + 1] - b, l = la < lb ? la : lb;
-        n = l > 0 ? (int32_t)(l < 0x7ffffffe ? l : 0x7ffffffe) : 0;
-    }
-    int32_t have = 0, most = n;              // `have` blocks agree; at most `most` do
-    while (__any(have < most)) {
-        // positions have + 1 .. most agree or not, in that order; sample 16 of them
-        const int64_t w = most - have;
-        const int32_t x = have + (int32_t)((int64_t)(sub + 1) * w / 16);       // a count of blocks, <= most
-        bool same = false;
-        if (have < most && x > have) same = chains[a + x - 1] == chains[b + x - 1];
-        else if (have < most) same = true;                                      // x == have: known
-        const uint32_t m = (uint32_t)(__ballot(same) >> shift) & 0xffffu;
-        if (have < most) {
-            const int k = __popc(m);         // the first k samples agree
-            const int32_t new_have = have + (int32_t)((int64_t)k * w / 16);
-            if (k < 16) most = have + (int32_t)((int64_t)(k + 1) * w / 16) - 1;
-            have = new_have;
-        }
-    }
-    if (pair && sub == 0) atomicMin(&shared[lo], have);
+    const int32_t n = common_blocks(chains, chain_off, i, f, pair, sub, shift);
+    if (pair && sub == 0) atomicMin(&shared[lo], n);
 }
 
 // --------------------------------------------------------------- block tables
@@ -264,7 +292,7 @@ struct TableLds {
     uint32_t base[kBatchMax];                // first of the request's blocks in the free list
     int64_t tok[kBatchMax + 1];              // tokens before the request's
     uint32_t fill[kBatchMax + 1];            // entries to write before the request's
-    int64_t tmp[16];
+    int64_t tmp[48];
     int32_t bad;
 };
 
@@ -290,14 +318,15 @@ __global__ __launch_bounds__(kBatchThreads) void tables_kernel(
     __shared__ TableLds s;
     const int tid = threadIdx.x;
     const bool tell = blockIdx.x == 0;       // one workgroup reports
+    const int32_t per = (B + kBatchThreads - 1) / kBatchThreads;             // requests of a thread, side by side
     if (tid == 0) s.bad = 0;
     __syncthreads();
     int32_t kv[kPer], nw[kPer], hv[kPer];
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
-        const int32_t i = kPer * tid + u;
+        const int32_t i = per * tid + u;
         kv[u] = nw[u] = hv[u] = 0;
-        if (i >= B) continue;
+        if (u >= per || i >= B) continue;
         kv[u] = kv_len[i];
         nw[u] = new_len[i];
         hv[u] = have[i];
@@ -321,9 +350,9 @@ __global__ __launch_bounds__(kBatchThreads) void tables_kernel(
     int64_t count[kPer], blocks = 0, tokens = 0, fills = 0;
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
-        const int32_t i = kPer * tid + u;
+        const int32_t i = per * tid + u;
         count[u] = 0;
-        if (i >= B) continue;
+        if (u >= per || i >= B) continue;
         int32_t f = i, lead = 0;
         if (groups) {
             const int32_t g = last_le(s.goff, B, i);
@@ -343,13 +372,37 @@ __global__ __launch_bounds__(kBatchThreads) void tables_kernel(
         tokens += nw[u];
         fills += need > hv[u] ? need - hv[u] : 0;
     }
-    int64_t blocks_at = group_incl_sum(blocks, s.tmp) - blocks;
-    int64_t tokens_at = group_incl_sum(tokens, s.tmp) - tokens;
-    int64_t fills_at = group_incl_sum(fills, s.tmp) - fills;
+    int64_t blocks_at = blocks, tokens_at = tokens, fills_at = fills;
+    {
+        const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t x = __shfl_up(blocks_at, d), y = __shfl_up(tokens_at, d), z = __shfl_up(fills_at, d);
+            if (lane >= d) {
+                blocks_at += x;
+                tokens_at += y;
+                fills_at += z;
+            }
+        }
+        if (lane == 63) {
+            s.tmp[wave] = blocks_at;
+            s.tmp[16 + wave] = tokens_at;
+            s.tmp[32 + wave] = fills_at;
+        }
+        __syncthreads();
+        blocks_at -= blocks;
+        tokens_at -= tokens;
+        fills_at -= fills;
+        for (int w = 0; w < wave; ++w) {
+            blocks_at += s.tmp[w];
+            tokens_at += s.tmp[16 + w];
+            fills_at += s.tmp[32 + w];
+        }
+    }
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
-        const int32_t i = kPer * tid + u;
-        if (i >= B) continue;
+        const int32_t i = per * tid + u;
+        if (u >= per || i >= B) continue;
         s.base[i] = blocks_at < 0x7fffffff ? (uint32_t)blocks_at : 0x7fffffffu;
         s.tok[i] = tokens_at;
         s.fill[i] = (uint32_t)fills_at;
@@ -458,7 +511,7 @@ int rk_prefix_groups(int32_t B, const uint64_t* chains, const int64_t* chain_off
     hipStream_t s = (hipStream_t)stream;
     hipLaunchKernelGGL(group_kernel, dim3(1), dim3(kBatchThreads), 0, s, B, chains, chain_off, min_blocks, order,
                        group_off, shared, n_groups, st);
-    if (B > 1)
+    if (B > kFewGroups)
         hipLaunchKernelGGL(common_kernel, dim3((unsigned)((B + 15) / 16)), dim3(256), 0, s, B, chains, chain_off, order,
                            group_off, shared);
     return hip_check(hipGetLastError(), "rk_prefix_groups launch");

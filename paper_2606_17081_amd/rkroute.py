@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import threading
 from typing import Optional
 
@@ -113,6 +114,8 @@ def library_available() -> bool:
 def lib():
     """Load librkroute.so; raises if it has not been built."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -157,7 +160,7 @@ def lib():
             L.rk_prefix_attention_workspace_size.restype = sz
             L.rk_prefix_attention_workspace_size.argtypes = [i64, i32, i32, i32, i32]
             L.rk_prefix_attention.restype = C.c_int
-            L.rk_prefix_attention.argtypes = [C.POINTER(Attention), vp, sz, vp]
+            L.rk_prefix_attention.argtypes = [vp, vp, sz, vp]
             _lib = L
     return _lib
 
@@ -383,24 +386,41 @@ def poa_estimate_noalloc(win_off, ep_win_off, n_rows: int, max_window: int, W: i
 
 
 # ------------------------------------------------------------------ a worker's step
+#
+# These run once or more per layer of a model on batches that take the GPU microseconds, so a call's own time counts: checks go
+# by device numbers and stride tuples, and arguments are passed as plain numbers.
+
+_NARROW = {}                                   # names of 16-bit types, filled with torch
+
+
+def _where(name, t):
+    """The number of the GPU that holds t."""
+    dev = t.get_device()
+    if dev < 0:
+        _torch()
+        raise RkError(f"{name} must be a CUDA tensor")
+    return dev
+
 
 class _On:
-    """Where a call with tensors on `device` runs: on the given stream, or on that device's current one.  Meanwhile
-    it is the current stream, so that what the call allocates is that stream's too."""
+    """Where a call with tensors on GPU `dev` runs: on the given stream, or on that GPU's current one (both as the raw
+    handle).  Meanwhile it is the current stream, so that what the call allocates is that stream's too."""
+    __slots__ = ("context", "dev")
 
-    def __init__(self, device, stream):
-        torch = _torch()
+    def __init__(self, dev, stream):
+        torch = _found_torch or _torch()
+        self.dev, self.context = dev, None
         if stream is not None:
-            if stream.device != device:
-                raise RkError(f"the stream is on {stream.device}, the tensors are on {device}")
+            if stream.device.index != dev:
+                raise RkError(f"the stream is on {stream.device}, the tensors are on cuda:{dev}")
             self.context = torch.cuda.stream(stream)
-        else:
-            self.context = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+        elif torch._C._cuda_getDevice() != dev:
+            self.context = torch.cuda.device(dev)
 
     def __enter__(self):
         if self.context is not None:
             self.context.__enter__()
-        return _stream()
+        return _found_torch._C._cuda_getCurrentRawStream(self.dev)
 
     def __exit__(self, *exc):
         if self.context is not None:
@@ -408,41 +428,43 @@ class _On:
         return False
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise RkError(f"{name} is on {t.device}, not on {device}")
-
-
-def _size(name, t, n):
-    if t is not None and t.numel() < n:
+def _flat(name, t, dtype, dev, n):
+    """The address of a contiguous tensor of at least n elements (None: of none)."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise RkError(f"{name} is on {t.device}, not on cuda:{dev}")
+    if t.dtype != dtype or not t.is_contiguous():
+        if not (name in _HASH_ARGS and t.dtype == _found_torch.uint64 and t.is_contiguous()):
+            raise RkError(f"{name} must be a contiguous CUDA tensor of {dtype}")
+    if t.numel() < n:
         raise RkError(f"{name} holds {t.numel()} elements, {n} needed")
+    return t.data_ptr()
 
 
 def prefix_groups(chains, chain_off, min_blocks: int = 1, order=None, group_off=None, shared=None, n_groups=None,
                   stream=None):
     """The batch ordered by shared prompt prefix (rk_prefix_groups): (order, group_off, shared, n_groups)."""
-    torch = _torch()
-    _need(chains, torch.uint64, "chains")
-    _need(chain_off, torch.int64, "chain_off")
-    if chain_off.numel() < 1:
-        raise RkError("chain_off is empty")
-    B, dev = chain_off.numel() - 1, chain_off.device
+    dev = _where("chain_off", chain_off)
     with _On(dev, stream) as st:
-        def out(t, n, dtype, name):
-            if t is None:
-                t = torch.empty(n, dtype=dtype, device=dev)
-            _need(t, dtype, name)
-            _size(name, t, n)
-            return t
-
-        order = out(order, B, torch.int32, "order")
-        group_off = out(group_off, B + 1, torch.int64, "group_off")
-        shared = out(shared, B, torch.int32, "shared")
-        n_groups = out(n_groups, 1, torch.int32, "n_groups")
-        _same_device(dev, chains=chains, order=order, group_off=group_off, shared=shared, n_groups=n_groups)
-        _check(lib().rk_prefix_groups(B, _ptr(chains), _ptr(chain_off), min_blocks, _ptr(order), _ptr(group_off),
-                                      _ptr(shared), _ptr(n_groups), st), "rk_prefix_groups")
+        torch = _found_torch
+        i32, i64 = torch.int32, torch.int64
+        B = chain_off.numel() - 1
+        if B < 0:
+            raise RkError("chain_off is empty")
+        at = chain_off.device
+        if order is None:
+            order = torch.empty(B, dtype=i32, device=at)
+        if group_off is None:
+            group_off = torch.empty(B + 1, dtype=i64, device=at)
+        if shared is None:
+            shared = torch.empty(B, dtype=i32, device=at)
+        if n_groups is None:
+            n_groups = torch.empty(1, dtype=i32, device=at)
+        _check(lib().rk_prefix_groups(
+            B, _flat("chains", chains, i64, dev, 0), _flat("chain_off", chain_off, i64, dev, 0), min_blocks,
+            _flat("order", order, i32, dev, B), _flat("group_off", group_off, i64, dev, B + 1),
+            _flat("shared", shared, i32, dev, B), _flat("n_groups", n_groups, i32, dev, 1), st), "rk_prefix_groups")
     return order, group_off, shared, n_groups
 
 
@@ -450,77 +472,107 @@ def block_tables(tables, kv_len, new_len, have, free_blocks, n_slots: int, group
                  q_off=None, taken=None, stream=None):
     """Block tables (in place) and slot map of a step (rk_block_tables): (tables, slots, q_off, taken).
     tables is [B, stride]; n_slots is the number of slots wanted, the step's new tokens or more."""
-    torch = _torch()
-    for t, name in ((tables, "tables"), (kv_len, "kv_len"), (new_len, "new_len"), (have, "have"),
-                    (free_blocks, "free_blocks"), (shared, "shared")):
-        _need(t, torch.int32, name)
-    _need(group_off, torch.int64, "group_off")
-    B, dev = kv_len.numel(), kv_len.device
-    if tables.dim() != 2 or tables.shape[0] < B:
-        raise RkError("tables must be [B, stride]")
-    for t, n, name in ((new_len, B, "new_len"), (have, B, "have"), (group_off, B + 1, "group_off"), (shared, B, "shared")):
-        _size(name, t, n)
+    dev = _where("kv_len", kv_len)
     with _On(dev, stream) as st:
-        def out(t, n, dtype, name):
-            if t is None:
-                t = torch.empty(n, dtype=dtype, device=dev)
-            _need(t, dtype, name)
-            _size(name, t, n)
-            return t
-
-        slots = out(slots, n_slots, torch.int64, "slots")
-        q_off = out(q_off, B + 1, torch.int64, "q_off")
-        taken = out(taken, 1, torch.int32, "taken")
-        _same_device(dev, tables=tables, new_len=new_len, have=have, free_blocks=free_blocks, group_off=group_off,
-                     shared=shared, slots=slots, q_off=q_off, taken=taken)
-        _check(lib().rk_block_tables(B, _ptr(kv_len), _ptr(new_len), _ptr(have), _ptr(group_off), _ptr(shared),
-                                     _ptr(free_blocks), free_blocks.numel(), _ptr(tables), tables.shape[1], _ptr(slots),
-                                     n_slots, _ptr(q_off), _ptr(taken), st), "rk_block_tables")
+        torch = _found_torch
+        i32, i64 = torch.int32, torch.int64
+        B, at = kv_len.numel(), kv_len.device
+        rows, stride = _table_shape(tables, B)
+        if slots is None:
+            slots = torch.empty(n_slots, dtype=i64, device=at)
+        if q_off is None:
+            q_off = torch.empty(B + 1, dtype=i64, device=at)
+        if taken is None:
+            taken = torch.empty(1, dtype=i32, device=at)
+        _check(lib().rk_block_tables(
+            B, _flat("kv_len", kv_len, i32, dev, B), _flat("new_len", new_len, i32, dev, B),
+            _flat("have", have, i32, dev, B), _flat("group_off", group_off, i64, dev, B + 1),
+            _flat("shared", shared, i32, dev, B), _flat("free_blocks", free_blocks, i32, dev, 0), free_blocks.numel(),
+            _flat("tables", tables, i32, dev, 0), stride, _flat("slots", slots, i64, dev, n_slots), n_slots,
+            _flat("q_off", q_off, i64, dev, B + 1), _flat("taken", taken, i32, dev, 1), st), "rk_block_tables")
     return tables, slots, q_off, taken
 
 
-def _rows(t, name, dtype=None):
-    """A [tokens, heads, D] tensor with its heads' elements side by side: its strides of tokens and heads."""
-    torch = _torch()
-    if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float16) or (dtype is not None and t.dtype != dtype):
-        raise RkError(f"{name} must be a CUDA tensor of {dtype or 'bfloat16 or float16'}")
-    if t.dim() != 3 or (t.numel() and t.stride(2) != 1):
-        raise RkError(f"{name} must be [tokens, heads, D] with a head's elements side by side")
-    n, heads, _ = t.shape
-    return t.stride(0) if n > 1 else 0, t.stride(1) if n and heads > 1 else 0       # of one, any stride will do
+def _table_shape(tables, B):
+    shape = tables.shape
+    if len(shape) != 2 or shape[0] < B:
+        raise RkError("tables must be [B, stride]")
+    return shape
 
 
-def _cache_strides(t, name, dtype, heads, D):
-    if not t.is_cuda or t.dtype != dtype:
-        raise RkError(f"{name} must be a CUDA tensor of {dtype}")
-    if t.dim() != 4 or t.shape[1:] != (RK_BLOCK_TOKENS, heads, D) or (t.numel() and t.stride(3) != 1):
-        raise RkError(f"{name} must be [blocks, {RK_BLOCK_TOKENS}, {heads}, {D}] with a head's elements side by side")
-    n = t.shape[0]
-    return CacheStrides(t.stride(0) if n > 1 else 0, t.stride(1) if n else D, t.stride(2) if n and heads > 1 else 0)
+def _rows(name, t, dev, dtype, shape):
+    """The strides of tokens and heads of a [tokens, heads, D] tensor with its heads' elements side by side."""
+    if t.get_device() != dev or t.dtype != dtype:
+        raise RkError(f"{name} must be a tensor of {dtype} on cuda:{dev}")
+    if t.shape != shape:
+        raise RkError(f"{name} must be {list(shape)}, it is {list(t.shape)}")
+    token, head, one = t.stride()
+    if one != 1 and t.numel():
+        raise RkError(f"{name} must have a head's elements side by side")
+    return token if shape[0] > 1 else 0, head if shape[0] and shape[1] > 1 else 0      # of one, any stride will do
+
+
+_strides_made = {}
+
+
+def _cache_strides(name, t, dev, dtype, shape):
+    if t.get_device() != dev or t.dtype != dtype:
+        raise RkError(f"{name} must be a tensor of {dtype} on cuda:{dev}")
+    if t.shape != shape:
+        raise RkError(f"{name} must be {list(shape)}, it is {list(t.shape)}")
+    block, token, head, one = t.stride()
+    if not t.numel():
+        block, token, head = 0, shape[3], 0
+    elif one != 1:
+        raise RkError(f"{name} must have a head's elements side by side")
+    return block if shape[0] > 1 else 0, token, head if shape[2] > 1 else 0
+
+
+def _as_strides(s):
+    """The three strides as the ABI's struct (made once for each, and never written)."""
+    got = _strides_made.get(s)
+    if got is None:
+        if len(_strides_made) > 256:
+            _strides_made.clear()
+        got = _strides_made[s] = CacheStrides(*s)
+    return got
+
+
+def _heads(name, t, dims):
+    """dtype and shape of a tensor of 16-bit floating values."""
+    if not _NARROW:
+        torch = _torch()
+        _NARROW.update({torch.bfloat16: RK_BF16, torch.float16: RK_F16})
+    if t.dtype not in _NARROW or t.dim() != dims:
+        raise RkError(f"{name} must be a CUDA tensor of bfloat16 or float16 with {dims} dimensions")
+    return t.dtype, t.shape
 
 
 def kv_write(k, v, k_cache, v_cache, slots, stream=None):
     """Keys and values [T, Hkv, D] of new tokens into the block cache [blocks, 16, Hkv, D] (rk_kv_write)."""
-    torch = _torch()
-    k_token, k_head = _rows(k, "k")
-    v_token, v_head = _rows(v, "v", k.dtype)
-    _need(slots, torch.int64, "slots")
-    T, Hkv, D = k.shape
-    if tuple(v.shape) != (T, Hkv, D):
-        raise RkError("k and v differ in shape")
-    _size("slots", slots, T)
-    ks = _cache_strides(k_cache, "k_cache", k.dtype, Hkv, D)
-    vs = _cache_strides(v_cache, "v_cache", k.dtype, Hkv, D)
-    if k_cache.shape[0] != v_cache.shape[0]:
-        raise RkError("k_cache and v_cache differ in blocks")
-    _same_device(k.device, v=v, k_cache=k_cache, v_cache=v_cache, slots=slots)
-    with _On(k.device, stream) as st:
-        _check(lib().rk_kv_write(T, Hkv, D, _ptr(k), k_token, k_head, _ptr(v), v_token, v_head, _ptr(k_cache), ks,
-                                 _ptr(v_cache), vs, k_cache.shape[0], _ptr(slots), st), "rk_kv_write")
+    dev = _where("k", k)
+    dtype, shape = _heads("k", k, 3)
+    T, Hkv, D = shape
+    k_token, k_head = _rows("k", k, dev, dtype, shape)
+    v_token, v_head = _rows("v", v, dev, dtype, shape)
+    if k_cache.dim() != 4:
+        raise RkError("k_cache must be [blocks, 16, heads, D]")
+    blocks = k_cache.shape[0]
+    cache = (blocks, RK_BLOCK_TOKENS, Hkv, D)
+    ks = _as_strides(_cache_strides("k_cache", k_cache, dev, dtype, cache))
+    vs = _as_strides(_cache_strides("v_cache", v_cache, dev, dtype, cache))
+    with _On(dev, stream) as st:
+        _check(lib().rk_kv_write(T, Hkv, D, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head,
+                                 k_cache.data_ptr(), ks, v_cache.data_ptr(), vs, blocks,
+                                 _flat("slots", slots, _found_torch.int64, dev, T), st), "rk_kv_write")
 
 
 def prefix_attention_workspace_size(T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
     return int(lib().rk_prefix_attention_workspace_size(T, B, Hq, Hkv, D))
+
+
+_attention_struct = struct.Struct("@7ifq" + "P2q" + "P3qP3q" + "5P" + "P2qP")
+assert _attention_struct.size == C.sizeof(Attention)
 
 
 def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None, shared=None, scale=None, out=None,
@@ -528,43 +580,40 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
     """Attention of new tokens q [T, Hq, D] over the block cache (rk_prefix_attention): (out, lse or None).
     scale defaults to D ** -0.5.  Rows behind the last request's stay as they were (in an `out` allocated here,
     uninitialised)."""
-    torch = _torch()
-    q_token, q_head = _rows(q, "q")
-    T, Hq, D = q.shape
+    dev = _where("q", q)
+    dtype, shape = _heads("q", q, 3)
+    T, Hq, D = shape
+    q_token, q_head = _rows("q", q, dev, dtype, shape)
     if k_cache.dim() != 4:
         raise RkError("k_cache must be [blocks, 16, heads, D]")
-    Hkv = k_cache.shape[2]
-    ks = _cache_strides(k_cache, "k_cache", q.dtype, Hkv, D)
-    vs = _cache_strides(v_cache, "v_cache", q.dtype, Hkv, D)
-    if k_cache.shape[0] != v_cache.shape[0]:
-        raise RkError("k_cache and v_cache differ in blocks")
-    for t, name in ((tables, "tables"), (kv_len, "kv_len"), (shared, "shared")):
-        _need(t, torch.int32, name)
-    _need(q_off, torch.int64, "q_off")
-    _need(group_off, torch.int64, "group_off")
-    B, dev = kv_len.numel(), q.device
-    if tables.dim() != 2 or tables.shape[0] < B:
-        raise RkError("tables must be [B, stride]")
-    for t, n, name in ((q_off, B + 1, "q_off"), (group_off, B + 1, "group_off"), (shared, B, "shared")):
-        _size(name, t, n)
+    blocks, _, Hkv, _ = k_cache.shape
+    cache = (blocks, RK_BLOCK_TOKENS, Hkv, D)
+    ks = _cache_strides("k_cache", k_cache, dev, dtype, cache)
+    vs = _cache_strides("v_cache", v_cache, dev, dtype, cache)
     with _On(dev, stream) as st:
+        torch = _found_torch
+        i32, i64 = torch.int32, torch.int64
+        B, at = kv_len.numel(), q.device
+        _, stride = _table_shape(tables, B)
         if out is None:
-            out = torch.empty((T, Hq, D), dtype=q.dtype, device=dev)
-        out_token, out_head = _rows(out, "out", q.dtype)
-        if tuple(out.shape) != (T, Hq, D):
-            raise RkError("out and q differ in shape")
+            out = torch.empty(shape, dtype=dtype, device=at)
+            out_token, out_head = Hq * D, D
+        else:
+            out_token, out_head = _rows("out", out, dev, dtype, shape)
         if lse is None and want_lse:
-            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
-        _need(lse, torch.float32, "lse")
-        _size("lse", lse, T * Hq)
+            lse = torch.empty((T, Hq), dtype=torch.float32, device=at)
         if workspace is None:
-            workspace = torch.empty(prefix_attention_workspace_size(T, B, Hq, Hkv, D), dtype=torch.uint8, device=dev)
-        _same_device(dev, k_cache=k_cache, v_cache=v_cache, tables=tables, kv_len=kv_len, q_off=q_off,
-                     group_off=group_off, shared=shared, out=out, lse=lse, workspace=workspace)
-        a = Attention(B, Hq, Hkv, D, RK_BF16 if q.dtype == torch.bfloat16 else RK_F16, k_cache.shape[0], tables.shape[1],
-                      D ** -0.5 if scale is None else scale, T, _ptr(q), q_token, q_head, _ptr(k_cache), ks,
-                      _ptr(v_cache), vs, _ptr(tables), _ptr(kv_len), _ptr(q_off), _ptr(group_off), _ptr(shared),
-                      _ptr(out), out_token, out_head, _ptr(lse))
-        _check(lib().rk_prefix_attention(C.byref(a), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                         st), "rk_prefix_attention")
+            ws_bytes = prefix_attention_workspace_size(T, B, Hq, Hkv, D)
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=at)
+        elif workspace.get_device() != dev or not workspace.is_contiguous():
+            raise RkError(f"workspace must be a contiguous tensor on cuda:{dev}")
+        else:
+            ws_bytes = workspace.numel() * workspace.element_size()
+        a = _attention_struct.pack(
+            B, Hq, Hkv, D, _NARROW[dtype], blocks, stride, D ** -0.5 if scale is None else scale, T, q.data_ptr(),
+            q_token, q_head, k_cache.data_ptr(), *ks, v_cache.data_ptr(), *vs, _flat("tables", tables, i32, dev, 0),
+            _flat("kv_len", kv_len, i32, dev, B), _flat("q_off", q_off, i64, dev, B + 1),
+            _flat("group_off", group_off, i64, dev, B + 1) or 0, _flat("shared", shared, i32, dev, B) or 0,
+            out.data_ptr(), out_token, out_head, _flat("lse", lse, torch.float32, dev, T * Hq) or 0)
+        _check(lib().rk_prefix_attention(a, workspace.data_ptr(), ws_bytes, st), "rk_prefix_attention")
     return out, lse
