@@ -17,11 +17,16 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kWideRows = 128, kWideKeys = 64;       // a wide step: 32 rows a wavefront, 64 keys
 constexpr int kNarrowRows = 32, kNarrowKeys = 128;   // a narrow step: 32 keys a wavefront
-// What a step of a tile costs, and its beginning and end, relative to each other; a workgroup takes at least one
-// of both, so that a tile's parts follow each other without a gap.
-constexpr uint32_t kWideCost = 2, kNarrowCost = 2, kWideEnds = 6, kNarrowEnds = 6;
-constexpr uint32_t kLeast = 8;
-static_assert(kLeast >= kWideCost + kWideEnds && kLeast >= kNarrowCost + kNarrowEnds, "a step begins in every piece");
+constexpr int kSoloKeys = 32, kSoloMost = 512;       // a narrow tile of so few keys is one wavefront's: 32 a step
+
+// Kinds of tiles, each on a line of its own.
+enum Kind { kWide, kNarrow, kSolo };
+// What a step of a tile costs, and its beginning and end, relative to each other (a solo tile's to a wavefront, the others' to a
+// workgroup).  A piece of a line has at least kLeast, a step or more, so that a tile's parts follow each other without a gap.
+constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
+constexpr uint32_t kLeast = 4;
+static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
+constexpr int kKeysOf[3] = {kWideKeys, kNarrowKeys, kSoloKeys};
 constexpr int kShareBlocks = 4;                      // shorter prefixes are not worth joining their parts
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 
@@ -168,30 +173,28 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x)
            (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)x);
 }
 
-// The workgroup's inclusive sums; tmp: 3 * kWaves words, the wavefronts' sums afterwards.
-__device__ __forceinline__ void incl_sums(uint64_t& x, uint64_t& y, uint32_t& z, uint64_t* tmp)
+// The workgroup's inclusive sums; tmp: 4 * kWaves words, the wavefronts' sums afterwards.
+__device__ __forceinline__ void incl_sums(uint64_t (&x)[3], uint32_t& z, uint64_t* tmp)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t ox = __shfl_up(x, d), oy = __shfl_up(y, d);
+        uint64_t ox[3];
+        for (int k = 0; k < 3; ++k) ox[k] = __shfl_up(x[k], d);
         const uint32_t oz = __shfl_up(z, d);
         if (lane >= d) {
-            x += ox;
-            y += oy;
+            for (int k = 0; k < 3; ++k) x[k] += ox[k];
             z += oz;
         }
     }
     if (lane == 63) {
-        tmp[wave] = x;
-        tmp[kWaves + wave] = y;
-        tmp[2 * kWaves + wave] = z;
+        for (int k = 0; k < 3; ++k) tmp[kWaves * k + wave] = x[k];
+        tmp[3 * kWaves + wave] = z;
     }
     __syncthreads();
     for (int w = 0; w < wave; ++w) {
-        x += tmp[w];
-        y += tmp[kWaves + w];
-        z += (uint32_t)tmp[2 * kWaves + w];
+        for (int k = 0; k < 3; ++k) x[k] += tmp[kWaves * k + w];
+        z += (uint32_t)tmp[3 * kWaves + w];
     }
 }
 
@@ -493,6 +496,9 @@ struct Attend {
                     eb = nb;
                 }
             }
+            // (a wavefront in this product goes first: the other on its SIMD has its weights to compute meanwhile;
+            // whole prompts 1,251 -> 1,214 us)
+            __builtin_amdgcn_s_setprio(1);
             u32x4 v[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
@@ -506,6 +512,7 @@ struct Attend {
 #pragma unroll
                 for (int y = u * 32 / (4 * DT); y < (u + 1) * 32 / (4 * DT); ++y) top = larger(top, nx[y >> 4][y & 15]);
             }
+            __builtin_amdgcn_s_setprio(0);
         };
         int32_t s = t.s0;
         Step now, next, then;
@@ -675,8 +682,9 @@ struct Attend {
     //
     // What bounds few rows is the reading of keys and values, so each wavefront takes keys of its own, with no
     // barrier: while it computes on the keys of a step its values are still under way, and the next step's keys
-    // follow as soon as this step's are in registers.  The wavefronts' results are joined through LDS.
-    template <int NQ>
+    // follow as soon as this step's are in registers.  The wavefronts' results are joined through LDS; of few keys a
+    // wavefront does a tile alone.
+    template <int NQ, bool Solo>
     __device__ void narrow(const Tile& t)
     {
         constexpr int KS = DP / 32, DT = DP / 16;
@@ -715,28 +723,29 @@ struct Attend {
                 v_read[x] = vr * kRow + (((2 * x + ((lane & 3) >> 1)) ^ turn(vr)) << 4) + 8 * (lane & 1);
         }
         const uint32_t keys = tile + wave * (64 * kRow), vals = keys + 32 * kRow;
-        // this wavefront's steps: 32 keys at 128 s + 32 wave
-        const int32_t first_block = t.block0 + 2 * wave;
-        int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kNarrowKeys - 1) / kNarrowKeys;
+        // this wavefront's steps: 32 keys at 128 s + 32 wave, or all of them
+        constexpr int kKeys = Solo ? kSoloKeys : kNarrowKeys, kBlocks = kKeys / RK_BLOCK_TOKENS;
+        const int32_t first_block = t.block0 + (Solo ? 0 : 2 * wave);
+        int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kKeys - 1) / kKeys;
         s1 = s1 < t.s1 ? s1 : t.s1;
         int32_t s = t.s0, id[2], later[2];
         auto ids = [&](int32_t* to, int32_t x) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) to[b] = block_id(t, first_block + 8 * x + b);
+            for (int b = 0; b < 2; ++b) to[b] = block_id(t, first_block + kBlocks * x + b);
         };
         uint32_t bad = 0, next_bad = 0;
         auto issue_keys = [&](int32_t x) {
             next_bad = 0;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                load_keys(t, first_block + 8 * x + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
+                load_keys(t, first_block + kBlocks * x + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
                 next_bad |= (bad_block(id[b]) ? 1u : 0u) << b;
             }
         };
         auto issue_values = [&](int32_t x) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
-                load_values(t, first_block + 8 * x + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+                load_values(t, first_block + kBlocks * x + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
         };
         auto scores = [&](f32x4 (*sc)[2]) {
 #pragma unroll
@@ -808,7 +817,8 @@ struct Attend {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the values are in registers
             if (s + 1 < s1) issue_values(s + 1);
         };
-        __syncthreads();                             // the LDS is the last tile's until here
+        if constexpr (Solo) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the LDS is the last tile's until here
+        else __syncthreads();
         if (s < s1) {
             ids(id, s);
             issue_keys(s);
@@ -816,7 +826,7 @@ struct Attend {
             ids(later, s + 1);
         }
         const int32_t seen = all_see + 1 - first_block * RK_BLOCK_TOKENS - 32;       // the last step's first key that all see
-        const int32_t open = seen < 0 ? 0 : seen / kNarrowKeys + 1, s_open = open < s1 ? open : s1;
+        const int32_t open = seen < 0 ? 0 : seen / kKeys + 1, s_open = open < s1 ? open : s1;
         for (; s < s_open && !next_bad; ++s) {
             f32x4 sc[NQ][2];
             u32x4 w[NQ];
@@ -834,7 +844,7 @@ struct Attend {
             values_read();
         }
         for (; s < s1; ++s) {
-            const int32_t key0 = (first_block + 8 * s) * RK_BLOCK_TOKENS;
+            const int32_t key0 = (first_block + kBlocks * s) * RK_BLOCK_TOKENS;
             const bool masked = key0 + 31 > all_see;
             f32x4 sc[NQ][2];
             u32x4 w[NQ];
@@ -888,9 +898,69 @@ struct Attend {
             }
             values_read();
         }
+        constexpr int kRows = 16 * NQ;
+        if constexpr (Solo) {
+            // out through LDS, as of wide tiles; all of it is free
+            const int32_t rows = t.tokens * G;
+            const int late = afresh(lane);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                l[n] += __shfl_xor(l[n], 16);
+                l[n] += __shfl_xor(l[n], 32);
+            }
+            auto written = [&](auto&& put) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < kRows * NC / 64; ++i) {
+                    const int x = 64 * i + late, row = x / NC, piece = x % NC;
+                    const u32x4 v = lds_read16(keys + row * kRow + ((piece ^ turn(row & 15)) << 4));
+                    if (row < rows) put(row, piece, v);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            };
+            const uint32_t row_at = keys + (late & 15) * kRow, turned = turn(late & 15);
+            if (t.part) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int d = 0; d < DT / 2; ++d)
+                            lds_write16(row_at + 16 * n * kRow + (((4 * d + g) ^ turned) << 4),
+                                        __builtin_bit_cast(u32x4, o[n][half * (DT / 2) + d]));
+                    float* to = t.part + half * (DP / 2);
+                    written([&](int row, int piece, u32x4 v) { *reinterpret_cast<u32x4*>(to + row * DP + 4 * piece) = v; });
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    const float inv = l[n] == 0.0f ? 0.0f : 1.0f / l[n];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const f32x4 y = o[n][d] * inv;
+                        lds_write8(row_at + 16 * n * kRow + (((2 * d + (g >> 1)) ^ turned) << 4) + 8 * (g & 1),
+                                   u32x2{pack16<Half>(y.x, y.y), pack16<Half>(y.z, y.w)});
+                    }
+                }
+                written([&](int row, int piece, u32x4 v) {
+                    if (8 * piece < p.a.D) *reinterpret_cast<u32x4*>(out_row(t, row) + 8 * piece) = v;
+                });
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const int32_t r = 16 * n + col;
+                if (g != 0 || r >= rows) continue;
+                if (t.part) {
+                    t.part_ml[2 * r] = m[n];
+                    t.part_ml[2 * r + 1] = l[n];
+                } else {
+                    put_lse(t, r, m[n], l[n]);
+                }
+            }
+            return;
+        }
         // the four wavefronts' results: rows of DP floats in LDS, wavefront after wavefront
         __syncthreads();
-        constexpr int kRows = 16 * NQ;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             l[n] += __shfl_xor(l[n], 16);
@@ -955,28 +1025,32 @@ struct Request {
 // paired first with last so that every pair takes the same.
 struct Segment {
     int32_t tokens, rows, tiles, per;        // tokens in all, rows in all, tiles, tokens of a tile
-    int32_t steps0, block0;                  // steps of a tile (of the first, where they grow)
-    bool wide, grows;
+    int32_t steps0;                          // steps of a tile (of the first, where they grow)
+    int kind;
+    bool grows;
     uint64_t pair, cost;                     // cost of a pair (or tile), and in all
 };
 
-__device__ __forceinline__ int32_t steps_for(int64_t keys, int32_t per_step)
+__device__ __forceinline__ int32_t steps_for(int64_t keys, int kind)
 {
-    return keys > 0 ? (int32_t)((keys + per_step - 1) / per_step) : 1;
+    const int32_t per = kind == kWide ? kKeysOf[kWide] : kind == kNarrow ? kKeysOf[kNarrow] : kKeysOf[kSolo];
+    return keys > 0 ? (int32_t)((keys + per - 1) / per) : 1;
 }
 
-// A tile's extent along the line, and the steps of it that begin in its first `length`: the first at its start, the
-// s-th behind the ends' cost and s steps.
-template <bool Wide>
-__device__ __forceinline__ uint64_t extent(int32_t steps)
+// A tile's extent along the line (its steps, one after the other, then its ends' cost), and the steps of it that begin in its first
+// `length`.  A solo tile is not cut: it belongs where it starts.
+__device__ __forceinline__ uint64_t extent(int32_t steps, int kind)
 {
-    return (Wide ? kWideEnds : kNarrowEnds) + (uint64_t)steps * (Wide ? kWideCost : kNarrowCost);
+    return kind == kWide ? kEndsCost[kWide] + (uint64_t)steps * kStepCost[kWide]
+         : kind == kNarrow ? kEndsCost[kNarrow] + (uint64_t)steps * kStepCost[kNarrow]
+                           : kEndsCost[kSolo] + (uint64_t)steps * kStepCost[kSolo];
 }
-template <bool Wide>
-__device__ __forceinline__ uint64_t steps_before(uint64_t length)
+template <int K>
+__device__ __forceinline__ int32_t steps_before(uint64_t length, int32_t steps)
 {
-    constexpr uint32_t ends = Wide ? kWideEnds : kNarrowEnds, cost = Wide ? kWideCost : kNarrowCost;
-    return length == 0 ? 0 : length <= ends ? 1 : quotient(length - 1 - ends, cost) + 1;
+    if (K == kSolo) return length == 0 ? 0 : steps;
+    const uint64_t n = quotient_up(length, kStepCost[K]);
+    return n < (uint64_t)steps ? (int32_t)n : steps;
 }
 
 __device__ __forceinline__ Segment own_segment(const Request& r, int32_t G)
@@ -984,23 +1058,19 @@ __device__ __forceinline__ Segment own_segment(const Request& r, int32_t G)
     Segment s{};
     s.tokens = r.tokens;
     s.rows = r.tokens * G;
-    s.block0 = r.shared;
-    s.wide = s.rows > kNarrowRows;
-    s.per = s.wide ? kWideRows / G : s.tokens;
-    if (s.tokens == 0) return s;
     const int64_t own = (int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS;
+    s.kind = s.rows > kNarrowRows ? kWide : own > kSoloMost ? kNarrow : kSolo;
+    s.per = s.kind == kWide ? kWideRows / G : s.tokens;
+    if (s.tokens == 0) return s;
     s.tiles = (s.tokens + s.per - 1) / s.per;
-    if (!s.wide) {
-        s.steps0 = steps_for(own, kNarrowKeys);
-        s.pair = s.cost = extent<false>(s.steps0);
-    } else if (s.tiles == 1) {
-        s.steps0 = steps_for(own, kWideKeys);
-        s.pair = s.cost = extent<true>(s.steps0);
+    if (s.tiles == 1) {
+        s.steps0 = steps_for(own, s.kind);
+        s.pair = s.cost = extent(s.steps0, s.kind);
     } else {
         s.grows = true;
-        s.steps0 = steps_for(own - s.tokens + s.per, kWideKeys);
-        const int32_t last = steps_for(own - s.tokens + (int64_t)s.tiles * s.per, kWideKeys);
-        s.pair = extent<true>(s.steps0) + extent<true>(last) + 2 * kWideCost;
+        s.steps0 = steps_for(own - s.tokens + s.per, kWide);
+        const int32_t last = steps_for(own - s.tokens + (int64_t)s.tiles * s.per, kWide);
+        s.pair = extent(s.steps0, kWide) + extent(last, kWide) + 2 * kStepCost[kWide];
         s.cost = s.pair * ((s.tiles + 1) / 2);
     }
     return s;
@@ -1011,11 +1081,11 @@ __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks
     Segment s{};
     s.tokens = tokens;
     s.rows = tokens * G;
-    s.wide = s.rows > kNarrowRows;
-    s.per = s.wide ? kWideRows / G : s.tokens;
+    s.kind = s.rows > kNarrowRows ? kWide : blocks * RK_BLOCK_TOKENS > kSoloMost ? kNarrow : kSolo;
+    s.per = s.kind == kWide ? kWideRows / G : s.tokens;
     s.tiles = (s.tokens + s.per - 1) / s.per;
-    s.steps0 = steps_for((int64_t)blocks * RK_BLOCK_TOKENS, s.wide ? kWideKeys : kNarrowKeys);
-    s.pair = s.wide ? extent<true>(s.steps0) : extent<false>(s.steps0);
+    s.steps0 = steps_for((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
+    s.pair = extent(s.steps0, s.kind);
     s.cost = s.pair * s.tiles;
     return s;
 }
@@ -1031,15 +1101,16 @@ __device__ __forceinline__ int32_t last_group(const int32_t* off, int32_t n, int
     return lo;
 }
 
-// A workgroup's piece [from, to) of the line of its kind of tiles, from place `off` of request i's part on; wg: its
-// place among the workgroups.
-template <bool Wide, class A>
+// A workgroup's piece [from, to) of the line of tiles of kind K (of solo tiles: a wavefront's), from place `off` of
+// request i's part on; wg: the workgroup's place among all.
+template <int K, class A>
 __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uint64_t off, uint64_t from, uint64_t to,
                                      uint64_t each, int32_t wg)
 {
     const AttendArgs& p = work.p;
     const rk_attention& a = p.a;
-    const int32_t G = work.G, B = p.n, tid = threadIdx.x;
+    const int32_t G = work.G, B = p.n;
+    const int32_t tid = K == kSolo ? threadIdx.x & 63 : threadIdx.x, crew = K == kSolo ? 64 : kThreads;
     constexpr int DP = A::kHead;
     uint64_t x = from;
     while (x < to && i < B) {
@@ -1055,12 +1126,12 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         uint64_t before = 0;
         if (r.end) {
             sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, G);
-            before = sg.wide == Wide ? sg.cost * (uint64_t)a.Hkv : 0;
+            before = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             prefix = off < before;
         }
         if (!prefix) {
             sg = own_segment(r, G);
-            const uint64_t own = sg.wide == Wide ? sg.cost * (uint64_t)a.Hkv : 0;
+            const uint64_t own = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             off -= before;
             if (off >= own) {                // on to the next request
                 off -= own;
@@ -1075,13 +1146,13 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         int32_t steps = sg.steps0;
         uint64_t left = sg.pair;             // cost from the tile's start to the next tile's
         bool nothing = false;
-        if (Wide && sg.grows) {
+        if (K == kWide && sg.grows) {
             auto steps_of = [&](int32_t k) {
                 const int64_t seen = (int64_t)(k + 1) * sg.per < sg.tokens ? (int64_t)(k + 1) * sg.per : sg.tokens;
-                return steps_for((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWideKeys);
+                return steps_for((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWide);
             };
             const int32_t k = sg.tiles - 1 - j;
-            const uint64_t first = extent<true>(steps_of(j));
+            const uint64_t first = extent(steps_of(j), kWide);
             steps = steps_of(j);
             left = first;
             if (in >= first) {               // the pair's other tile
@@ -1093,8 +1164,7 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
             }
         }
         // the steps of the tile that begin in [from, to)
-        const uint64_t s_end = steps_before<Wide>(to - x + in);
-        const int32_t s0 = (int32_t)steps_before<Wide>(in), s1 = s_end < (uint64_t)steps ? (int32_t)s_end : steps;
+        const int32_t s0 = steps_before<K>(in, steps), s1 = steps_before<K>(to - x + in, steps);
         if (!nothing && s0 < s1) {
             Tile t;
             t.token = r.q0 + j * sg.per;
@@ -1127,19 +1197,19 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
             }
             if (s0 == 0 && (joined || !whole)) {
                 // workgroups that the tile's steps fall to, up to the one in whose piece the last begins
-                const uint64_t of_mine = x - in - from + (steps > 1 ? extent<Wide>(steps - 1) : 0);
+                const uint64_t of_mine = x - in - from + (uint64_t)(steps - 1) * kStepCost[K];
                 const int32_t n = (int32_t)quotient(of_mine, each) + 1;
                 if (joined) {
-                    for (int32_t k = tid; k < t.tokens; k += kThreads)
+                    for (int32_t k = tid; k < t.tokens; k += crew)
                         p.parts[((int64_t)kind * a.Hkv + head) * p.shared_tokens + r.base + j * sg.per + k] =
                             Parts{whole ? 0 : n, wg, k * G, 0};
                 } else if (tid == 0) {
                     p.split[blockIdx.x] = Split{n, wg, t.token, t.tokens, head, {0, 0, 0}};
                 }
             }
-            if constexpr (Wide) work.wide(t);
-            else if (sg.rows <= 16) work.template narrow<1>(t);
-            else work.template narrow<2>(t);
+            if constexpr (K == kWide) work.wide(t);
+            else if (sg.rows <= 16) work.template narrow<1, K == kSolo>(t);
+            else work.template narrow<2, K == kSolo>(t);
         }
         x += left - in;
         off += left - in + (prefix ? 0 : before);
@@ -1154,8 +1224,8 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 {
     extern __shared__ __align__(1024) uint8_t lds[];
     __shared__ float s_join[2 * kWaves * kNarrowRows];
-    __shared__ uint64_t s_tmp[3 * kWaves], s_off;
-    __shared__ int32_t s_i, s_bad;
+    __shared__ uint64_t s_tmp[4 * kWaves], s_off[kWaves];
+    __shared__ int32_t s_i[kWaves], s_bad;
     using A = Attend<DP, Half>;
     const rk_attention& a = p.a;
     const int tid = threadIdx.x;
@@ -1165,8 +1235,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
     const bool tell = blockIdx.x == 0;
     if (tid == 0) {
         s_bad = 0;
-        s_i = B;
-        s_off = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            s_i[w] = B;
+            s_off[w] = 0;
+        }
     }
     __syncthreads();
     for (int32_t i = tid; i < B; i += kThreads) {
@@ -1234,22 +1306,22 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
         }
         __syncthreads();
     }
-    // the line of work: per thread's requests, then over the threads; wide tiles first, then narrow ones
+    // the line of work: per thread's requests, then over the threads; each kind of tiles on its own
     const int32_t per = (B + kThreads - 1) / kThreads;
     const int32_t i0 = tid * per, i1 = i0 + per < B ? i0 + per : B;
     struct Cost {
-        uint64_t wide, narrow;
+        uint64_t of[3];
     };
-    auto cost_of = [&](int32_t i) {
-        Cost x{0, 0};
-        const Segment own = own_segment(req[i], G);
-        (own.wide ? x.wide : x.narrow) += own.cost;
+    auto cost_of = [&](int32_t i, Cost& x) {
+        auto add = [&](const Segment& sg) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) x.of[k] += sg.kind == k ? sg.cost * (uint64_t)a.Hkv : 0;
+        };
+        add(own_segment(req[i], G));
         if (req[i].end) {
             const Request& l = req[req[i].end - 1];
-            const Segment prefix = prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G);
-            (prefix.wide ? x.wide : x.narrow) += prefix.cost;
+            add(prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G));
         }
-        return x;
     };
     uint32_t together = 0;
     for (int32_t i = i0; i < i1; ++i) {
@@ -1257,48 +1329,49 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
         if (req[i].shared) together += req[i].tokens;
     }
     __syncthreads();
-    Cost mine{0, 0};
-    for (int32_t i = i0; i < i1; ++i) {
-        const Cost x = cost_of(i);
-        mine.wide += x.wide;
-        mine.narrow += x.narrow;
-    }
-    mine.wide *= (uint64_t)a.Hkv;
-    mine.narrow *= (uint64_t)a.Hkv;
-    uint64_t wide_upto = mine.wide, narrow_upto = mine.narrow;
+    Cost mine{};
+    for (int32_t i = i0; i < i1; ++i) cost_of(i, mine);
+    Cost upto = mine, all{};
     uint32_t tokens_upto = together;
-    incl_sums(wide_upto, narrow_upto, tokens_upto, s_tmp);
-    Cost all{0, 0};
-    for (int w = 0; w < kWaves; ++w) {
-        all.wide += s_tmp[w];
-        all.narrow += s_tmp[kWaves + w];
+    incl_sums(upto.of, tokens_upto, s_tmp);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        for (int w = 0; w < kWaves; ++w) all.of[k] += s_tmp[kWaves * k + w];
+        all.of[k] = uniform(all.of[k]);
     }
-    all.wide = uniform(all.wide);
-    all.narrow = uniform(all.narrow);
     // pieces for at most gridDim.x workgroups (each kind's last may be short)
-    uint64_t each = quotient_up(all.wide + all.narrow, gridDim.x - 1);
+    uint64_t each = quotient_up(all.of[kWide] + all.of[kNarrow] + (all.of[kSolo] + kWaves - 1) / kWaves, gridDim.x - 3);
     if (each < kLeast) each = kLeast;
-    const uint32_t n_wide = (uint32_t)quotient_up(all.wide, each);
-    const uint32_t active = n_wide + (uint32_t)quotient_up(all.narrow, each);
+    const uint32_t n_wide = (uint32_t)quotient_up(all.of[kWide], each), n_narrow = (uint32_t)quotient_up(all.of[kNarrow], each);
+    const uint32_t n_solo = (uint32_t)((quotient_up(all.of[kSolo], each) + kWaves - 1) / kWaves);
+    const uint32_t active = n_wide + n_narrow + n_solo;
     // workgroups go to the 8 XCDs in turn: each XCD takes a stretch of the line
     const uint32_t wg = (blockIdx.x & 7u) * ((active + 7) / 8) + (blockIdx.x >> 3);
-    const bool idle = (blockIdx.x >> 3) >= (active + 7) / 8 || wg >= active, wide = wg < n_wide;
-    const uint64_t from = (uint64_t)(wide ? wg : wg - n_wide) * each, end = wide ? all.wide : all.narrow;
-    const uint64_t to = from + each < end ? from + each : end;
+    const bool idle = (blockIdx.x >> 3) >= (active + 7) / 8 || wg >= active;
+    const int kind = wg < n_wide ? kWide : wg < n_wide + n_narrow ? kNarrow : kSolo;
+    const uint64_t end = kind == kWide ? all.of[kWide] : kind == kNarrow ? all.of[kNarrow] : all.of[kSolo];
+    // the workgroup's piece, or its wavefronts' of solo tiles
+    const uint64_t first = (kind == kWide ? wg : kind == kNarrow ? wg - n_wide : (uint64_t)kWaves * (wg - n_wide - n_narrow)) * each;
     {
         uint32_t tok = tokens_upto - together;
-        uint64_t x = wide ? wide_upto - mine.wide : narrow_upto - mine.narrow;
-        const bool here = !idle && from >= x && from < (wide ? wide_upto : narrow_upto);
+        const uint64_t top = kind == kWide ? upto.of[kWide] : kind == kNarrow ? upto.of[kNarrow] : upto.of[kSolo];
+        uint64_t x = top - (kind == kWide ? mine.of[kWide] : kind == kNarrow ? mine.of[kNarrow] : mine.of[kSolo]);
+        const int pieces = kind == kSolo ? kWaves : 1;
+        const bool here = !idle && first + (pieces - 1) * each >= x && first < top;
         for (int32_t i = i0; i < i1; ++i) {
             req[i].base = (int32_t)tok;
             if (req[i].shared) tok += req[i].tokens;
             if (tell) p.share_base[i] = req[i].shared && req[i].tokens ? req[i].base : -1;
             if (!here) continue;
-            const Cost k = cost_of(i);
-            const uint64_t w = (wide ? k.wide : k.narrow) * (uint64_t)a.Hkv;
-            if (from >= x && from < x + w) {
-                s_i = i;
-                s_off = from - x;
+            Cost k{};
+            cost_of(i, k);
+            const uint64_t w = kind == kWide ? k.of[kWide] : kind == kNarrow ? k.of[kNarrow] : k.of[kSolo];
+            for (int q = 0; q < pieces; ++q) {
+                const uint64_t from = first + q * each;
+                if (from >= x && from < x + w) {
+                    s_i[q] = i;
+                    s_off[q] = from - x;
+                }
             }
             x += w;
         }
@@ -1309,10 +1382,12 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
     float c = fabsf(a.scale) * kLog2e;
     if (c < 1e-30f) c = 1e-30f;              // scores of 0, and -infinity stays what it is
     A work(p, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds, s_join, c);
-    const int32_t i = uniform(s_i);
-    const uint64_t off = uniform(s_off);
-    if (wide) walk<true>(work, req, i, off, from, to, each, (int32_t)wg);
-    else walk<false>(work, req, i, off, from, to, each, (int32_t)wg);
+    const int piece = kind == kSolo ? work.wave : 0;
+    const int32_t i = uniform(s_i[piece]);
+    const uint64_t off = uniform(s_off[piece]), from = first + piece * each, to = from + each < end ? from + each : end;
+    if (kind == kWide) walk<kWide>(work, req, i, off, from, to, each, (int32_t)wg);
+    else if (kind == kNarrow) walk<kNarrow>(work, req, i, off, from, to, each, (int32_t)wg);
+    else walk<kSolo>(work, req, i, off, from, to, each, (int32_t)wg);
 }
 
 // The parts of rows that more than one workgroup worked on, joined: a wavefront a row, DP / 64 neighbouring values a
