@@ -40,17 +40,31 @@ struct __align__(16) Parts {
     int32_t n, wg, row, pad;                 // n = 0: one part, in the shared rows' own place
 };
 
+// A request whose group attends to its prefix together: its first token, tokens (0: there is no such thing) and
+// those of such requests before it.
+struct __align__(16) Shared {
+    int32_t q0, tokens, base, pad;
+};
+
 struct AttendArgs {
     rk_attention a;
     int32_t* status;
     int32_t b0, n;                           // the launch's requests: n from b0 on
+    int32_t solo_most;                       // most keys of a solo tile
     Split* split;                            // [grid]
-    int32_t* share_base;                     // [n]: first shared token of a request, -1: it shares nothing
+    Shared* shared;                          // [n]: the requests' tokens that share a prefix
     Parts* parts;                            // [2][Hkv][shared tokens]
-    float *part, *part_ml;                   // [2 grid][kWideRows][DP], [..][2]: first and last tile of a workgroup
-    float *whole, *whole_ml;                 // [2][Hkv][shared rows][DP], [..][2]
-    int32_t shared_rows, shared_tokens;      // what whole and parts hold, of a head
+    // Rows of [DP] values, and their [2] statistics: first [2 grid][kWideRows], the first and last tile of each workgroup,
+    // then [2][Hkv][shared rows], the whole tiles of rows that share a prefix.
+    float *part, *part_ml;
+    int32_t shared_rows, shared_tokens;      // of a head
 };
+
+// The first row of the whole tiles of a kind (prefixes: 0, requests' own keys: 1) and key head.
+__device__ __forceinline__ int64_t whole_row(const AttendArgs& p, uint32_t grid, int kind, int32_t head)
+{
+    return 2 * (int64_t)grid * kWideRows + ((int64_t)kind * p.a.Hkv + head) * p.shared_rows;
+}
 
 template <bool Half>
 __device__ __forceinline__ uint32_t pack16(float x, float y)
@@ -1053,13 +1067,13 @@ __device__ __forceinline__ int32_t steps_before(uint64_t length, int32_t steps)
     return n < (uint64_t)steps ? (int32_t)n : steps;
 }
 
-__device__ __forceinline__ Segment own_segment(const Request& r, int32_t G)
+__device__ __forceinline__ Segment own_segment(const Request& r, int32_t G, int32_t solo_most)
 {
     Segment s{};
     s.tokens = r.tokens;
     s.rows = r.tokens * G;
     const int64_t own = (int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS;
-    s.kind = s.rows > kNarrowRows ? kWide : own > kSoloMost ? kNarrow : kSolo;
+    s.kind = s.rows > kNarrowRows ? kWide : own > solo_most ? kNarrow : kSolo;
     s.per = s.kind == kWide ? kWideRows / G : s.tokens;
     if (s.tokens == 0) return s;
     s.tiles = (s.tokens + s.per - 1) / s.per;
@@ -1076,12 +1090,12 @@ __device__ __forceinline__ Segment own_segment(const Request& r, int32_t G)
     return s;
 }
 
-__device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks, int32_t G)
+__device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks, int32_t G, int32_t solo_most)
 {
     Segment s{};
     s.tokens = tokens;
     s.rows = tokens * G;
-    s.kind = s.rows > kNarrowRows ? kWide : blocks * RK_BLOCK_TOKENS > kSoloMost ? kNarrow : kSolo;
+    s.kind = s.rows > kNarrowRows ? kWide : blocks * RK_BLOCK_TOKENS > solo_most ? kNarrow : kSolo;
     s.per = s.kind == kWide ? kWideRows / G : s.tokens;
     s.tiles = (s.tokens + s.per - 1) / s.per;
     s.steps0 = steps_for((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
@@ -1125,12 +1139,12 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         bool prefix = false;
         uint64_t before = 0;
         if (r.end) {
-            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, G);
+            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, G, p.solo_most);
             before = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             prefix = off < before;
         }
         if (!prefix) {
-            sg = own_segment(r, G);
+            sg = own_segment(r, G, p.solo_most);
             const uint64_t own = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             off -= before;
             if (off >= own) {                // on to the next request
@@ -1191,9 +1205,9 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
                 t.part = p.part + slot * kWideRows * DP;
                 t.part_ml = p.part_ml + slot * kWideRows * 2;
             } else if (joined) {
-                const int64_t row = ((int64_t)kind * a.Hkv + head) * p.shared_rows + (int64_t)(r.base + j * sg.per) * G;
-                t.part = p.whole + row * DP;
-                t.part_ml = p.whole_ml + row * 2;
+                const int64_t row = whole_row(p, gridDim.x, kind, head) + (int64_t)(r.base + j * sg.per) * G;
+                t.part = p.part + row * DP;
+                t.part_ml = p.part_ml + row * 2;
             }
             if (s0 == 0 && (joined || !whole)) {
                 // workgroups that the tile's steps fall to, up to the one in whose piece the last begins
@@ -1317,10 +1331,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 #pragma unroll
             for (int k = 0; k < 3; ++k) x.of[k] += sg.kind == k ? sg.cost * (uint64_t)a.Hkv : 0;
         };
-        add(own_segment(req[i], G));
+        add(own_segment(req[i], G, p.solo_most));
         if (req[i].end) {
             const Request& l = req[req[i].end - 1];
-            add(prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G));
+            add(prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G, p.solo_most));
         }
     };
     uint32_t together = 0;
@@ -1361,7 +1375,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
         for (int32_t i = i0; i < i1; ++i) {
             req[i].base = (int32_t)tok;
             if (req[i].shared) tok += req[i].tokens;
-            if (tell) p.share_base[i] = req[i].shared && req[i].tokens ? req[i].base : -1;
+            if (tell) p.shared[i] = Shared{req[i].q0, req[i].shared ? req[i].tokens : 0, req[i].base, 0};
             if (!here) continue;
             Cost k{};
             cost_of(i, k);
@@ -1391,7 +1405,8 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 }
 
 // The parts of rows that more than one workgroup worked on, joined: a wavefront a row, DP / 64 neighbouring values a
-// lane.  The parts' weights come first, a lane each; then their values, several loads under way at a time.
+// lane.  The parts' weights come first, a lane each; then their values, several loads under way at a time.  Waiting for
+// loads is all that bounds it, but of the rows of whole prompts' 500 cut tiles (33 us for 100 MB).
 template <int DP, bool Half>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks, int32_t shared_chunks)
 {
@@ -1399,103 +1414,87 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t gr
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int32_t G = a.Hq / a.Hkv;
     constexpr int N = DP / 64;
-    struct Sum {
-        float o[N], m, l;
-    };
-    // n parts of a row: the first the last that workgroup wg began, the others the first of the workgroups
-    // after it; rows of kWideRows a place
-    auto add = [&](Sum& s, int32_t n, const float* part, const float* ml, int64_t first, int64_t next) {
+    // n parts at the rows row_of(k), to the output's row of the token and query head
+    auto join = [&](int32_t n, auto&& row_of, int64_t token, int32_t h) {
+        float o[N] = {}, m = -INFINITY, l = 0.0f;
         for (int32_t k0 = 0; k0 < n; k0 += 64) {
             const int32_t k = k0 + lane;
             float pm = -INFINITY, pl = 0.0f;
             if (k < n) {
-                const int64_t row = k == 0 ? first : next + (int64_t)(k - 1) * (2 * kWideRows);
-                pm = ml[2 * row];
-                pl = ml[2 * row + 1];
+                const int64_t row = row_of(k);
+                pm = p.part_ml[2 * row];
+                pl = p.part_ml[2 * row + 1];
             }
             float top = pm;
 #pragma unroll
             for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-            const float nm = fmaxf(s.m, top);
+            const float nm = fmaxf(m, top);
             if (nm == -INFINITY) continue;
-            const float old = __builtin_amdgcn_exp2f(s.m - nm), w = __builtin_amdgcn_exp2f(pm - nm);
+            const float old = __builtin_amdgcn_exp2f(m - nm), w = __builtin_amdgcn_exp2f(pm - nm);
             float sum = w * pl;
 #pragma unroll
             for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-            s.l = s.l * old + sum;
-            s.m = nm;
+            l = l * old + sum;
+            m = nm;
 #pragma unroll
-            for (int x = 0; x < N; ++x) s.o[x] = old == 0.0f ? 0.0f : s.o[x] * old;
+            for (int x = 0; x < N; ++x) o[x] = old == 0.0f ? 0.0f : o[x] * old;
             const int32_t here = n - k0 < 64 ? n - k0 : 64;
             constexpr int kAtOnce = 8;
             for (int32_t q = 0; q < here; q += kAtOnce) {
                 float v[kAtOnce][N];
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) {
-                    const int32_t at = k0 + (q + u < here ? q + u : here - 1);
-                    const int64_t row = at == 0 ? first : next + (int64_t)(at - 1) * (2 * kWideRows);
+                    const int64_t row = row_of(k0 + (q + u < here ? q + u : here - 1));
 #pragma unroll
-                    for (int x = 0; x < N; ++x) v[u][x] = part[row * DP + N * lane + x];
+                    for (int x = 0; x < N; ++x) v[u][x] = p.part[row * DP + N * lane + x];
                 }
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) {
                     const float f = q + u < here ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), q + u)) : 0.0f;
-                    if (f != 0.0f)
+                    if (f != 0.0f)           // (a weight of 0 takes nothing of a part, whatever that holds)
 #pragma unroll
-                        for (int x = 0; x < N; ++x) s.o[x] += f * v[u][x];
+                        for (int x = 0; x < N; ++x) o[x] += f * v[u][x];
                 }
             }
         }
-    };
-    auto put = [&](const Sum& s, int64_t token, int32_t h) {
-        const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         uint16_t* to = (uint16_t*)a.out + token * a.out_token + h * a.out_head + N * lane;
-        if (N * lane < a.D) {
-            if constexpr (N % 2 == 0) {
 #pragma unroll
-                for (int x = 0; x < N; x += 2)
-                    if (N * lane + x < a.D) *reinterpret_cast<uint32_t*>(to + x) = pack16<Half>(s.o[x] * inv, s.o[x + 1] * inv);
-            } else {
-#pragma unroll
-                for (int x = 0; x < N; ++x)
-                    if (N * lane + x < a.D) to[x] = (uint16_t)pack16<Half>(s.o[x] * inv, 0.0f);
-            }
+        for (int x = 0; x < N; x += N % 2 ? 1 : 2) {
+            if (N * lane + x >= a.D) break;
+            if constexpr (N % 2 == 0) *reinterpret_cast<uint32_t*>(to + x) = pack16<Half>(o[x] * inv, o[x + 1] * inv);
+            else to[x] = (uint16_t)pack16<Half>(o[x] * inv, 0.0f);
         }
-        if (lane == 0 && a.lse) a.lse[token * a.Hq + h] = s.l == 0.0f ? -INFINITY : (s.m + __builtin_log2f(s.l)) * kLn2;
+        if (lane == 0 && a.lse) a.lse[token * a.Hq + h] = l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
     };
-    auto tail = [&](int32_t wg, int32_t r) { return (2 * (int64_t)wg + 1) * kWideRows + r; };
-    auto heads = [&](int32_t wg, int32_t r) { return 2 * (int64_t)(wg + 1) * kWideRows + r; };
-    if ((int32_t)blockIdx.x < grid * chunks) {
-        const Split t = p.split[blockIdx.x / chunks];
+    // the k-th part of a cut tile's row r that workgroup wg began: its last, then the first of those after it
+    auto cut = [&](int32_t wg, int32_t r, int32_t k) { return (2 * (int64_t)(wg + k) + (k == 0 ? 1 : 0)) * kWideRows + r; };
+    const int32_t of_shared = a.group_off ? p.n * a.Hkv * shared_chunks : 0;
+    if ((int32_t)blockIdx.x >= of_shared) {
+        const int32_t b = (int32_t)blockIdx.x - of_shared;
+        const Split t = p.split[b / chunks];
         const int32_t rows = t.tokens * G;
         if (t.n == 0) return;
-        for (int32_t r = (int32_t)(blockIdx.x % chunks) * kWaves + wave; r < rows; r += chunks * kWaves) {
-            Sum s{{}, -INFINITY, 0.0f};
-            add(s, t.n, p.part, p.part_ml, tail(t.wg, r), heads(t.wg, r));
-            put(s, t.token + (int64_t)(r / G), t.head * G + r % G);
-        }
+        for (int32_t r = b % chunks * kWaves + wave; r < rows; r += chunks * kWaves)
+            join(t.n, [&](int32_t k) { return cut(t.wg, r, k); }, t.token + (int64_t)(r / G), t.head * G + r % G);
         return;
     }
-    // a request whose group attends to its prefix together
-    const int32_t b = (int32_t)blockIdx.x - grid * chunks, u = b / shared_chunks, i = u / a.Hkv, head = u % a.Hkv;
-    const int32_t base = p.share_base[i];
-    const int64_t q0 = a.q_off[p.b0 + i], q1 = a.q_off[p.b0 + i + 1];
-    if (base < 0) return;
-    const int32_t rows = (int32_t)(q1 - q0) * G;
-    for (int32_t r = (b % shared_chunks) * kWaves + wave; r < rows; r += shared_chunks * kWaves) {
+    const int32_t u = (int32_t)blockIdx.x / shared_chunks, head = u % a.Hkv;
+    const Shared t = p.shared[u / a.Hkv];
+    const int32_t rows = t.tokens * G;
+    for (int32_t r = (int32_t)blockIdx.x % shared_chunks * kWaves + wave; r < rows; r += shared_chunks * kWaves) {
         const int32_t tok = r / G, h = r % G;
-        Parts t[2];
+        Parts x[2];
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
-            t[kind] = p.parts[((int64_t)kind * a.Hkv + head) * p.shared_tokens + base + tok];
-        Sum s{{}, -INFINITY, 0.0f};
-#pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-            const int32_t n = uniform(t[kind].n), wg = uniform(t[kind].wg), row = uniform(t[kind].row) + h;
-            if (n == 0) add(s, 1, p.whole, p.whole_ml, ((int64_t)kind * a.Hkv + head) * p.shared_rows + (int64_t)base * G + r, 0);
-            else add(s, n, p.part, p.part_ml, tail(wg, row), heads(wg, row));
-        }
-        put(s, q0 + tok, head * G + h);
+            x[kind] = p.parts[((int64_t)kind * a.Hkv + head) * p.shared_tokens + t.base + tok];
+        const int32_t n0 = uniform(x[0].n), n1 = uniform(x[1].n), first = n0 > 0 ? n0 : 1;
+        const int32_t wg0 = uniform(x[0].wg), wg1 = uniform(x[1].wg), r0 = uniform(x[0].row) + h, r1 = uniform(x[1].row) + h;
+        join(first + (n1 > 0 ? n1 : 1), [&](int32_t k) {
+            const bool own = k >= first;
+            if ((own ? n1 : n0) == 0) return whole_row(p, grid, own ? 1 : 0, head) + (int64_t)t.base * G + r;
+            return own ? cut(wg1, r1, k - first) : cut(wg0, r0, k);
+        }, t.q0 + (int64_t)tok, head * G + h);
     }
 }
 
@@ -1518,7 +1517,7 @@ inline int32_t grid_for(int dp, int32_t n)
 }
 
 struct AttendLayout {
-    size_t split, share_base, parts, part, part_ml, whole, whole_ml, bytes;
+    size_t split, shared, parts, part, part_ml, bytes;
     int32_t grid, shared_rows, shared_tokens;
 };
 
@@ -1539,12 +1538,11 @@ inline AttendLayout attend_layout(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
         return at;
     };
     L.split = take(sizeof(Split) * (size_t)L.grid);
-    L.share_base = take(4 * (size_t)n);
+    L.shared = take(sizeof(Shared) * (size_t)n);
     L.parts = take(sizeof(Parts) * 2 * (size_t)Hkv * L.shared_tokens);
-    L.part_ml = take(4 * 2 * (size_t)kWideRows * 2 * L.grid);
-    L.part = take(4 * (size_t)dp * kWideRows * 2 * L.grid);
-    L.whole_ml = take(4 * 2 * 2 * (size_t)Hkv * L.shared_rows);
-    L.whole = take(4 * (size_t)dp * 2 * (size_t)Hkv * L.shared_rows);
+    const size_t all_rows = 2 * (size_t)L.grid * kWideRows + 2 * (size_t)Hkv * L.shared_rows;
+    L.part_ml = take(4 * 2 * all_rows);
+    L.part = take(4 * (size_t)dp * all_rows);
     L.bytes = o;
     return L;
 }
@@ -1557,6 +1555,9 @@ static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
     const int32_t shared_chunks = (p.a.Hq / p.a.Hkv + kWaves - 1) / kWaves;       // a row a wavefront, of one new token
     for (p.b0 = 0; p.b0 < p.a.B; p.b0 += p.n) {
         p.n = launch_size(p.a.B - p.b0);
+        // With few tiles, one wavefront with all of a tile's keys would be what the others wait for (16 requests of 300 tokens
+        // on 2 key heads 25 us, 21 by workgroups; 64 of 128 on 8 22 us, 27 by workgroups).
+        p.solo_most = (int64_t)p.n * p.a.Hkv > grid / 2 ? kSoloMost : 0;
         hipLaunchKernelGGL((attend_kernel<DP, Half>), dim3((unsigned)grid), dim3(kThreads), lds_bytes(DP, p.n), s, p);
         int rc = hip_check(hipGetLastError(), "rk_prefix_attention launch");
         if (rc) return rc;
@@ -1641,12 +1642,10 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
     p.status = status_word();
     if (!p.status) return fail(RK_EHIP, "rk_prefix_attention: no status word");
     p.split = (Split*)(ws + L.split);
-    p.share_base = (int32_t*)(ws + L.share_base);
+    p.shared = (Shared*)(ws + L.shared);
     p.parts = (Parts*)(ws + L.parts);
     p.part = (float*)(ws + L.part);
     p.part_ml = (float*)(ws + L.part_ml);
-    p.whole = (float*)(ws + L.whole);
-    p.whole_ml = (float*)(ws + L.whole_ml);
     p.shared_rows = L.shared_rows;
     p.shared_tokens = L.shared_tokens;
     return a->dtype == RK_F16 ? launch_of<true>(p, L.grid, (hipStream_t)stream) : launch_of<false>(p, L.grid, (hipStream_t)stream);
