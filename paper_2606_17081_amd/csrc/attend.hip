@@ -15,6 +15,7 @@ typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4;
+constexpr int32_t kLaunch = 1024;                    // requests of a launch: what is known of each is kept in LDS
 constexpr int kWideRows = 128, kWideKeys = 64;       // a wide step: 32 rows a wavefront, 64 keys
 constexpr int kNarrowRows = 32, kNarrowKeys = 128;   // a narrow step: 32 keys a wavefront
 constexpr int kSoloKeys = 32, kSoloMost = 512;       // a narrow tile of so few keys is one wavefront's: 32 a step
@@ -1287,29 +1288,32 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             int32_t lent, first, end;
             bool whole;                      // the group's first request is among them
         };
-        auto members = [&](int32_t i) {
+        constexpr int kMost = kLaunch / kThreads;
+        Members of[kMost];
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int32_t i = tid + u * kThreads;
+            Members& m = of[u];
+            m.lent = 0;
+            if (i >= B) continue;
             const int32_t g = last_group(goff, a.B, p.b0 + i), f = goff[g];
-            Members m;
             m.whole = f >= p.b0;
             m.first = m.whole ? f - p.b0 : 0;
             m.end = goff[g + 1] - p.b0 < B ? goff[g + 1] - p.b0 : B;
-            m.lent = 0;
             if (m.end - m.first >= 2) {
                 const int32_t most = a.kv_len[f] / RK_BLOCK_TOKENS, sh = a.shared[g];
                 m.lent = sh < most ? sh : most;
             }
-            return m;
-        };
-        for (int32_t i = tid; i < B; i += kThreads) {
-            const Members m = members(i);
             const int32_t tokens = req[i].tokens;
             if (m.lent > 0 && (tokens < 0 || (tokens > 0 && req[i].kv - tokens < m.lent * RK_BLOCK_TOKENS - 1)))
                 atomicOr(&req[m.first].base, i == m.first && m.whole ? 1 : 2);       // (base is not needed yet)
         }
         __syncthreads();
-        for (int32_t i = tid; i < B; i += kThreads) {
-            const Members m = members(i);
-            if (m.lent < kShareBlocks) continue;
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int32_t i = tid + u * kThreads;
+            const Members& m = of[u];
+            if (i >= B || m.lent < kShareBlocks) continue;
             const int32_t broken = req[m.first].base, f = m.first + (broken & 1);
             if (m.end - f < 2 || (broken & 2) || i < f) continue;
             // together where most members have fewer rows than a wide tile
@@ -1502,8 +1506,6 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t gr
 
 inline int head_size(int32_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 192 ? 192 : 256; }
 
-// requests of a launch: their places along the line of work are kept in LDS
-constexpr int32_t kLaunch = 1024;
 inline int32_t launch_size(int32_t B) { return B < kLaunch ? B : kLaunch; }
 
 inline size_t lds_bytes(int dp, int32_t n) { return (size_t)512 * dp + sizeof(Request) * (size_t)n; }

@@ -85,12 +85,14 @@ __device__ __forceinline__ void sort_pass(const int32_t* el, const int32_t* key,
     __syncthreads();
 }
 
-// Leading blocks that request i's chain has in common with request f's, by a team of 16 lanes (sub: the lane's place,
-// shift: its first lane); 0 for lanes with pair = false, which take part all the same.  Chained hashes agree up to the first block that
-// differs and nowhere after it, so each round tests 16 positions and keeps a sixteenth of the interval.
+// Leading blocks that request i's chain has in common with request f's, by a team of Team lanes; 0 for teams with
+// pair = false, which take part all the same.  Chained hashes agree up to the first block that
+// differs and nowhere after it, so each round tests Team positions and keeps a Team-th of the interval.
+template <int Team>
 __device__ __forceinline__ int32_t common_blocks(const uint64_t* __restrict__ chains, const int64_t* __restrict__ chain_off,
-                                                 int32_t i, int32_t f, bool pair, int sub, int shift)
+                                                 int32_t i, int32_t f, bool pair)
 {
+    const int sub = threadIdx.x & (Team - 1), shift = threadIdx.x & 63 & ~(Team - 1);
     int64_t a = 0, b = 0;
     int32_t have = 0, most = 0;              // `have` blocks agree; at most `most` do
     if (pair) {
@@ -101,14 +103,14 @@ __device__ __forceinline__ int32_t common_blocks(const uint64_t* __restrict__ ch
     }
     while (__any(have < most)) {
         const int64_t w = most - have;
-        const int32_t x = have + (int32_t)((int64_t)(sub + 1) * w / 16);       // a count of blocks, <= most
+        const int32_t x = have + (int32_t)((int64_t)(sub + 1) * w / Team);     // a count of blocks, <= most
         bool same = false;
         if (have < most) same = x == have || chains[a + x - 1] == chains[b + x - 1];
-        const uint32_t m = (uint32_t)(__ballot(same) >> shift) & 0xffffu;
+        const uint32_t m = (uint32_t)(__ballot(same) >> shift) & ((1u << Team) - 1);
         if (have < most) {
             const int k = __popc(m);         // the first k samples agree
-            const int32_t agreed = have + (int32_t)((int64_t)k * w / 16);
-            if (k < 16) most = have + (int32_t)((int64_t)(k + 1) * w / 16) - 1;
+            const int32_t agreed = have + (int32_t)((int64_t)k * w / Team);
+            if (k < Team) most = have + (int32_t)((int64_t)(k + 1) * w / Team) - 1;
             have = agreed;
         }
     }
@@ -123,22 +125,31 @@ __global__ __launch_bounds__(kBatchThreads) void group_kernel(int32_t B, const u
 {
     __shared__ GroupLds s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int x = tid; x < kGroupSlots; x += kBatchThreads) {
+    int32_t slot[kPer], first[kPer];
+    uint64_t key[kPer];
+    int64_t c0[kPer], c1[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        const int32_t i = 64 * (kPer * wave + u) + lane;
+        c0[u] = c1[u] = 0;
+        if (i < B) {
+            c0[u] = chain_off[i];
+            c1[u] = chain_off[i + 1];
+        }
+    }
+    for (int x = tid; x < kGroupSlots; x += kBatchThreads) {       // (while the offsets come)
         s.key[x] = 0ull;
         s.first[x] = 0x7fffffff;
     }
     for (int x = tid; x <= kBatchMax; x += kBatchThreads) s.off[x] = 0;
-    int32_t slot[kPer], first[kPer];
-    uint64_t key[kPer];
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
         const int32_t i = 64 * (kPer * wave + u) + lane;
         key[u] = 0ull;
         if (i < B) {
-            const int64_t c0 = chain_off[i], c1 = chain_off[i + 1];
-            if (c1 < c0 || c0 < 0) atomicOr(status, RK_DEV_BAD_OFFSETS);
-            else if (c1 - c0 >= min_blocks) {
-                key[u] = chains[c0 + min_blocks - 1];
+            if (c1[u] < c0[u] || c0[u] < 0) atomicOr(status, RK_DEV_BAD_OFFSETS);
+            else if (c1[u] - c0[u] >= min_blocks) {
+                key[u] = chains[c0[u] + min_blocks - 1];
                 if (key[u] == 0ull) atomicOr(status, RK_DEV_ZERO_KEY);
             }
         }
@@ -221,7 +232,7 @@ __global__ __launch_bounds__(kBatchThreads) void group_kernel(int32_t B, const u
         __syncthreads();
         for (int32_t i0 = 0; i0 < B; i0 += kBatchThreads / 16) {
             const int32_t i = i0 + (tid >> 4), f = i < B ? first_of[i] : i;
-            const int32_t n = common_blocks(chains, chain_off, i, f, f != i, tid & 15, tid & 48);
+            const int32_t n = common_blocks<16>(chains, chain_off, i, f, f != i);
             if (f != i && (tid & 15) == 0) atomicMin(&s.off[group_of[i]], n);
         }
         __syncthreads();
@@ -253,30 +264,42 @@ __global__ __launch_bounds__(kBatchThreads) void group_kernel(int32_t B, const u
 }
 
 // shared_g: the least number of leading blocks that a member has in common with its group's first request; a team of
-// 16 lanes per place in the order.
+// 4 lanes per place in the order.  A workgroup's 64 places are those of at most 64 groups, one after the other, so it
+// makes one global minimum a group: a popular group's members would wait for each other there (one a member:
+// 20 us for 4,096 requests of 256 groups).
 __global__ __launch_bounds__(256) void common_kernel(int32_t B, const uint64_t* __restrict__ chains,
                                                      const int64_t* __restrict__ chain_off,
                                                      const int32_t* __restrict__ order,
                                                      const int64_t* __restrict__ group_off, int32_t* __restrict__ shared)
 {
-    const int sub = threadIdx.x & 15, shift = threadIdx.x & 48;
-    const int32_t r = (int32_t)(blockIdx.x * (blockDim.x >> 4) + (threadIdx.x >> 4));
-    // the group that holds place r: the last g with group_off[g] <= r
-    int32_t lo = 0, hi = B;                  // group_off[lo] <= r < group_off[hi]
-    const bool in = r < B;
-    while (__any(in && hi - lo > 1)) {
-        const int32_t x = lo + (int32_t)((int64_t)(sub + 1) * (hi - lo) / 17);
-        const bool le = in && group_off[x < B ? x : B] <= r;
-        const uint32_t m = (uint32_t)(__ballot(le) >> shift) & 0xffffu;
-        const int k = __popc(m);             // the first k samples are <= r
-        const int32_t w = hi - lo;
-        if (k < 16) hi = lo + (int32_t)((int64_t)(k + 1) * w / 17);
-        if (k > 0) lo = lo + (int32_t)((int64_t)k * w / 17);
+    __shared__ int32_t s_least[64], s_group;
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (tid < 64) s_least[tid] = 0x7fffffff;
+    // the group that holds the wavefront's first place: the last g with group_off[g] <= r0
+    const int32_t r0 = (int32_t)(blockIdx.x * 64 + (tid >> 6) * 16), r = r0 + (lane >> 2);
+    int32_t lo = 0, hi = B;                  // group_off[lo] <= r0 < group_off[hi], if r0 is a place
+    while (r0 < B && hi - lo > 1) {
+        const int32_t w = hi - lo, x = lo + (int32_t)((int64_t)(lane + 1) * w / 65);
+        const int k = __popcll(__ballot(group_off[x] <= r0));      // the first k samples are <= r0
+        if (k < 64) hi = lo + (int32_t)((int64_t)(k + 1) * w / 65);
+        if (k > 0) lo = lo + (int32_t)((int64_t)k * w / 65);
     }
-    const int32_t f = in ? order[group_off[lo]] : 0, i = in ? order[r] : 0;
+    if (tid == 0) s_group = lo;
+    // the 16 places' groups are among the next 16
+    const int32_t next = lo + 1 + (lane & 15);
+    const int64_t start = group_off[next < B ? next : B];
+    int32_t g = lo;
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+        if (__shfl(start, u) <= r && r < B) g = lo + 1 + u;
+    const bool in = r < B;
+    const int32_t f = in ? order[group_off[g]] : 0, i = in ? order[r] : 0;
     const bool pair = in && f != i;
-    const int32_t n = common_blocks(chains, chain_off, i, f, pair, sub, shift);
-    if (pair && sub == 0) atomicMin(&shared[lo], n);
+    const int32_t n = common_blocks<4>(chains, chain_off, i, f, pair);
+    __syncthreads();
+    if (pair && (lane & 3) == 0) atomicMin(&s_least[(g - s_group) & 63], n);
+    __syncthreads();
+    if (tid < 64 && s_least[tid] != 0x7fffffff) atomicMin(&shared[s_group + tid], s_least[tid]);
 }
 
 // --------------------------------------------------------------- block tables
@@ -512,7 +535,7 @@ int rk_prefix_groups(int32_t B, const uint64_t* chains, const int64_t* chain_off
     hipLaunchKernelGGL(group_kernel, dim3(1), dim3(kBatchThreads), 0, s, B, chains, chain_off, min_blocks, order,
                        group_off, shared, n_groups, st);
     if (B > kFewGroups)
-        hipLaunchKernelGGL(common_kernel, dim3((unsigned)((B + 15) / 16)), dim3(256), 0, s, B, chains, chain_off, order,
+        hipLaunchKernelGGL(common_kernel, dim3((unsigned)((B + 63) / 64)), dim3(256), 0, s, B, chains, chain_off, order,
                            group_off, shared);
     return hip_check(hipGetLastError(), "rk_prefix_groups launch");
 }
