@@ -592,7 +592,7 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
  * with sums and softmax statistics in fp32 and the w_j of a tile rounded to the cache's type for
  * the product with the values.  With groups, the first lead entries (as in
  * rk_block_tables) of a group's rows are the same blocks, and where that is the faster way
- * the group's rows attend to them together, read through the first row.
+ * the group's rows attend to them together, read through the row of one of them.
  * No key or value past a token's position has a part in its result, whatever
  * it holds; the tokens of q behind q_off[B] are not read, and their rows of out and lse stay
  * as they were.
@@ -603,11 +603,12 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
  *   q, out      [T, Hq, D], strides q_token, q_head, out_token, out_head
  *   k_cache, v_cache  [n_blocks, 16, Hkv, D], strides ks, vs (token stride >= D and
  *               < 2^26)
- *   tables      int32 [B * table_stride]
+ *   tables      int32 [B * table_stride], table_stride at most 2^26
  *   kv_len      int32 [B]    tokens of each sequence, the new ones included
  *   q_off       int64 [B+1]  tokens of q of each request
  *   group_off, shared        as in rk_block_tables, or both NULL
  *   lse         float [T * Hq], or NULL
+ *   scale       -1e18..1e18
  * Strides are multiples of 8 elements (>= 0), pointers of 16 bytes; out overlaps no input.
  * workspace: rk_prefix_attention_workspace_size bytes, 256-byte aligned, of any content, for this
  * call alone until it has run.

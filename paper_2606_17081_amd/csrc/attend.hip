@@ -51,6 +51,8 @@ struct AttendArgs {
     rk_attention a;
     int32_t* status;
     int32_t b0, n;                           // the launch's requests: n from b0 on
+    int32_t G, wide_tokens;                  // query heads of a key head, tokens of a wide tile
+    uint32_t g_inverse;                      // 2^16 / G, rounded up
     int32_t solo_most;                       // most keys of a solo tile
     Split* split;                            // [grid]
     Shared* shared;                          // [n]: the requests' tokens that share a prefix
@@ -255,7 +257,7 @@ struct Attend {
     float* const join;                                // LDS: 2 * kWaves * kNarrowRows
     const int wave;
     const int32_t G;                                  // query heads of a key head
-    const uint32_t g_inverse;                         // 2^16 / G, rounded up: exact quotients of rows of a tile
+    const uint32_t g_inverse;                         // (exact quotients of a tile's rows: fewer than 2^7)
     const float c;                                    // |scale| log2(e)
     const uint32_t last_piece;                        // of a row: the bytes before it
     // the pieces of a block that the lane loads: whole rows a load, or not
@@ -263,8 +265,8 @@ struct Attend {
     uint32_t k_at[kEven ? 2 : NI], v_at[kEven ? 2 : NI];
 
     __device__ __forceinline__ Attend(const AttendArgs& args, uint32_t lds, float* j, float scale)
-        : p(args), tile(lds), join(j), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), G(args.a.Hq / args.a.Hkv),
-          g_inverse((65535 + args.a.Hq / args.a.Hkv) / (args.a.Hq / args.a.Hkv)), c(scale),
+        : p(args), tile(lds), join(j), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), G(args.G),
+          g_inverse(args.g_inverse), c(scale),
           last_piece(2 * args.a.D - 16)
     {
         const int lane = threadIdx.x & 63;
@@ -1068,14 +1070,14 @@ __device__ __forceinline__ int32_t steps_before(uint64_t length, int32_t steps)
     return n < (uint64_t)steps ? (int32_t)n : steps;
 }
 
-__device__ __forceinline__ Segment own_segment(const Request& r, int32_t G, int32_t solo_most)
+__device__ __forceinline__ Segment own_segment(const Request& r, const AttendArgs& p)
 {
     Segment s{};
     s.tokens = r.tokens;
-    s.rows = r.tokens * G;
+    s.rows = r.tokens * p.G;
     const int64_t own = (int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS;
-    s.kind = s.rows > kNarrowRows ? kWide : own > solo_most ? kNarrow : kSolo;
-    s.per = s.kind == kWide ? kWideRows / G : s.tokens;
+    s.kind = s.rows > kNarrowRows ? kWide : own > p.solo_most ? kNarrow : kSolo;
+    s.per = s.kind == kWide ? p.wide_tokens : s.tokens;
     if (s.tokens == 0) return s;
     s.tiles = (s.tokens + s.per - 1) / s.per;
     if (s.tiles == 1) {
@@ -1091,13 +1093,13 @@ __device__ __forceinline__ Segment own_segment(const Request& r, int32_t G, int3
     return s;
 }
 
-__device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks, int32_t G, int32_t solo_most)
+__device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks, const AttendArgs& p)
 {
     Segment s{};
     s.tokens = tokens;
-    s.rows = tokens * G;
-    s.kind = s.rows > kNarrowRows ? kWide : blocks * RK_BLOCK_TOKENS > solo_most ? kNarrow : kSolo;
-    s.per = s.kind == kWide ? kWideRows / G : s.tokens;
+    s.rows = tokens * p.G;
+    s.kind = s.rows > kNarrowRows ? kWide : blocks * RK_BLOCK_TOKENS > p.solo_most ? kNarrow : kSolo;
+    s.per = s.kind == kWide ? p.wide_tokens : s.tokens;
     s.tiles = (s.tokens + s.per - 1) / s.per;
     s.steps0 = steps_for((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
     s.pair = extent(s.steps0, s.kind);
@@ -1140,12 +1142,12 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         bool prefix = false;
         uint64_t before = 0;
         if (r.end) {
-            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, G, p.solo_most);
+            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, p);
             before = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             prefix = off < before;
         }
         if (!prefix) {
-            sg = own_segment(r, G, p.solo_most);
+            sg = own_segment(r, p);
             const uint64_t own = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             off -= before;
             if (off >= own) {                // on to the next request
@@ -1244,7 +1246,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
     using A = Attend<DP, Half>;
     const rk_attention& a = p.a;
     const int tid = threadIdx.x;
-    const int32_t B = p.n, G = a.Hq / a.Hkv;
+    const int32_t B = p.n, G = p.G;
     Request* req = reinterpret_cast<Request*>(lds + A::kTileBytes);
     int32_t* goff = reinterpret_cast<int32_t*>(lds);                 // until the keys and values come
     const bool tell = blockIdx.x == 0;
@@ -1335,10 +1337,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 #pragma unroll
             for (int k = 0; k < 3; ++k) x.of[k] += sg.kind == k ? sg.cost * (uint64_t)a.Hkv : 0;
         };
-        add(own_segment(req[i], G, p.solo_most));
+        add(own_segment(req[i], p));
         if (req[i].end) {
             const Request& l = req[req[i].end - 1];
-            add(prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, G, p.solo_most));
+            add(prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, p));
         }
     };
     uint32_t together = 0;
@@ -1381,8 +1383,11 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             if (req[i].shared) tok += req[i].tokens;
             if (tell) p.shared[i] = Shared{req[i].q0, req[i].shared ? req[i].tokens : 0, req[i].base, 0};
             if (!here) continue;
-            Cost k{};
-            cost_of(i, k);
+            Cost k = mine;
+            if (per > 1) {
+                k = Cost{};
+                cost_of(i, k);
+            }
             const uint64_t w = kind == kWide ? k.of[kWide] : kind == kNarrow ? k.of[kNarrow] : k.of[kSolo];
             for (int q = 0; q < pieces; ++q) {
                 const uint64_t from = first + q * each;
@@ -1416,7 +1421,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t gr
 {
     const rk_attention& a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int32_t G = a.Hq / a.Hkv;
+    const int32_t G = p.G;
     constexpr int N = DP / 64;
     // n parts at the rows row_of(k), to the output's row of the token and query head
     auto join = [&](int32_t n, auto&& row_of, int64_t token, int32_t h) {
@@ -1433,7 +1438,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t gr
 #pragma unroll
             for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
             const float nm = fmaxf(m, top);
-            if (nm == -INFINITY) continue;
+            if (nm == -INFINITY) {           // no key seen, or scores that are no numbers: l tells
+#pragma unroll
+                for (int d = 32; d > 0; d >>= 1) pl += __shfl_xor(pl, d);
+                l += pl;
+                continue;
+            }
             const float old = __builtin_amdgcn_exp2f(m - nm), w = __builtin_amdgcn_exp2f(pm - nm);
             float sum = w * pl;
 #pragma unroll
@@ -1552,9 +1562,9 @@ inline AttendLayout attend_layout(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
 template <int DP, bool Half>
 static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
 {
-    const int64_t rows = p.a.T * (p.a.Hq / p.a.Hkv);
+    const int64_t rows = p.a.T * p.G;
     const int32_t chunks = rows <= 4 ? 1 : rows <= 32 ? 4 : 8;
-    const int32_t shared_chunks = (p.a.Hq / p.a.Hkv + kWaves - 1) / kWaves;       // a row a wavefront, of one new token
+    const int32_t shared_chunks = (p.G + kWaves - 1) / kWaves;       // a row a wavefront, of one new token
     for (p.b0 = 0; p.b0 < p.a.B; p.b0 += p.n) {
         p.n = launch_size(p.a.B - p.b0);
         // With few tiles, one wavefront with all of a tile's keys would be what the others wait for (16 requests of 300 tokens
@@ -1619,6 +1629,7 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
         return fail(rc, "rk_prefix_attention: %s", what);
     if (a->dtype != RK_BF16 && a->dtype != RK_F16) return fail(RK_EUNSUPPORTED, "rk_prefix_attention: dtype %d", a->dtype);
     if (a->n_blocks < 0 || a->table_stride < 0) return fail(RK_EINVAL, "rk_prefix_attention: a negative size");
+    if (a->table_stride > 1 << 26) return fail(RK_EUNSUPPORTED, "rk_prefix_attention: table_stride > 2^26 blocks");
     if (!(fabsf(a->scale) <= 1e18f)) return fail(RK_EINVAL, "rk_prefix_attention: scale outside -1e18..1e18");
     const int64_t strides[] = {a->q_token, a->q_head, a->out_token, a->out_head, a->ks.block, a->ks.token, a->ks.head,
                                a->vs.block, a->vs.token, a->vs.head};
@@ -1648,6 +1659,9 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
     p.parts = (Parts*)(ws + L.parts);
     p.part = (float*)(ws + L.part);
     p.part_ml = (float*)(ws + L.part_ml);
+    p.G = a->Hq / a->Hkv;
+    p.wide_tokens = kWideRows / p.G;
+    p.g_inverse = (uint32_t)((65535 + p.G) / p.G);
     p.shared_rows = L.shared_rows;
     p.shared_tokens = L.shared_tokens;
     return a->dtype == RK_F16 ? launch_of<true>(p, L.grid, (hipStream_t)stream) : launch_of<false>(p, L.grid, (hipStream_t)stream);

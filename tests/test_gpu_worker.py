@@ -421,6 +421,22 @@ def test_attend_not_finite_in_later_tokens(gpu, Hq, new):
                 assert np.array_equal(np.isinf(o[:new]), np.isinf(host(out)[:new]))
 
 
+@pytest.mark.parametrize("kv,new,Hq", [(60, 1, 2), (9000, 1, 4), (700, 300, 8), (9000, 2, 64)])
+def test_attend_scores_that_are_no_numbers(gpu, kv, new, Hq):
+    """A query that is NaN gives NaN, also where its parts are joined; a key that is NaN, to the tokens that see it."""
+    torch, rk = gpu
+    b = Batch(torch, rng_of("nan", kv, new), [kv, 50], [new, 1], Hq, 1, 64)
+    b.q[0, Hq - 1, 5] = float("nan")
+    a, more = b.args(rk)
+    out, lse = rk.prefix_attention(*a, want_lse=True)
+    b.check(out, lse)
+    assert np.isnan(host(out)[0, Hq - 1]).all() and np.isfinite(host(out)[1:]).all()
+    b.caches[0][int(b.tables[0, 1]), 2, 0, 3] = float("nan")           # position 18
+    out, lse = rk.prefix_attention(*a, want_lse=True)
+    b.check(out, lse)
+    assert np.isnan(host(out)[:new]).all() and np.isnan(host(lse)[:new]).all() and np.isfinite(host(out)[new:]).all()
+
+
 def test_attend_large_scores(gpu):
     """Scores in the thousands: one key takes all, none overflows."""
     rng = rng_of("large")
@@ -533,6 +549,42 @@ def test_attend_two_streams_at_once(gpu):
     torch.cuda.synchronize()
     for k in range(2):
         assert all(torch.equal(want[k], g) for g in got[k])
+
+
+def test_attend_captured_by_a_fresh_process(gpu):
+    """The process's first calls of the library may be captured ones."""
+    import subprocess
+    import sys
+    code = """
+import numpy as np, torch
+from paper_2606_17081_amd import rkroute as rk
+B, D = 5, 64
+t = torch.arange(40, dtype=torch.int32, device="cuda").view(B, 8)
+k, v = (torch.randn(40, 16, 2, D, device="cuda", dtype=torch.float16) for _ in range(2))
+q = torch.randn(B, 4, D, device="cuda", dtype=torch.float16)
+kv = torch.tensor([3, 128, 17, 60, 99], dtype=torch.int32, device="cuda")
+off = torch.arange(B + 1, device="cuda")
+one, have = torch.ones_like(kv), torch.full_like(kv, 8)
+chains = torch.arange(1, 11, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    groups = rk.prefix_groups(chains, 2 * off, 1)
+    _, slots, q_off, _ = rk.block_tables(t, kv, one, have, t.view(-1), B)
+    rk.kv_write(k[0, :B], v[0, :B], k, v, slots)
+    out, _ = rk.prefix_attention(q, k, v, t, kv, q_off)
+for _ in range(3):
+    q.normal_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, rk.prefix_attention(q, k, v, t, kv, off)[0])
+assert int(groups[3]) == 5 and rk.device_status() == 0
+print("replayed")
+"""
+    import os
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and "replayed" in r.stdout, r.stderr[-2000:]
 
 
 # ------------------------------------------------------------------ together

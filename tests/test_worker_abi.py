@@ -90,7 +90,8 @@ def test_attention_refusals(L):
     assert rc(Hq=7) == rc(Hq=0) == rc(Hkv=0) == rk.RK_EINVAL
     assert rc(B=rk.RK_MAX_BATCH + 1) == rc(Hq=2 * 129) == rc(D=12) == rc(D=264) == rc(D=0) == rk.RK_EUNSUPPORTED
     assert rc(T=1 << 40) == rc(dtype=2) == rc(dtype=-1) == rk.RK_EUNSUPPORTED
-    assert rc(scale=float("nan")) == rc(scale=float("inf")) == rk.RK_EINVAL
+    assert rc(scale=float("nan")) == rc(scale=float("inf")) == rc(scale=-2e18) == rk.RK_EINVAL
+    assert rc(table_stride=(1 << 26) + 1) == rk.RK_EUNSUPPORTED
     for k in ("q_token", "q_head", "out_token", "out_head"):
         assert rc(**{k: 4}) == rc(**{k: -8}) == rk.RK_EINVAL
     for k in ("ks", "vs"):
