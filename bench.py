@@ -629,6 +629,63 @@ def scoring_bench(torch, rk, wl, stream, steps, oracle=False):
     return out
 
 
+def worker_bench(torch, rk, wl, stream, steps, requests=768, Hq=16, Hkv=2, D=128):
+    """One worker's steps on the requests that the router sends it: the 1P/5D-shaped prompts hashed and routed by the
+    block index of what six workers hold, then the first worker's batch ordered by shared prefix, given blocks, its keys and
+    values written and attended to (one layer's heads on one of four GPUs), first the prompts, then one token for each."""
+    W, cap = 6, 32768
+    tr = wl.sweep70b_trace(0, 2 * requests)
+    up = rk.to_device
+    n_tok = np.diff(tr.tok_off)
+    chain_off = np.concatenate([[0], np.cumsum(tr.chain_blocks)]).astype(np.int64)
+    chains = rk.hash_chains(up(tr.tokens), up(tr.tok_off), up(chain_off))
+    # what the workers hold: the chains of the first half of the requests, dealt out in turn
+    owner = np.arange(requests) % W
+    pick = [np.concatenate([np.arange(chain_off[i], chain_off[i + 1]) for i in np.nonzero(owner == j)[0]]) for j in range(W)]
+    keys = chains[up(np.concatenate(pick))].contiguous()
+    key_off = np.concatenate([[0], np.cumsum([x.size for x in pick])]).astype(np.int64)
+    lg = index_log2_slots(int(key_off[-1]))
+    index = rk.index_build(keys, key_off, lg)
+    late = chain_off[requests:] - chain_off[requests]
+    mine = chains[int(chain_off[requests]):].contiguous()
+    _, _, am = rk.route_score_index(mine, up(late), index, lg, up(np.zeros(W, np.int32)), cap_blocks=cap)
+    batch = np.nonzero(am.cpu().numpy() == 0)[0][:rk.RK_MAX_BATCH]
+    B = batch.size
+    blocks = np.diff(late)[batch]
+    off = np.concatenate([[0], np.cumsum(blocks)]).astype(np.int64)
+    rows = np.concatenate([np.arange(late[i], late[i + 1]) for i in batch])
+    step_chains, step_off = mine[up(rows)].contiguous(), up(off)
+    groups = rk.prefix_groups(step_chains, step_off, 4)
+    order = groups[0].cpu().numpy()
+    kv = n_tok[requests:][batch][order].astype(np.int64)
+    group_off, shared = groups[1], groups[2]
+    first = np.repeat(group_off.cpu().numpy()[:-1], np.diff(group_off.cpu().numpy()))
+    lead = np.where(first == np.arange(B), 0, np.minimum(np.repeat(shared.cpu().numpy(), np.diff(group_off.cpu().numpy())),
+                                                         kv[first] // 16))
+    stride = int(kv.max()) // 16 + 2
+    n_blocks = int((kv // 16 + 2).sum())
+    caches = [torch.randn((n_blocks, 16, Hkv, D), device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    tables = torch.zeros((B, stride), dtype=torch.int32, device="cuda")
+    free = torch.randperm(n_blocks, device="cuda").to(torch.int32)
+    i32 = lambda a: up(np.ascontiguousarray(a, np.int32))  # noqa: E731
+    out = {"workload": f"{B} of {requests} 1P/5D-shaped requests routed to one of {W} workers, {Hq} query and {Hkv} key heads of {D}",
+           "groups": int(groups[3]), "shared_blocks": int(lead.sum())}
+    out["prefix_groups_ms"] = burst_ms(torch, stream, lambda: rk.prefix_groups(step_chains, step_off, 4), max(steps, 10))
+    for name, length, new, have in (("prompts", kv, kv - 16 * lead, 0 * kv), ("decode", kv + 1, 0 * kv + 1, -(-kv // 16))):
+        T = int(new.sum())
+        args = (tables, i32(length), i32(new), i32(have), free, T)
+        _, slots, q_off, taken = rk.block_tables(*args, group_off=group_off, shared=shared)
+        q, k, v = (torch.randn((T, h, D), device="cuda", dtype=torch.bfloat16) for h in (Hq, Hkv, Hkv))
+        calls = {"block_tables": lambda: rk.block_tables(*args, group_off=group_off, shared=shared),
+                 "kv_write": lambda: rk.kv_write(k, v, *caches, slots),
+                 "prefix_attention": lambda: rk.prefix_attention(q, *caches, tables, args[1], q_off, group_off, shared),
+                 "attention_without_groups": lambda: rk.prefix_attention(q, *caches, tables, args[1], q_off)}
+        out[name] = {"tokens": T, **{c + "_ms": round(burst_ms(torch, stream, f, max(steps, 10)), 5) for c, f in calls.items()}}
+        free = free[int(taken):].contiguous()
+    assert rk.device_status(reset=True) == 0
+    return out
+
+
 def policy_bench(torch, rk, wl, stream, steps):
     """The 1P/5D-shaped traces under every selection policy: 16 seeds x 5
     concurrency levels x (5 policies + the regime controller) in one launch."""
@@ -773,7 +830,8 @@ def main():
     ap.add_argument("--no-pipeline", action="store_true", help=argparse.SUPPRESS)
     ap.add_argument("--cpu-seeds", type=int, default=32, help="saturation seeds the oracle runs (all 40 episodes each)")
     ap.add_argument("--no-cpu-baseline", action="store_true")
-    ap.add_argument("--only", choices=("all", "saturation", "sweep", "scoring", "policies", "multiturn", "tiny"),
+    ap.add_argument("--only", choices=("all", "saturation", "sweep", "scoring", "policies", "multiturn", "tiny",
+                                       "worker"),
                     default="all", help="profiling passes: run one leg only, without the oracle")
     ap.add_argument("--calibrate-copy-mib", type=int, default=0,
                     help="only run a plain device copy of this size (counter calibration)")
@@ -806,6 +864,9 @@ def main():
         return
     if only == "tiny":
         print(json.dumps({"tiny": tiny_bench(torch, rk, wl, stream, args.steps, oracle=False)}), flush=True)
+        return
+    if only == "worker":
+        print(json.dumps({"worker": worker_bench(torch, rk, wl, stream, args.steps)}), flush=True)
         return
     if only == "policies":
         print(json.dumps({"policies": policy_bench(torch, rk, wl, stream, args.steps)}), flush=True)

@@ -28,7 +28,7 @@ constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
 constexpr uint32_t kLeast = 4;
 static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
 constexpr int kKeysOf[3] = {kWideKeys, kNarrowKeys, kSoloKeys};
-constexpr int kShareBlocks = 4;                      // shorter prefixes are not worth joining their parts
+constexpr int kJoinCost = 2;                         // of a request whose prefix and own keys are joined
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 
 // A tile that more than one workgroup worked on, as the workgroup that began it noted it; n = 0: none.
@@ -1315,12 +1315,16 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
         for (int u = 0; u < kMost; ++u) {
             const int32_t i = tid + u * kThreads;
             const Members& m = of[u];
-            if (i >= B || m.lent < kShareBlocks) continue;
+            if (i >= B || m.lent <= 0) continue;
             const int32_t broken = req[m.first].base, f = m.first + (broken & 1);
             if (m.end - f < 2 || (broken & 2) || i < f) continue;
-            // together where most members have fewer rows than a wide tile
-            const int64_t rows = (int64_t)(req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0) * G;
-            if (rows == 0 || rows >= (int64_t)kWideRows * (m.end - f)) continue;
+            // Together where that costs less along the line than each member's own steps over the prefix, a join a member
+            // counted; and only if most members have fewer rows than a wide tile (what the workspace holds).
+            const int64_t n = m.end - f, tokens = req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0, rows = tokens * G;
+            if (rows == 0 || rows >= kWideRows * n) continue;
+            const Segment sg = prefix_segment((int32_t)tokens, m.lent, p);
+            const int64_t apart = n * m.lent * (rows > kNarrowRows * n ? 2 : 1), costs = sg.kind == kSolo ? 1 : 4;    // in quarters
+            if ((int64_t)sg.cost * costs + 4 * kJoinCost * n >= apart) continue;
             req[i].shared = m.lent;
             if (i == f) req[i].end = m.end;
         }

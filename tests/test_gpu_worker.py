@@ -350,15 +350,63 @@ def test_attend_groups(gpu, sizes, shared, tail, new, dtype):
     assert gpu[1].device_status(reset=True) == 0
 
 
+@pytest.mark.parametrize("sizes,shared,tail,new,Hq,Hkv,D,dtype,apart", [
+    ([30], [100], 20, 1, 8, 2, 128, "bf16", ()), ([2], [300], 100, 1, 4, 4, 64, "fp16", ()), ([3], [90], 700, 1, 12, 1, 192, "bf16", ()),
+    ([40, 2, 50], [60, 200, 33], 40, 3, 7, 1, 80, "bf16", (1,)), ([64, 70], [70, 50], 1, 1, 16, 1, 256, "fp16", ()),
+    ([9, 200, 7], [25, 40, 31], 30, 1, 8, 8, 64, "bf16", ()), ([5], [120], 60, 12, 16, 2, 128, "bf16", ()),
+    ([20], [4000], 30, 1, 8, 1, 128, "bf16", ()), ([300], [20], 16, 1, 1, 1, 128, "fp16", ())])
+def test_attend_prefix_read_once(gpu, sizes, shared, tail, new, Hq, Hkv, D, dtype, apart):
+    """Prefixes long enough that a group attends to them together: through one row, the others' entries are not read.
+    apart: groups of the case whose members do it each for themselves all the same.  (In the fourth case two members of 200
+    shared blocks have up to 42 rows: one wide tile of 50 steps, 4 (12 + 2 * 50) + 4 * 2 * 2 = 464 quarters of the cost
+    unit, against 2 * 200 = 400 for the members' own steps.)"""
+    torch, rk = gpu
+    rng = rng_of("once", sizes, shared)
+    B = sum(sizes)
+    goff = np.concatenate([offsets(sizes), np.full(B - len(sizes), B)]).astype(np.int64)
+    sh = np.zeros(B, np.int32)
+    sh[:len(sizes)] = shared
+    own = rng.integers(1, tail + 1, B)
+    n = np.minimum(rng.integers(1, new + 1, B), own)
+    b = Batch(torch, rng, BLOCK * np.repeat(shared, sizes) + own, n, Hq, Hkv, D, dtype, goff=goff, shared=sh,
+              heads_first=Hq == 8)
+    want = b.want()
+    attend(gpu, b)
+    for i in range(B):
+        g = int(np.searchsorted(goff, i, side="right")) - 1
+        if i != goff[g] and g not in apart:
+            b.tables[i, :sh[g]] = -1
+    a, more = b.args(rk)
+    out, lse = rk.prefix_attention(*a, **more, want_lse=True)
+    b.check(out, lse, want=want)
+    assert rk.device_status(reset=True) == 0
+
+
+def test_attend_groups_over_several_launches(gpu):
+    """More requests than a launch takes: a group that spans two of them is attended to in parts."""
+    rng = rng_of("spans")
+    sizes, sh = [700, 900, 3, 497], [40, 30, 200, 60]
+    B = sum(sizes)
+    goff = np.concatenate([offsets(sizes), np.full(B - 4, B)]).astype(np.int64)
+    shared = np.zeros(B, np.int32)
+    shared[:4] = sh
+    kv = BLOCK * np.repeat(sh, sizes) + rng.integers(1, 30, B)
+    attend(gpu, Batch(gpu[0], rng, kv, np.ones(B, np.int64), 2, 1, 64, goff=goff, shared=shared))
+    assert gpu[1].device_status(reset=True) == 0
+
+
 def test_attend_group_brings_its_prefix(gpu):
     """The step in which a group arrives: the first request's new tokens are the prefix that the others share; and one
     member whose own new tokens lie in the prefix too."""
     rng = rng_of("brings")
-    kv, new = [200, 180, 170, 165, 161], [200, 20, 170, 5, 1]
-    for shared in (10, 9, 12, 1, 1000):
-        goff, sh = np.array([0, 5, 5, 5, 5, 5]), np.array([shared, 0, 0, 0, 0], np.int32)
-        b = Batch(gpu[0], rng, kv, new, 4, 2, 64, goff=goff, shared=sh)
-        attend(gpu, b)
+    for kv, new, most in (([200, 180, 170, 165, 161], [200, 20, 170, 5, 1], 10),
+                          ([1700, 1620, 1700, 1605, 1601], [1700, 20, 3, 5, 1], 100),
+                          ([1700, 1620, 1700, 1605, 1601], [1, 1, 300, 1, 1], 100),
+                          ([1700, 1620, 1700, 1605, 1601], [1, 30, 1, 0, 1], 100)):
+        for shared in (most, most - 1, most + 2, 1, 1000):
+            goff, sh = np.array([0, 5, 5, 5, 5, 5]), np.array([shared, 0, 0, 0, 0], np.int32)
+            b = Batch(gpu[0], rng, kv, new, 4, 2, 64, goff=goff, shared=sh)
+            attend(gpu, b)
     # members shorter than what they share
     b = Batch(gpu[0], rng, [200, 30, 16, 0, 200], [1, 1, 1, 0, 2], 4, 2, 64, goff=goff,
               shared=np.array([12, 0, 0, 0, 0], np.int32))
@@ -596,13 +644,13 @@ def test_whole_steps_together(gpu):
     rng = rng_of("whole")
     Hq, Hkv, D, B = 8, 2, 64, 23
     group = rng.integers(0, 4, B)
-    prefixes = rng.integers(0, 32000, (4, 160)).astype(np.int32)
+    prefixes = rng.integers(0, 32000, (4, 640)).astype(np.int32)
     prompts = [np.concatenate([prefixes[g], rng.integers(0, 32000, rng.integers(1, 90)).astype(np.int32)]) for g in group]
     n_tok = np.array([len(p) for p in prompts])
     chains = rk.hash_chains(rk.to_device(np.concatenate(prompts)), rk.to_device(offsets(n_tok)), rk.to_device(offsets(n_tok // 16)))
     order, goff, shared, n_groups = rk.prefix_groups(chains, rk.to_device(offsets(n_tok // 16)), 4)
     o = host(order)
-    assert int(n_groups) == len(set(group.tolist())) and (host(shared)[:int(n_groups)] >= 10).all()
+    assert int(n_groups) == len(set(group.tolist())) and (host(shared)[:int(n_groups)] >= 40).all()
     n_tok = n_tok[o]
     first, lead = ow.leads(n_tok, host(goff), host(shared))
 
@@ -611,7 +659,7 @@ def test_whole_steps_together(gpu):
 
     emb = torch.randn((32000, 2, Hkv, D), device="cuda", dtype=torch.bfloat16)
 
-    stride, blocks = 24, 23 * 24
+    stride, blocks = 52, 23 * 52
     tables = torch.zeros((B, stride), dtype=torch.int32, device="cuda")
     k_cache = torch.full((blocks, BLOCK, Hkv, D), float("nan"), dtype=torch.bfloat16, device="cuda")
     v_cache = torch.full_like(k_cache, float("nan"))
