@@ -432,19 +432,42 @@ struct Attend {
         auto issue_values = [&](int32_t x, const Step& e) {
             load_values(t, t.block0 + 4 * x + wave, e.own, values_at(x) + wave * (RK_BLOCK_TOKENS * kRow));
         };
-        auto key_piece = [&](uint32_t at, int x) {   // of the x-th product
-            const int kt = x & 1, ks = x >> 1;
-            return lds_read16(at + k_read[ks % (kTurn / 2)] + (uint32_t)(kt * 32 * kRow + ks / (kTurn / 2) * (16 * kTurn)));
+        // the x-th product's piece of the keys, or values, in a stage; what differs by constants is added by the reads
+        struct Keys {
+            uint32_t at[kTurn / 2];
         };
-        auto value_piece = [&](uint32_t at, int x) {
+        struct Values {
+            uint32_t at[kTurn / 4], at8[kTurn / 4];  // (of rows 8 further, less those rows)
+        };
+        auto keys_in = [&](uint32_t at) {
+            Keys k;
+#pragma unroll
+            for (int x = 0; x < kTurn / 2; ++x) k.at[x] = at + k_read[x];
+            return k;
+        };
+        auto values_in = [&](uint32_t at) {
+            Values v;
+#pragma unroll
+            for (int x = 0; x < kTurn / 4; ++x) {
+                v.at[x] = at + v_read[x];
+                v.at8[x] = v.at[x] ^ 16 * turn(8);
+            }
+            return v;
+        };
+        auto key_piece = [&](const Keys& k, int x) {
+            const int kt = x & 1, ks = x >> 1;
+            return lds_read16(k.at[ks % (kTurn / 2)] + (uint32_t)(kt * 32 * kRow + ks / (kTurn / 2) * (16 * kTurn)));
+        };
+        auto value_piece = [&](const Values& v, int x) {
             constexpr int n = kTurn / 4;
             const int d = x % DT, kk = x / DT;
-            const uint32_t y = at + v_read[d % n] + (uint32_t)(d / n * (16 * kTurn) + 16 * kk * kRow);
-            const u32x2 lo = lds_read_columns(y), up = lds_read_columns((y ^ 16 * turn(8)) + 8 * kRow);
+            const uint32_t y = (uint32_t)(d / n * (16 * kTurn) + 16 * kk * kRow);
+            const u32x2 lo = lds_read_columns(v.at[d % n] + y), up = lds_read_columns(v.at8[d % n] + y + 8 * kRow);
             return u32x4{lo.x, lo.y, up.x, up.y};
         };
         u32x4 q[KS];
-        auto scores = [&](uint32_t at, f32x16* sc) {
+        auto scores = [&](uint32_t stage, f32x16* sc) {
+            const Keys at = keys_in(stage);
             u32x4 k[kAhead];
             sc[0] = sc[1] = f32x16{};
 #pragma unroll
@@ -489,7 +512,7 @@ struct Attend {
         // A step whose keys every row sees: sc its scores, top their largest; the next step's into nx.
         auto open_step = [&](int32_t x, const f32x16* sc, f32x16* nx, float& top) {
             const float base = follow(top);
-            const uint32_t ka = keys_at(x + 1), va = values_at(x);
+            const Keys ka = keys_in(keys_at(x + 1));
             constexpr int n = 2 * KS;
             u32x4 k[kAhead], w[4];
             nx[0] = nx[1] = f32x16{};
@@ -516,6 +539,7 @@ struct Attend {
             // (a wavefront in this product goes first: the other on its SIMD has its weights to compute meanwhile;
             // whole prompts 1,251 -> 1,214 us)
             __builtin_amdgcn_s_setprio(1);
+            const Values va = values_in(values_at(x));
             u32x4 v[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
@@ -631,14 +655,15 @@ struct Attend {
                     asm volatile("" ::: "memory");
                 }
             }
+            const Values vs = values_in(va);
             u32x4 v[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
+            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(vs, u);
 #pragma unroll
             for (int u = 0; u < 4 * DT; ++u) {
                 __builtin_amdgcn_sched_barrier(0);
                 o[u % DT] = mfma32<Half>(v[u % kAhead], w[u / DT], o[u % DT]);
-                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(va, u + kAhead);
+                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(vs, u + kAhead);
             }
             if (s + 1 >= t.s1) break;
             scores(keys_at(s + 1), sa);
