@@ -1331,9 +1331,13 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
                 const int32_t most = a.kv_len[f] / RK_BLOCK_TOKENS, sh = a.shared[g];
                 m.lent = sh < most ? sh : most;
             }
+            if (m.lent <= 0) continue;
             const int32_t tokens = req[i].tokens;
-            if (m.lent > 0 && (tokens < 0 || (tokens > 0 && req[i].kv - tokens < m.lent * RK_BLOCK_TOKENS - 1)))
+            if (tokens < 0 || (tokens > 0 && req[i].kv - tokens < m.lent * RK_BLOCK_TOKENS - 1))
                 atomicOr(&req[m.first].base, i == m.first && m.whole ? 1 : 2);       // (base is not needed yet)
+            // one without new tokens may be shorter than the prefix, but not the one whose row is read for all
+            else if (i - m.first < 2 && req[i].kv < m.lent * RK_BLOCK_TOKENS)
+                atomicOr(&req[m.first].base, i == m.first ? 4 : 8);
         }
         __syncthreads();
 #pragma unroll
@@ -1342,7 +1346,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             const Members& m = of[u];
             if (i >= B || m.lent <= 0) continue;
             const int32_t broken = req[m.first].base, f = m.first + (broken & 1);
-            if (m.end - f < 2 || (broken & 2) || i < f) continue;
+            if (m.end - f < 2 || (broken & 2) || (broken & (broken & 1 ? 8 : 4)) || i < f) continue;
             // Together where that costs less along the line than each member's own steps over the prefix, a join a member
             // counted; and only if most members have fewer rows than a wide tile (what the workspace holds).
             const int64_t n = m.end - f, tokens = req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0, rows = tokens * G;

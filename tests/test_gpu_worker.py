@@ -414,6 +414,25 @@ def test_attend_group_brings_its_prefix(gpu):
     assert gpu[1].device_status(reset=True) == 0
 
 
+def test_attend_group_whose_next_member_waits(gpu):
+    """The first request brings the prefix, and the next has neither new tokens nor the prefix's length: its row, which
+    names other blocks there, is not the one that the others' prefix is read through.  The same where it is the first
+    of a group's rest in another launch."""
+    rng = rng_of("waits")
+    kv, new = [1700, 10, 1620, 1605, 1601, 1630, 1640], [1700, 0, 1, 1, 1, 1, 1]
+    b = Batch(gpu[0], rng, kv, new, 4, 2, 64, goff=np.array([0] + [7] * 7), shared=np.array([100] + [0] * 6, np.int32))
+    b.tables[1, 1:100] = b.tables[2, 100]
+    attend(gpu, b)
+    B = 1100
+    kv = 16 * 40 + rng.integers(1, 60, B)
+    new = np.ones(B, np.int64)
+    kv[1024], new[1024] = 20, 0
+    b = Batch(gpu[0], rng, kv, new, 2, 1, 64, goff=np.array([0] + [B] * B), shared=np.array([40] + [0] * (B - 1), np.int32))
+    b.tables[1024, 2:40] = b.tables[0, 40]
+    attend(gpu, b)
+    assert gpu[1].device_status(reset=True) == 0
+
+
 def test_attend_many_requests(gpu):
     rng = rng_of("many")
     kv = rng.integers(1, 60, 4096)
