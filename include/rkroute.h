@@ -614,7 +614,7 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
  * call alone until it has run.
  * A request whose tokens, length or table do not fit (RK_DEV_BAD_OFFSETS;
  * RK_DEV_TOO_LARGE for kv_len > 16 table_stride) is skipped, its rows left as
- * they were; the keys of a block number outside 0..n_blocks-1 are left out
+ * they were, and where q_off steps back nothing is read together; the keys of a block number outside 0..n_blocks-1 are left out
  * (RK_DEV_BAD_BLOCK), and a token that sees no key gets 0 and -infinity.
  */
 typedef struct {

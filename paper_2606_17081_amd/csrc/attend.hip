@@ -1288,6 +1288,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
         const int64_t q0 = a.q_off[p.b0 + i], q1 = a.q_off[p.b0 + i + 1];
         const int32_t kv = a.kv_len[p.b0 + i];
         const bool large = (int64_t)kv > (int64_t)a.table_stride * RK_BLOCK_TOKENS;
+        if (q1 < q0) s_bad = 1;              // then requests may claim the same tokens, and what groups share have no room
         if (q0 < 0 || q1 < q0 || q1 > a.T || q1 - q0 > kv || large) {
             if (tell) atomicOr(p.status, large ? RK_DEV_TOO_LARGE : RK_DEV_BAD_OFFSETS);
             r.tokens = -1;

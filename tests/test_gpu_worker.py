@@ -563,6 +563,29 @@ def test_attend_bad_lengths(gpu):
         assert torch.equal(out, good) and rk.device_status(reset=True) == 0x1
 
 
+@pytest.mark.parametrize("B,G", [(12, 1), (600, 4)])
+def test_attend_offsets_that_go_back(gpu, B, G):
+    """Offsets with steps back between good ones, so that groups claim the same two tokens again and again, more of them
+    than there are: each request attends for itself, in the workspace of two tokens and not behind it."""
+    torch, rk = gpu
+    one = Batch(torch, rng_of("back", B), [1640, 1640, 1640], [1, 1, 0], G, 1, 64)
+    one.tables[1] = one.tables[0]
+    one.q[1] = one.q[0]
+    a, _ = one.args(rk)
+    want = rk.prefix_attention(*a)[0]
+    n = B // 3
+    q_off = np.concatenate([np.tile([0, 1, 2], n), [0]])
+    goff = np.concatenate([(3 * np.arange(n)[:, None] + [0, 2]).reshape(-1), np.full(B + 1 - 2 * n, B)])
+    up = rk.to_device
+    need = rk.prefix_attention_workspace_size(2, B, G, 1, 64)
+    ws = torch.full((need + 2 ** 22,), 77, dtype=torch.uint8, device="cuda")
+    got = rk.prefix_attention(one.q, *one.caches, up(np.tile(one.tables[0], (B, 1))), up(np.full(B, 1640, np.int32)), up(q_off),
+                              group_off=up(goff), shared=up(np.full(B, 100, np.int32)), workspace=ws)[0]
+    assert rk.device_status(reset=True) == 0x1
+    assert torch.allclose(got.float(), want.float(), rtol=4 * STEP["bf16"], atol=4 * STEP["bf16"])
+    assert (ws[need:] == 77).all()
+
+
 def test_attend_past_32_bits(gpu):
     """Blocks whose elements lie past 2^32 in the cache."""
     torch, rk = gpu
