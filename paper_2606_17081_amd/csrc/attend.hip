@@ -1258,6 +1258,16 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
     }
 }
 
+// Of `of` places, n spread evenly: whether place `at` is one of them.  at: its number among these, or among the others.
+__device__ __forceinline__ bool spread(uint32_t& at, uint32_t n, uint32_t of)
+{
+    if (of == 0) return false;
+    const uint32_t before = at * n / of;
+    const bool in = (at + 1) * n / of > before;
+    at = in ? before : at - before;
+    return in;
+}
+
 // One launch over a line of work: request after request (a group's prefix before its first member's own keys), key head
 // after key head, tile after tile, step after step.  The line is cut into equal pieces, a workgroup each, whatever the
 // lengths are; a tile that is cut is joined by the next kernel.
@@ -1399,13 +1409,15 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
     const uint32_t n_wide = (uint32_t)quotient_up(all.of[kWide], each), n_narrow = (uint32_t)quotient_up(all.of[kNarrow], each);
     const uint32_t n_solo = (uint32_t)((quotient_up(all.of[kSolo], each) + kWaves - 1) / kWaves);
     const uint32_t active = n_wide + n_narrow + n_solo;
-    // workgroups go to the 8 XCDs in turn: each XCD takes a stretch of the line
-    const uint32_t wg = (blockIdx.x & 7u) * ((active + 7) / 8) + (blockIdx.x >> 3);
-    const bool idle = (blockIdx.x >> 3) >= (active + 7) / 8 || wg >= active;
-    const int kind = wg < n_wide ? kWide : wg < n_wide + n_narrow ? kNarrow : kSolo;
+    // workgroups go to the 8 XCDs in turn: each XCD takes a stretch of each kind's line, the kinds mixed
+    const uint32_t stretch = (active + 7) / 8, place = (blockIdx.x & 7u) * stretch + (blockIdx.x >> 3);
+    const bool idle = (blockIdx.x >> 3) >= stretch || place >= active;
+    uint32_t at = place;                     // the number among its kind's
+    const int kind = spread(at, n_wide, active) ? kWide : spread(at, n_narrow, n_narrow + n_solo) ? kNarrow : kSolo;
+    const uint32_t wg = at + (kind == kWide ? 0 : kind == kNarrow ? n_wide : n_wide + n_narrow);
     const uint64_t end = kind == kWide ? all.of[kWide] : kind == kNarrow ? all.of[kNarrow] : all.of[kSolo];
     // the workgroup's piece, or its wavefronts' of solo tiles
-    const uint64_t first = (kind == kWide ? wg : kind == kNarrow ? wg - n_wide : (uint64_t)kWaves * (wg - n_wide - n_narrow)) * each;
+    const uint64_t first = (kind == kSolo ? (uint64_t)kWaves * at : at) * each;
     {
         uint32_t tok = tokens_upto - together;
         const uint64_t top = kind == kWide ? upto.of[kWide] : kind == kNarrow ? upto.of[kNarrow] : upto.of[kSolo];
