@@ -1,4 +1,15 @@
 // attend.hip -- attention of a step's new tokens over the block cache.
+//
+// out_t = sum_j w_j v_j / sum_j w_j, w_j = exp(scale q_t . k_j), in one pass over the keys: with m at least near the largest
+// score so far, o = sum 2^(s_j - m) v_j and l = sum 2^(s_j - m) (scores in units of log2) are rescaled when m moves, and
+// any split of the keys is joined by the same rule, o = sum_p 2^(m_p - m) o_p.  Both products run on matrix
+// instructions; m, l, o and the scores are fp32.  The w_j of a step are rounded to the cache's 16 bits, the only operands that the
+// instructions take: half a step of that type each, relative, so as much of the mean of |v| in a result (l sums them unrounded).
+//
+// What bounds it: few rows (a decoding batch) the reading of keys and values, 4 D bytes a key and head for 4 D
+// operations a row; from some hundred rows a key head on (a prompt, or a group on its prefix) the matrix instructions.  So there are tiles of two
+// shapes, wide and narrow, and solo ones for what is short.  128 requests on one prefix of 8,192 tokens (64 / 8 heads of 128):
+// 70 + 10 us; prompts of 2,500-6,000 tokens: 1.15-1.26 ms, 860-940 TFLOP/s; 5 requests of 60,000-131,072 tokens: 198 us, 5.1 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -23,7 +34,10 @@ constexpr int kSoloKeys = 32, kSoloMost = 512;       // a narrow tile of so few 
 // Kinds of tiles, each on a line of its own.
 enum Kind { kWide, kNarrow, kSolo };
 // What a step of a tile costs, and its beginning and end, relative to each other (a solo tile's to a wavefront, the others' to a
-// workgroup).  A piece of a line has at least kLeast, a step or more, so that a tile's parts follow each other without a gap.
+// workgroup): a wide or narrow step takes about 2 us, what comes before a wide tile's first and after its last 12 (a prologue without
+// products, and results out).  Measured: ends of 4 for narrow and solo ones, 128 requests on one prefix 82 -> 87 us, of 8,
+// groups of 200 62 -> 70; of 10 or 16 for wide ones, 0-5% more.  A piece of a line has at least kLeast, a step or more, so that a tile's
+// parts follow each other without a gap.
 constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
 constexpr uint32_t kLeast = 4;
 static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
@@ -222,7 +236,7 @@ __device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b)
 }
 __device__ __forceinline__ uint64_t quotient_up(uint64_t a, uint64_t b) { return quotient(a + b - 1, b); }
 
-// One tile's work: rows of the tokens [token, token + tokens) on key head `head`, steps [s0, s1) of n_steps.
+// One tile's work, or a part of it: rows of the tokens [token, token + tokens) on key head `head`, steps [s0, s1).
 struct Tile {
     const __attribute__((address_space(4))) int32_t* row;        // the block table's row
     int32_t block0;                          // first block of the segment
@@ -384,6 +398,13 @@ struct Attend {
     // Scores are computed transposed, keys x rows: a lane then holds 32 of the 64 scores of one row (lane
     // % 32) in registers, in the order in which the product with the values takes them: the row of
     // the value that lane half h multiplies with its j-th weight is the key whose score it holds.
+    //
+    // Bound by nothing alone: at D = 128 the two wavefronts of a SIMD have 2,048 cycles of matrix instructions a step, their CU's eight
+    // 2,048 of LDS reads (32 KB each at 128 B a cycle), and 1,600 of vector instructions, two thirds of them for exponentials and
+    // sums; on whole prompts the matrix units are busy 43% of the time.  Rows of 64 a wavefront would halve the LDS
+    // reads, but need 300 registers of the 256 that two wavefronts a SIMD have; one a SIMD (as for D > 128) reaches
+    // half the rate: pieces of prompts with D = 192, 104 us for 52 GFLOP.  Keys and values in LDS are read with no bank conflict.
+    // One prompt of 8,192 tokens, 64 / 8 heads of 128: 1.12 ms, 975 TFLOP/s.
     __device__ void wide(const Tile& t)
     {
         constexpr int KS = DP / 16, DT = DP / 32;
@@ -410,7 +431,8 @@ struct Attend {
         }
         constexpr uint32_t kKeys = kWideKeys * kRow;   // bytes of a step's keys; two of them, then two steps' values
         // Keys come two steps ahead, values one: while a step's weights are computed, the products of the next step's
-        // scores run beside them.  Pieces are read from LDS kAhead products before the one that takes them.
+        // scores run beside them (whole prompts 1,440 -> 1,360 us).  Pieces are read from LDS kAhead products before the one that
+        // takes them: 3 are as good, 6 spill registers (whole prompts 1,230 -> 1,500 us).
         constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
         struct Step {
             int32_t own;                             // this wavefront's block
@@ -670,8 +692,8 @@ struct Attend {
             advance();
         }
         l += __shfl_xor(l, 32);
-        // Out through LDS, so that whole rows are written: a lane's own pieces of a row are 8 or 16 bytes each, and writing those
-        // took 20 us a tile.  The keys' stages are free: everyone has read the last keys.
+        // Out through LDS, so that whole rows are written: a lane's own pieces of a row are 8 or 16 bytes each, of 32 rows at a
+        // time.  The keys' stages are free: everyone has read the last keys.
         const uint32_t mine = tile + wave * (32 * kRow);
         const int32_t rows = t.tokens * G - 32 * wave;
         const int late = afresh(lane);
@@ -725,7 +747,9 @@ struct Attend {
     // What bounds few rows is the reading of keys and values, so each wavefront takes keys of its own, with no
     // barrier: while it computes on the keys of a step its values are still under way, and the next step's keys
     // follow as soon as this step's are in registers.  The wavefronts' results are joined through LDS; of few keys a
-    // wavefront does a tile alone.
+    // wavefront does a tile alone.  Measured: 5 requests of 60,000-131,072 tokens, 16 / 4 heads of 128, 198 us for 1.01 GB, 5.1 TB/s; 128 of
+    // 2,048 tokens, 8 key heads, 215 us, 5.0 TB/s; one of 8,192 tokens 21 us, of 100 tokens 12 us, both waits one after the
+    // other (lengths, block numbers, keys, join).
     template <int NQ, bool Solo>
     __device__ void narrow(const Tile& t)
     {
@@ -1132,17 +1156,6 @@ __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks
     return s;
 }
 
-__device__ __forceinline__ int32_t last_group(const int32_t* off, int32_t n, int32_t v)
-{
-    int32_t lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (off[mid] <= v) lo = mid;
-        else hi = mid;
-    }
-    return lo;
-}
-
 // A workgroup's piece [from, to) of the line of tiles of kind K (of solo tiles: a wavefront's), from place `off` of
 // request i's part on; wg: the workgroup's place among all.
 template <int K, class A>
@@ -1270,7 +1283,10 @@ __device__ __forceinline__ bool spread(uint32_t& at, uint32_t n, uint32_t of)
 
 // One launch over a line of work: request after request (a group's prefix before its first member's own keys), key head
 // after key head, tile after tile, step after step.  The line is cut into equal pieces, a workgroup each, whatever the
-// lengths are; a tile that is cut is joined by the next kernel.
+// lengths are; a tile that is cut is joined by the next kernel.  Every workgroup works out the line for itself, from lengths
+// that only the device knows: 4-6 us, as long as another launch that told them would take.  Each kind has a line of its own, so
+// that a workgroup keeps to one kind's code; workgroups of different kinds lie side by side on a CU, where one waits for memory while the other
+// computes (128 requests on one prefix 86 -> 83 us, groups of 200 64 -> 62 us against kind after kind).
 template <int DP, bool Half>
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs p)
 {
@@ -1293,28 +1309,53 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
         }
     }
     __syncthreads();
-    for (int32_t i = tid; i < B; i += kThreads) {
-        Request r{};
-        const int64_t q0 = a.q_off[p.b0 + i], q1 = a.q_off[p.b0 + i + 1];
-        const int32_t kv = a.kv_len[p.b0 + i];
-        const bool large = (int64_t)kv > (int64_t)a.table_stride * RK_BLOCK_TOKENS;
-        if (q1 < q0) s_bad = 1;              // then requests may claim the same tokens, and what groups share have no room
-        if (q0 < 0 || q1 < q0 || q1 > a.T || q1 - q0 > kv || large) {
-            if (tell) atomicOr(p.status, large ? RK_DEV_TOO_LARGE : RK_DEV_BAD_OFFSETS);
-            r.tokens = -1;
-        } else {
-            r.kv = kv;
-            r.q0 = (int32_t)q0;
-            r.tokens = (int32_t)(q1 - q0);
+    // (loads of all of a thread's requests, or groups, together: one after the other, 533 requests take 2 us more)
+    constexpr int kMost = kLaunch / kThreads;
+    {
+        int64_t q0[kMost], q1[kMost];
+        int32_t kv[kMost];
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int32_t i = p.b0 + (tid + u * kThreads < B ? tid + u * kThreads : B - 1);
+            q0[u] = a.q_off[i];
+            q1[u] = a.q_off[i + 1];
+            kv[u] = a.kv_len[i];
         }
-        req[i] = r;
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int32_t i = tid + u * kThreads;
+            if (i >= B) break;
+            Request r{};
+            const bool large = (int64_t)kv[u] > (int64_t)a.table_stride * RK_BLOCK_TOKENS;
+            if (q1[u] < q0[u]) s_bad = 1;    // then requests may claim the same tokens, and what groups share have no room
+            if (q0[u] < 0 || q1[u] < q0[u] || q1[u] > a.T || q1[u] - q0[u] > kv[u] || large) {
+                if (tell) atomicOr(p.status, large ? RK_DEV_TOO_LARGE : RK_DEV_BAD_OFFSETS);
+                r.tokens = -1;
+            } else {
+                r.kv = kv[u];
+                r.q0 = (int32_t)q0[u];
+                r.tokens = (int32_t)(q1[u] - q0[u]);
+            }
+            req[i] = r;
+        }
     }
     if (a.group_off)
-        for (int32_t g = tid; g < a.B; g += kThreads) {
-            const int64_t x = a.group_off[g], y = a.group_off[g + 1];
-            if (x > y || x < 0 || y > a.B || (g == 0 && x != 0) || (g == a.B - 1 && y != a.B)) s_bad = 1;
-            goff[g] = (int32_t)x;
-            if (g == a.B - 1) goff[a.B] = (int32_t)y;
+        for (int32_t g0 = tid; g0 < a.B; g0 += kMost * kThreads) {
+            int64_t x[kMost], y[kMost];
+#pragma unroll
+            for (int u = 0; u < kMost; ++u) {
+                const int32_t g = g0 + u * kThreads < a.B ? g0 + u * kThreads : a.B - 1;
+                x[u] = a.group_off[g];
+                y[u] = a.group_off[g + 1];
+            }
+#pragma unroll
+            for (int u = 0; u < kMost; ++u) {
+                const int32_t g = g0 + u * kThreads;
+                if (g >= a.B) break;
+                if (x[u] > y[u] || x[u] < 0 || y[u] > a.B || (g == 0 && x[u] != 0) || (g == a.B - 1 && y[u] != a.B)) s_bad = 1;
+                goff[g] = (int32_t)x[u];
+                if (g == a.B - 1) goff[a.B] = (int32_t)y[u];
+            }
         }
     __syncthreads();
     const bool groups = a.group_off && !s_bad;
@@ -1326,22 +1367,30 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             int32_t lent, first, end;
             bool whole;                      // the group's first request is among them
         };
-        constexpr int kMost = kLaunch / kThreads;
         Members of[kMost];
+        int32_t group[kMost] = {}, most[kMost], sh[kMost];
+        for (int32_t step = 1 << (31 - __clz(a.B)); step > 0; step >>= 1)        // the last group that does not begin behind the request
+#pragma unroll
+            for (int u = 0; u < kMost; ++u) {
+                const int32_t g = group[u] + step < a.B ? group[u] + step : a.B;
+                if (goff[g] <= p.b0 + tid + u * kThreads && g < a.B) group[u] = g;
+            }
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int32_t f = goff[group[u]];
+            Members& m = of[u];
+            m.whole = f >= p.b0;
+            m.first = m.whole ? f - p.b0 : 0;
+            m.end = goff[group[u] + 1] - p.b0 < B ? goff[group[u] + 1] - p.b0 : B;
+            most[u] = a.kv_len[f < a.B ? f : a.B - 1];
+            sh[u] = a.shared[group[u]];
+        }
 #pragma unroll
         for (int u = 0; u < kMost; ++u) {
             const int32_t i = tid + u * kThreads;
             Members& m = of[u];
-            m.lent = 0;
-            if (i >= B) continue;
-            const int32_t g = last_group(goff, a.B, p.b0 + i), f = goff[g];
-            m.whole = f >= p.b0;
-            m.first = m.whole ? f - p.b0 : 0;
-            m.end = goff[g + 1] - p.b0 < B ? goff[g + 1] - p.b0 : B;
-            if (m.end - m.first >= 2) {
-                const int32_t most = a.kv_len[f] / RK_BLOCK_TOKENS, sh = a.shared[g];
-                m.lent = sh < most ? sh : most;
-            }
+            most[u] /= RK_BLOCK_TOKENS;
+            m.lent = i < B && m.end - m.first >= 2 ? (sh[u] < most[u] ? sh[u] : most[u]) : 0;
             if (m.lent <= 0) continue;
             const int32_t tokens = req[i].tokens;
             if (tokens < 0 || (tokens > 0 && req[i].kv - tokens < m.lent * RK_BLOCK_TOKENS - 1))
@@ -1359,7 +1408,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             const int32_t broken = req[m.first].base, f = m.first + (broken & 1);
             if (m.end - f < 2 || (broken & 2) || (broken & (broken & 1 ? 8 : 4)) || i < f) continue;
             // Together where that costs less along the line than each member's own steps over the prefix, a join a member
-            // counted; and only if most members have fewer rows than a wide tile (what the workspace holds).
+            // counted; and only if most members have fewer rows than a wide tile (what the workspace holds).  128 requests on
+            // 8,192 tokens: 80 us together, 507 us each for itself; 200 of 24 groups 62 and 129; pieces of prompts in 3 groups, of 350
+            // tokens each, 117 and 116 (there the matrix instructions bound both); 533 requests that share 5 blocks stay apart, for 141 us, 134
+            // when no groups are named.
             const int64_t n = m.end - f, tokens = req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0, rows = tokens * G;
             if (rows == 0 || rows >= kWideRows * n) continue;
             const Segment sg = prefix_segment((int32_t)tokens, m.lent, p);
@@ -1461,7 +1513,8 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 
 // The parts of rows that more than one workgroup worked on, joined: a wavefront a row, DP / 64 neighbouring values a
 // lane.  The parts' weights come first, a lane each; then their values, several loads under way at a time.  Waiting for
-// loads is all that bounds it, but of the rows of whole prompts' 500 cut tiles (33 us for 100 MB).
+// loads is all that bounds it (4 us with nothing to join, 8-10 us for decoding batches), but of the rows of whole prompts'
+// 500 cut tiles (30 us for 100 MB).
 template <int DP, bool Half>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks, int32_t shared_chunks)
 {
