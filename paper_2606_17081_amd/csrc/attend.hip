@@ -403,7 +403,7 @@ struct Attend {
     // 2,048 of LDS reads (32 KB each at 128 B a cycle), and 1,600 of vector instructions, two thirds of them for exponentials and
     // sums; on whole prompts the matrix units are busy 43% of the time.  Rows of 64 a wavefront would halve the LDS
     // reads, but need 300 registers of the 256 that two wavefronts a SIMD have; one a SIMD (as for D > 128) reaches
-    // half the rate: pieces of prompts with D = 192, 104 us for 52 GFLOP.  Keys and values in LDS are read with no bank conflict.
+    // half the rate: pieces of prompts with D = 192, 104 us for 52 GFLOP.  Conflicts of LDS banks are rare.
     // One prompt of 8,192 tokens, 64 / 8 heads of 128: 1.12 ms, 975 TFLOP/s.
     __device__ void wide(const Tile& t)
     {
