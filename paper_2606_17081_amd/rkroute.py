@@ -548,9 +548,16 @@ def _heads(name, t, dims):
     return t.dtype, t.shape
 
 
+def _no_gradient(what, *tensors):
+    for t in tensors:
+        if t.requires_grad and _torch().is_grad_enabled():
+            raise RkError(f"{what} has no gradient: call it under torch.no_grad(), or detach its arguments")
+
+
 def kv_write(k, v, k_cache, v_cache, slots, stream=None):
     """Keys and values [T, Hkv, D] of new tokens into the block cache [blocks, 16, Hkv, D] (rk_kv_write)."""
     dev = _where("k", k)
+    _no_gradient("kv_write", k, v, k_cache, v_cache)
     dtype, shape = _heads("k", k, 3)
     T, Hkv, D = shape
     k_token, k_head = _rows("k", k, dev, dtype, shape)
@@ -581,6 +588,7 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
     scale defaults to D ** -0.5.  Rows behind the last request's stay as they were (in an `out` allocated here,
     uninitialised)."""
     dev = _where("q", q)
+    _no_gradient("prefix_attention", q, k_cache, v_cache)
     dtype, shape = _heads("q", q, 3)
     T, Hq, D = shape
     q_token, q_head = _rows("q", q, dev, dtype, shape)
@@ -610,7 +618,7 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
         else:
             ws_bytes = workspace.numel() * workspace.element_size()
         a = _attention_struct.pack(
-            B, Hq, Hkv, D, _NARROW[dtype], blocks, stride, D ** -0.5 if scale is None else scale, T, q.data_ptr(),
+            B, Hq, Hkv, D, _NARROW[dtype], blocks, stride, max(D, 1) ** -0.5 if scale is None else scale, T, q.data_ptr(),
             q_token, q_head, k_cache.data_ptr(), *ks, v_cache.data_ptr(), *vs, _flat("tables", tables, i32, dev, 0),
             _flat("kv_len", kv_len, i32, dev, B), _flat("q_off", q_off, i64, dev, B + 1),
             _flat("group_off", group_off, i64, dev, B + 1) or 0, _flat("shared", shared, i32, dev, B) or 0,

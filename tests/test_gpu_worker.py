@@ -677,6 +677,25 @@ print("replayed")
     assert r.returncode == 0 and "replayed" in r.stdout, r.stderr[-2000:]
 
 
+def test_binding_refuses_gradients_and_empty_heads(gpu):
+    """What would go wrong without a word: results that a backward pass would take for constants; and heads of no values."""
+    torch, rk = gpu
+    b = Batch(torch, rng_of("grad"), [40], [3], 4, 2, 64)
+    a, _ = b.args(rk)
+    q, k = a[0].clone().requires_grad_(), a[1].clone().requires_grad_()
+    slots = torch.arange(3, device="cuda")
+    new = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: rk.prefix_attention(q, *a[1:]), lambda: rk.prefix_attention(a[0], k, *a[2:]),
+                 lambda: rk.kv_write(new.clone().requires_grad_(), new, a[1].clone(), a[2].clone(), slots)):
+        with pytest.raises(rk.RkError, match="gradient"):
+            call()
+    with torch.no_grad():
+        assert torch.equal(rk.prefix_attention(q, *a[1:])[0], rk.prefix_attention(*a)[0])
+    with pytest.raises(rk.RkError, match="multiple of 8"):
+        rk.prefix_attention(a[0][..., :0], a[1][..., :0], a[2][..., :0], *a[3:])
+    assert rk.device_status(reset=True) == 0
+
+
 # ------------------------------------------------------------------ together
 
 def test_whole_steps_together(gpu):
