@@ -231,7 +231,7 @@ __device__ __forceinline__ void incl_sums(uint64_t (&x)[3], uint32_t& z, uint64_
 
 // a / b of numbers below 2^51 (a line has at most 2^31 / 64 tiles of 2^24 steps): the quotient in 64-bit floating point, correctly
 // rounded, reaches the next whole number only if it is that, since what it lacks otherwise, 1 / b or more, is more than its rounding.
-// (Straight code, and little of it: the kernel's first instructions wait for each other's lines; integer division 0.5 us more a call.)
+// (Integer division, long code with a branch for large numbers, takes 0.5 us more a call.)
 __device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (uint64_t)((double)a / (double)b); }
 __device__ __forceinline__ uint64_t quotient_up(uint64_t a, uint64_t b) { return quotient(a + b - 1, b); }
 
