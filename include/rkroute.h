@@ -517,8 +517,9 @@ int rk_poa_estimate_noalloc(int32_t n_windows, const int64_t* win_off, int32_t n
  *                             can be handed on without their number
  *   shared      int32 [B]     shared_g, 0 from the last group on
  *   n_groups    int32 [1]
- * A hash of 0 at block min_blocks - 1 (a chain rk_hash_chains left short) names
- * no prefix: RK_DEV_ZERO_KEY, the request is a group of its own.
+ * A hash of 0 is a missing one (rk_hash_chains leaves the end of a chain so whose
+ * tokens were too few) and in common with none.  At block min_blocks - 1 it
+ * names no prefix: RK_DEV_ZERO_KEY, the request is a group of its own.
  */
 int rk_prefix_groups(int32_t B, const uint64_t* chains, const int64_t* chain_off, int32_t min_blocks,
                      int32_t* order, int64_t* group_off, int32_t* shared, int32_t* n_groups, void* stream);

@@ -12,9 +12,9 @@ BLOCK = 16
 
 
 def common_blocks(a, b) -> int:
-    """Leading blocks that two chains have in common."""
+    """Leading blocks that two chains have in common; a hash of 0 is missing, and in common with none."""
     n = 0
-    while n < min(len(a), len(b)) and a[n] == b[n]:
+    while n < min(len(a), len(b)) and a[n] == b[n] and a[n] != 0:
         n += 1
     return n
 

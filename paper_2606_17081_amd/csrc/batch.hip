@@ -90,7 +90,8 @@ __device__ __forceinline__ void sort_pass(const int32_t* el, const int32_t* key,
 
 // Leading blocks that request i's chain has in common with request f's, by a team of Team lanes; 0 for teams with
 // pair = false, which take part all the same.  Chained hashes agree up to the first block that
-// differs and nowhere after it, so each round tests Team positions and keeps a Team-th of the interval.
+// differs and nowhere after it, so each round tests Team positions and keeps a Team-th of the interval.  A hash of 0 is one that
+// is missing (from there on to the chain's end) and agrees with none.
 template <int Team>
 __device__ __forceinline__ int32_t common_blocks(const uint64_t* __restrict__ chains, const int64_t* __restrict__ chain_off,
                                                  int32_t i, int32_t f, bool pair)
@@ -108,10 +109,16 @@ __device__ __forceinline__ int32_t common_blocks(const uint64_t* __restrict__ ch
         const int64_t w = most - have;
         const int32_t x = have + (int32_t)((int64_t)(sub + 1) * w / Team);     // a count of blocks, <= most
         bool same = false;
-        if (have < most) same = x == have || chains[a + x - 1] == chains[b + x - 1];
+        if (have < most) {
+            same = x == have;
+            if (!same) {
+                const uint64_t h = chains[a + x - 1];
+                same = h != 0ull && h == chains[b + x - 1];
+            }
+        }
         const uint32_t m = (uint32_t)(__ballot(same) >> shift) & ((1u << Team) - 1);
         if (have < most) {
-            const int k = __popc(m);         // the first k samples agree
+            const int k = __ffs(~m) - 1;     // the first k samples agree (bit Team of m is 0)
             const int32_t agreed = have + (int32_t)((int64_t)k * w / Team);
             if (k < Team) most = have + (int32_t)((int64_t)(k + 1) * w / Team) - 1;
             have = agreed;

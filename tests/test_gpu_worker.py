@@ -100,6 +100,31 @@ def test_groups_zero_hash_and_bad_offsets(gpu):
     assert sorted(host(order).tolist()) == [0, 1, 2] and rk.device_status(reset=True) & 0x1
 
 
+@pytest.mark.parametrize("B", [2, 5, 64, 128, 129, 700])
+@pytest.mark.parametrize("longest", [6, 7, 33, 300])
+def test_groups_chains_left_short(gpu, B, longest):
+    """Chains whose last hashes are missing (0), agreeing with the group's first chain up to there or less far, and the first
+    chain itself left short: missing hashes are in common with none."""
+    rng = rng_of("short", B, longest)
+    base = rng.integers(1, 2 ** 62, longest).astype(np.uint64)
+    for first_missing in (0, 1, longest // 2):
+        rows = []
+        for i in range(B):
+            r = base.copy()
+            agree = int(rng.integers(1, longest + 1))
+            r[agree:] = rng.integers(1, 2 ** 62, longest - agree).astype(np.uint64)
+            missing = first_missing if i == 0 else int(rng.integers(0, longest))
+            r[longest - missing:] = 0
+            rows.append(r)
+        check_groups(gpu, np.concatenate(rows), offsets([longest] * B), 1)
+        # two blocks, of which one agrees, and nothing else
+        short = np.zeros((B, longest), np.uint64)
+        short[:, 0] = base[0]
+        short[:, 1] = base[1] + np.arange(B, dtype=np.uint64)
+        check_groups(gpu, short.reshape(-1), offsets([longest] * B), 1)
+    assert gpu[1].device_status(reset=True) == 0
+
+
 # ------------------------------------------------------------------ tables
 
 def lengths_of(rng, B, groups, shared_most, tail_most, new_most, fresh):

@@ -21,6 +21,16 @@ def test_groups_by_hand():
     assert shared.tolist() == [2, 1, 0, 0, 0, 0, 0]
 
 
+def test_groups_missing_hashes_by_hand():
+    chains = [[1, 2, 0, 0], [1, 5, 0, 0], [1, 2, 0, 0, 0], [7, 8, 0], [7, 8, 0]]
+    flat, off = np.concatenate([np.array(c, np.uint64) for c in chains]), _off([len(c) for c in chains])
+    order, goff, shared, n = ow.prefix_groups(flat, off, 1)
+    assert order.tolist() == [0, 1, 2, 3, 4] and n == 2 and shared[:2].tolist() == [1, 2]
+    order, goff, shared, n = ow.prefix_groups(flat, off, 2)
+    assert order.tolist() == [0, 2, 1, 3, 4] and n == 3 and shared[:3].tolist() == [2, 0, 2]
+    assert ow.prefix_groups(flat, off, 3)[3] == 5
+
+
 def test_tables_by_hand():
     # request 0 holds blocks 50, 51 and gets one more token; 1 and 2 are new and share 2 blocks
     tables = np.full((3, 4), -1, np.int32)
