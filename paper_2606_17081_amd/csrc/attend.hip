@@ -292,21 +292,27 @@ struct Attend {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const uint32_t x = 64 * i + lane, r = x / NC, piece = 16 * ((x % NC) ^ turn(r));
-                k_at[i] = r * (uint32_t)p.a.ks.token * 2 + (piece < last_piece ? piece : last_piece);
-                v_at[i] = r * (uint32_t)p.a.vs.token * 2 + (piece < last_piece ? piece : last_piece);
+                k_at[i] = place(r * (uint32_t)p.a.ks.token * 2, piece);
+                v_at[i] = place(r * (uint32_t)p.a.vs.token * 2, piece);
             }
         }
     }
 
-    // The byte offset in a block of the piece that the lane loads i-th.  Pieces behind D, of rows that D does not fill, are
-    // the last one again: the query's are 0, and the results of such values are not written.
+    // The byte offset of a row's piece, or, of a piece behind D (of rows that D does not fill), one past any block's end, whose load
+    // brings zeros: the query's are 0 there, and a product with anything that is not finite would not be.
+    __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece) const
+    {
+        return piece <= last_piece ? row + piece : 0x80000000u;
+    }
+
+    // The byte offset in a block of the piece that the lane loads i-th.
     __device__ __forceinline__ uint32_t offset(const uint32_t* at, int i, int64_t token) const
     {
         if constexpr (!kEven) {
             return at[i];
         } else {
             const uint32_t piece = at[1] ^ (16 * turn((uint32_t)i * (64 / NC)));
-            return at[0] + (uint32_t)(i * (64 / NC)) * (uint32_t)token * 2 + (piece < last_piece ? piece : last_piece);
+            return place(at[0] + (uint32_t)(i * (64 / NC)) * (uint32_t)token * 2, piece);
         }
     }
 

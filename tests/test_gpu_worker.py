@@ -513,6 +513,30 @@ def test_attend_not_finite_in_later_tokens(gpu, Hq, new):
                 assert np.array_equal(np.isinf(o[:new]), np.isinf(host(out)[:new]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("D", [8, 64, 72, 80, 96, 128, 136, 192, 200, 248])
+@pytest.mark.parametrize("kv,new,Hq", [(60, 1, 2), (3000, 1, 5), (700, 40, 2), (700, 300, 8)])
+def test_attend_infinite_keys(gpu, kv, new, Hq, D, dtype):
+    """A key with an infinity among its last 8 values, at every head size: where the query's value is of the other sign the
+    score is -infinity, and the key has no weight; where it is of the same one, the row is no number."""
+    torch, rk = gpu
+    b = Batch(torch, rng_of("infinite", kv, D), [kv, 40], [new, 1], Hq, 1, D, dtype)
+    last = D - 1 - 3 * (D > 8)
+    b.q[..., last] = b.q[..., last].abs() + 0.5
+    b.q[-1, 0, last] *= -1
+    for at in (3, 30):                          # in front of every new token of the first request
+        b.caches[0][int(b.tables[0, at // BLOCK]), at % BLOCK, 0, last] = float("-inf")
+    b.caches[0][int(b.tables[1, 0]), 5, 0, last] = float("-inf")
+    a, more = b.args(rk)
+    out, lse = rk.prefix_attention(*a, want_lse=True)
+    o, l, mean, _ = b.want()
+    b.caches[0][b.caches[0].isinf()] = 0        # (the roundings of the other scores)
+    b.check(out, lse, want=(o, l, mean, b.want()[3]))
+    got = host(out)
+    assert np.isfinite(got[:new]).all() and np.isnan(got[-1, 0]).all() and np.isfinite(got[-1, 1:]).all()
+    assert rk.device_status(reset=True) == 0
+
+
 @pytest.mark.parametrize("kv,new,Hq", [(60, 1, 2), (9000, 1, 4), (700, 300, 8), (9000, 2, 64)])
 def test_attend_scores_that_are_no_numbers(gpu, kv, new, Hq):
     """A query that is NaN gives NaN, also where its parts are joined; a key that is NaN, to the tokens that see it."""
