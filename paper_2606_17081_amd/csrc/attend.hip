@@ -5,6 +5,8 @@
 // any split of the keys is joined by the same rule, o = sum_p 2^(m_p - m) o_p.  Both products run on matrix
 // instructions; m, l, o and the scores are fp32.  The w_j of a step are rounded to the cache's 16 bits, the only operands that the
 // instructions take: half a step of that type each, relative, so as much of the mean of |v| in a result (l sums them unrounded).
+// fp16's range is narrow, so there m follows each step's own scores, down as well as up (`strays`): a key of far
+// larger weight takes no bits from those after it.
 //
 // What bounds it: few rows (a decoding batch) the reading of keys and values, 4 D bytes a key and head for 4 D
 // operations a row; from some hundred rows a key head on (a prompt, or a group on its prefix) the matrix instructions.  So there are tiles of two
@@ -388,6 +390,31 @@ struct Attend {
         return q;
     }
 
+    // Whether a step whose largest score is `top` asks for another divisor than 2^m of its weights.  bf16 has fp32's range: the divisor
+    // follows only when the scores have left it behind by 2^8, so that results are seldom rescaled.  fp16 weights lose bits
+    // below 2^-14, so there a step's largest is to lie in 2^-8..2^15: what a key below 2^-14 loses is 2^-25, 2^-17 of that
+    // largest at most, and the 64 of a step 2^-11, half a step of fp16, whatever other steps hold.  Scores that rise are given 2^7, so
+    // that a row's largest weight has that at least and the 64 lose 2^-26 of it, below fp16's smallest number; scores that fall,
+    // the middle.  (With a divisor that only rises, a key of value 0 took all from 131,071 others that it stood e^18 above, and with 2^7
+    // for the largest of all, 10% at e^20.)  Scores that spread by e^3 move it seldom, by e^8 in every step: prompts of
+    // 2,500-6,000 tokens 1,114 -> 1,153 and 1,115 -> 1,226 us.
+    static __device__ __forceinline__ bool strays(float top, float m)
+    {
+        if constexpr (Half) return !(fabsf(top - m - 3.5f) <= 11.5f);
+        else return top > m + 8.0f;
+    }
+    // The new m, where the row's weights so far are `sum` in the old one's units.  Sums are kept below 2^48 or so: a key whose weight is
+    // still too small there has no part in a 16-bit result.
+    static __device__ __forceinline__ float divisor(float top, float m, float sum)
+    {
+        if constexpr (Half) {
+            if (!(top > -INFINITY && strays(top, m))) return m;
+            return top > m ? top - 7.0f : larger(top - 3.5f, m + __builtin_log2f(sum) - 48.0f);
+        } else {
+            return larger(m, top);
+        }
+    }
+
     __device__ __forceinline__ uint16_t* out_row(const Tile& t, int32_t r) const
     {
         const int32_t tok = token_of(r);
@@ -516,12 +543,10 @@ struct Attend {
                 for (int i = 0; i < 16; ++i) top = larger(top, sc[kt][i]);
             return top;
         };
-        // The weights' divisor follows the largest score only when that has left it behind by 2^8: sums
-        // and weights stay far from fp32's and fp16's ends, and the results are seldom rescaled.
         auto follow = [&](float top) {
-            if (__any(top * c > m + 8.0f)) {
+            if (__any(strays(top * c, m))) {
                 top = larger(top, __shfl_xor(top, 32)) * c;
-                const float nm = larger(m, top);
+                const float nm = divisor(top, m, Half ? l + __shfl_xor(l, 32) : 0.0f);
                 const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - nm);
                 m = nm;
                 l *= keep;
@@ -843,10 +868,15 @@ struct Attend {
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[n][kt][i]);
-                if (__any(top * c > m[n] + 8.0f)) {                      // (as for wide tiles)
+                if (__any(strays(top * c, m[n]))) {
                     top = fmaxf(top, __shfl_xor(top, 16));
                     top = fmaxf(top, __shfl_xor(top, 32)) * c;
-                    const float nm = fmaxf(m[n], top);
+                    float sum = 0.0f;
+                    if constexpr (Half) {
+                        sum = l[n] + __shfl_xor(l[n], 16);
+                        sum += __shfl_xor(sum, 32);
+                    }
+                    const float nm = divisor(top, m[n], sum);
                     const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[n] - nm);
                     m[n] = nm;
                     l[n] *= keep;

@@ -564,6 +564,42 @@ def test_attend_large_scores(gpu):
         attend(gpu, b, scale=-0.5)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("others", ["equal", "spread"])
+@pytest.mark.parametrize("kv,new,Hq,Hkv,D,shared", [
+    ([3000], [1], 4, 1, 128, 0), ([2500, 40], [4, 1], 8, 1, 80, 0), ([300] * 40, [1] * 40, 8, 8, 64, 0),
+    ([700, 900], [300, 900], 8, 2, 64, 0), ([1000], [400], 4, 1, 192, 0), ([1700] * 30, [1] * 30, 8, 2, 128, 100),
+    ([100000], [1], 2, 1, 64, 0)])
+def test_attend_one_key_far_above(gpu, kv, new, Hq, Hkv, D, shared, others, dtype):
+    """A key of value 0 (at the front, in the middle, or the token's own) that stands far above the others: what is left of
+    these is the result, to the same relative roundings, down to what the type holds at all."""
+    torch, rk = gpu
+    rng = rng_of("far above", kv, new, others)
+    B = len(kv)
+    goff, sh = (np.array([0] + [B] * B), np.array([shared] + [0] * (B - 1), np.int32)) if shared else (None, None)
+    b = Batch(torch, rng, kv, new, Hq, Hkv, D, dtype, goff=goff, shared=sh)
+    b.q.zero_()
+    b.q[..., 0] = 1.0                                       # a key's first value is its score
+    k, v = b.caches
+    k[..., 0] = torch.from_numpy(rng.normal(size=tuple(k.shape[:3]))).to(k.dtype).cuda() if others == "spread" else 0.0
+    v[:] = v * 0.3 + 1.0
+    was = k.clone(), v.clone()
+    a, more = b.args(rk)
+    for gap in (8, 10.5, 12, 14, 15, 16, 17.5, 18, 20, 25, 33, 60):
+        for place in ("front", "middle", "own"):
+            for i in range(B):
+                at = {"front": 0, "middle": kv[i] // 2, "own": kv[i] - 1}[place]
+                slot = int(b.tables[i, at // BLOCK]), at % BLOCK
+                k[slot[0], slot[1], :, 0] = gap
+                v[slot[0], slot[1]] = 0.0
+            out, lse = rk.prefix_attention(*a, **more, scale=1.0, want_lse=True)
+            if gap in (8, 16, 18, 25) or kv[0] < 100000 and B == 1:       # (the oracle takes its time)
+                b.check(out, lse, scale=1.0)
+            k.copy_(was[0])
+            v.copy_(was[1])
+    assert rk.device_status(reset=True) == 0
+
+
 def test_attend_rows_behind_and_empty_requests(gpu):
     torch, rk = gpu
     b = Batch(torch, rng_of("behind"), [0, 9, 40, 0], [0, 2, 0, 0], 4, 2, 64, rows_behind=50)
