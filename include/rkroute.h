@@ -577,7 +577,8 @@ typedef struct {
  *   k, v               [T, Hkv, D], strides k_token, k_head, v_token, v_head
  *   k_cache, v_cache   [n_blocks, 16, Hkv, D], strides ks, vs
  *   slots              int64 [T]
- * All strides are multiples of 8 elements (>= 0), pointers of 16 bytes.
+ * All strides are multiples of 8 elements (>= 0), pointers of 16 bytes.  A cache's strides lay no two heads of
+ * D values over each other: in the order of their size, each steps over all that the smaller ones span (RK_EINVAL).
  */
 int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_token, int64_t k_head, const void* v,
                 int64_t v_token, int64_t v_head, void* k_cache, rk_cache_strides ks, void* v_cache,
@@ -612,7 +613,8 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
  *   group_off, shared        as in rk_block_tables, or both NULL
  *   lse         float [T * Hq], or NULL
  *   scale       -1e18..1e18
- * Strides are multiples of 8 elements (>= 0), pointers of 16 bytes; out overlaps no input.
+ * Strides are multiples of 8 elements (>= 0), pointers of 16 bytes; out overlaps no input, nor, by its strides, itself (as the
+ * caches of rk_kv_write).
  * workspace: rk_prefix_attention_workspace_size bytes, 256-byte aligned, of any content, for this
  * call alone until it has run.
  * A request whose tokens, length or table do not fit (RK_DEV_BAD_OFFSETS;

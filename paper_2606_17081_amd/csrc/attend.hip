@@ -1772,6 +1772,8 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
                                a->vs.block, a->vs.token, a->vs.head};
     for (int64_t x : strides)
         if (x < 0 || x % 8) return fail(RK_EINVAL, "rk_prefix_attention: a stride is negative or no multiple of 8");
+    if (!rows_apart({{a->T, a->out_token}, {a->Hq, a->out_head}}, a->D))
+        return fail(RK_EINVAL, "rk_prefix_attention: out's strides lay heads or tokens over each other");
     if (a->ks.token < a->D || a->vs.token < a->D || a->ks.token >= 1 << 26 || a->vs.token >= 1 << 26)
         return fail(RK_EINVAL, "rk_prefix_attention: a cache's token stride is below D or past 2^26");
     if (!a->group_off != !a->shared)

@@ -527,6 +527,27 @@ __global__ __launch_bounds__(256) void write_kernel(int64_t T, int32_t Hkv, int3
     }
 }
 
+// Whether no two of an array's rows of D elements share one, as the strides of its dimensions tell: by size, each steps over
+// all that the smaller ones span.
+bool rows_apart(std::initializer_list<ArrayDim> dims, int32_t D)
+{
+    ArrayDim d[4];
+    int n = 0;
+    for (const ArrayDim& x : dims) {
+        if (x.n == 0) return true;
+        if (x.n == 1) continue;
+        int at = n++;
+        for (; at > 0 && d[at - 1].stride > x.stride; --at) d[at] = d[at - 1];
+        d[at] = x;
+    }
+    __int128 span = D;
+    for (int k = 0; k < n; ++k) {
+        if (d[k].stride < span) return false;
+        span += (__int128)d[k].stride * (d[k].n - 1);
+    }
+    return true;
+}
+
 }  // namespace rk
 
 using namespace rk;
@@ -586,6 +607,9 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
     const int64_t strides[] = {k_token, k_head, v_token, v_head, ks.block, ks.token, ks.head, vs.block, vs.token, vs.head};
     for (int64_t x : strides)
         if (x < 0 || x % 8) return fail(RK_EINVAL, "rk_kv_write: a stride is negative or no multiple of 8");
+    for (const rk_cache_strides& c : {ks, vs})
+        if (!rows_apart({{n_blocks, c.block}, {RK_BLOCK_TOKENS, c.token}, {Hkv, c.head}}, D))
+            return fail(RK_EINVAL, "rk_kv_write: a cache's strides lay heads, tokens or blocks over each other");
     if (T == 0) return RK_OK;
     if (!k || !v || !slots || (n_blocks > 0 && (!k_cache || !v_cache)))
         return fail(RK_EINVAL, "rk_kv_write: NULL array");

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "rkroute.h"
 
 namespace rk {
@@ -404,5 +406,11 @@ struct EpisodeLayout {
 };
 EpisodeLayout episode_layout(int32_t W, int32_t cache_blocks, int32_t max_blocks, int32_t max_conv,
                              int32_t max_routes);
+
+// A dimension of an array: how many, and how far apart, in elements.
+struct ArrayDim {
+    int64_t n, stride;
+};
+bool rows_apart(std::initializer_list<ArrayDim> dims, int32_t D);
 
 }  // namespace rk

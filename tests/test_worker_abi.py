@@ -70,6 +70,37 @@ def test_write_refusals(L):
         assert rc(**{f"_{k}": C.c_void_p(4104)}) == rk.RK_EINVAL and b"aligned" in L.rk_last_error()
 
 
+def test_write_refuses_caches_that_overlap_themselves(L):
+    def rc(s, t=None, n_blocks=7, Hkv=2, D=64):
+        # a NULL slot map is refused, but not before the strides
+        rc = L.rk_kv_write(3, Hkv, D, P, 128, 64, P, 128, 64, P, rk.CacheStrides(*s), P, rk.CacheStrides(*(t or s)), n_blocks, None, None)
+        assert rc == rk.RK_EINVAL
+        return b"over each other" in L.rk_last_error()
+
+    good = [(2048, 128, 64), (2048, 64, 1024), (4096, 128, 64), (4096, 256, 128), (1024, 64, 7 * 1024), (64, 2 * 7 * 64, 7 * 64)]
+    for s in good:
+        assert not rc(s)
+    for s in ((2048, 56, 64), (2048, 128, 56), (2048, 64, 64), (2040, 128, 64), (0, 128, 64), (2048, 0, 64), (2048, 128, 0),
+              (1024, 64, 1024), (64, 64, 64), (2048, 64, 1016)):
+        assert rc(s) and rc(good[0], s) and rc(s, good[0])
+    # of one block or one head, that stride does not matter; of no block, none does
+    assert not rc((0, 128, 64), n_blocks=1) and not rc((1024, 64, 0), Hkv=1) and not rc((0, 0, 0), n_blocks=0)
+    assert rc((0, 56, 0), n_blocks=1, Hkv=1)
+    assert not rc((1 << 62, 1 << 58, 64)) and rc((1 << 62, 1 << 59, 64))
+
+
+def test_attention_refuses_an_output_that_overlaps_itself(L):
+    def rc(token, head, **change):
+        rc = L.rk_prefix_attention(C.byref(_attention(out_token=token, out_head=head, q=None, **change)), P, 1 << 40, None)
+        assert rc == rk.RK_EINVAL                       # the NULL query, if nothing before it
+        return b"over each other" in L.rk_last_error()
+
+    assert not rc(512, 64) and not rc(64, 640) and not rc(1024, 128) and not rc(1 << 60, 64)
+    for token, head in ((0, 64), (512, 0), (504, 64), (512, 56), (64, 64), (64, 632)):
+        assert rc(token, head)
+    assert not rc(0, 64, T=1) and not rc(64, 0, Hq=1, Hkv=1)
+
+
 def _attention(**change):
     s = rk.CacheStrides(16 * 2 * 64, 2 * 64, 64)
     v = P.value
