@@ -549,9 +549,16 @@ def _heads(name, t, dims):
 
 
 def _no_gradient(what, *tensors):
+    """Refuses tensors whose gradient, or forward-mode tangent, a call would drop (None: no tensor)."""
+    torch = _found_torch or _torch()
+    forward = torch.autograd.forward_ad
     for t in tensors:
-        if t.requires_grad and _torch().is_grad_enabled():
+        if t is None:
+            continue
+        if t.requires_grad and torch.is_grad_enabled():
             raise RkError(f"{what} has no gradient: call it under torch.no_grad(), or detach its arguments")
+        if forward._current_level >= 0 and forward.unpack_dual(t).tangent is not None:
+            raise RkError(f"{what} has no forward-mode derivative: call it on the primal tensors")
 
 
 def kv_write(k, v, k_cache, v_cache, slots, stream=None):
@@ -588,7 +595,7 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
     scale defaults to D ** -0.5.  Rows behind the last request's stay as they were (in an `out` allocated here,
     uninitialised)."""
     dev = _where("q", q)
-    _no_gradient("prefix_attention", q, k_cache, v_cache)
+    _no_gradient("prefix_attention", q, k_cache, v_cache, out, lse)
     dtype, shape = _heads("q", q, 3)
     T, Hq, D = shape
     q_token, q_head = _rows("q", q, dev, dtype, shape)

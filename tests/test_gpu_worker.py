@@ -781,6 +781,34 @@ def test_binding_refuses_gradients_and_empty_heads(gpu):
     assert rk.device_status(reset=True) == 0
 
 
+def test_binding_refuses_tangents_and_outputs_that_want_a_gradient(gpu):
+    torch, rk = gpu
+    import torch.autograd.forward_ad as fw
+    b = Batch(torch, rng_of("tangent"), [40], [3], 4, 2, 64)
+    a, _ = b.args(rk)
+    slots = torch.arange(3, device="cuda")
+    new = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    k, v = a[1].clone(), a[2].clone()
+    want = rk.prefix_attention(*a)[0]
+    with fw.dual_level():
+        dual = lambda t: fw.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: rk.prefix_attention(dual(a[0]), *a[1:]), lambda: rk.prefix_attention(a[0], dual(k), *a[2:]),
+                     lambda: rk.prefix_attention(*a[:2], dual(v), *a[3:]), lambda: rk.kv_write(dual(new), new, k, v, slots),
+                     lambda: rk.kv_write(new, dual(new), k, v, slots), lambda: rk.kv_write(new, new, dual(k), v, slots)):
+            with pytest.raises(rk.RkError, match="forward-mode"):
+                call()
+            with torch.no_grad(), pytest.raises(rk.RkError, match="forward-mode"):
+                call()
+        assert torch.equal(rk.prefix_attention(*a)[0], want)
+        assert torch.equal(rk.prefix_attention(fw.unpack_dual(dual(a[0])).primal, *a[1:])[0], want)
+    out, lse = torch.zeros_like(want), torch.zeros(want.shape[:2], device="cuda")
+    for kw in (dict(out=out.clone().requires_grad_()), dict(lse=lse.clone().requires_grad_())):
+        with pytest.raises(rk.RkError, match="gradient"):
+            rk.prefix_attention(*a, **kw)
+        with torch.no_grad():
+            assert torch.equal(rk.prefix_attention(*a, **kw)[0], want)
+
+
 # ------------------------------------------------------------------ together
 
 def test_whole_steps_together(gpu):
