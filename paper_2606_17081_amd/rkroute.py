@@ -442,6 +442,12 @@ def _flat(name, t, dtype, dev, n):
     return t.data_ptr()
 
 
+def _changed(*tensors):
+    """Counts a write for autograd, to which the library's are not visible: a backward pass that saved such a tensor is to say so.
+    (None: none.)"""
+    _found_torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def prefix_groups(chains, chain_off, min_blocks: int = 1, order=None, group_off=None, shared=None, n_groups=None,
                   stream=None):
     """The batch ordered by shared prompt prefix (rk_prefix_groups): (order, group_off, shared, n_groups)."""
@@ -453,6 +459,7 @@ def prefix_groups(chains, chain_off, min_blocks: int = 1, order=None, group_off=
         if B < 0:
             raise RkError("chain_off is empty")
         at = chain_off.device
+        given = order, group_off, shared, n_groups
         if order is None:
             order = torch.empty(B, dtype=i32, device=at)
         if group_off is None:
@@ -465,6 +472,7 @@ def prefix_groups(chains, chain_off, min_blocks: int = 1, order=None, group_off=
             B, _flat("chains", chains, i64, dev, 0), _flat("chain_off", chain_off, i64, dev, 0), min_blocks,
             _flat("order", order, i32, dev, B), _flat("group_off", group_off, i64, dev, B + 1),
             _flat("shared", shared, i32, dev, B), _flat("n_groups", n_groups, i32, dev, 1), st), "rk_prefix_groups")
+        _changed(*given)
     return order, group_off, shared, n_groups
 
 
@@ -478,6 +486,7 @@ def block_tables(tables, kv_len, new_len, have, free_blocks, n_slots: int, group
         i32, i64 = torch.int32, torch.int64
         B, at = kv_len.numel(), kv_len.device
         rows, stride = _table_shape(tables, B)
+        given = tables, slots, q_off, taken
         if slots is None:
             slots = torch.empty(n_slots, dtype=i64, device=at)
         if q_off is None:
@@ -490,6 +499,7 @@ def block_tables(tables, kv_len, new_len, have, free_blocks, n_slots: int, group
             _flat("shared", shared, i32, dev, B), _flat("free_blocks", free_blocks, i32, dev, 0), free_blocks.numel(),
             _flat("tables", tables, i32, dev, 0), stride, _flat("slots", slots, i64, dev, n_slots), n_slots,
             _flat("q_off", q_off, i64, dev, B + 1), _flat("taken", taken, i32, dev, 1), st), "rk_block_tables")
+        _changed(*given)
     return tables, slots, q_off, taken
 
 
@@ -579,6 +589,7 @@ def kv_write(k, v, k_cache, v_cache, slots, stream=None):
         _check(lib().rk_kv_write(T, Hkv, D, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head,
                                  k_cache.data_ptr(), ks, v_cache.data_ptr(), vs, blocks,
                                  _flat("slots", slots, _found_torch.int64, dev, T), st), "rk_kv_write")
+        _changed(k_cache, v_cache)
 
 
 def prefix_attention_workspace_size(T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
@@ -610,6 +621,7 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
         i32, i64 = torch.int32, torch.int64
         B, at = kv_len.numel(), q.device
         _, stride = _table_shape(tables, B)
+        given = [t for t in (out, lse) if t is not None]
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=at)
             out_token, out_head = Hq * D, D
@@ -631,4 +643,6 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
             _flat("group_off", group_off, i64, dev, B + 1) or 0, _flat("shared", shared, i32, dev, B) or 0,
             out.data_ptr(), out_token, out_head, _flat("lse", lse, torch.float32, dev, T * Hq) or 0)
         _check(lib().rk_prefix_attention(a, workspace.data_ptr(), ws_bytes, st), "rk_prefix_attention")
+        if given:
+            _changed(*given)
     return out, lse

@@ -809,6 +809,37 @@ def test_binding_refuses_tangents_and_outputs_that_want_a_gradient(gpu):
             assert torch.equal(rk.prefix_attention(*a, **kw)[0], want)
 
 
+def test_binding_counts_its_writes(gpu):
+    """A backward pass that saved what a call then wrote to says so, as for any write in place."""
+    torch, rk = gpu
+    b = Batch(torch, rng_of("counts"), [40, 20], [3, 1], 4, 2, 64)
+    a, _ = b.args(rk)
+    new = torch.ones((4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    k, v = a[1].nan_to_num(), a[2].nan_to_num()
+    x = torch.ones_like(k, requires_grad=True)
+    y = (x * k).sum()
+    rk.kv_write(new, new, k, v, torch.arange(4, device="cuda"))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    out, lse = torch.empty_like(b.q), torch.empty((4, 4), device="cuda")
+    chains, off = torch.arange(1, 5, device="cuda"), torch.tensor([0, 2, 4], device="cuda")
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    i64 = lambda n: torch.zeros(n, dtype=torch.int64, device="cuda")  # noqa: E731
+    groups, tables = (i32(2), i64(3), i32(2), i32(1)), (i32(2, 4), i64(4), i64(3), i32(1))
+    written = [k, v, out, lse, *groups, *tables]
+    was = [t._version for t in written]
+    rk.kv_write(new, new, k, v, torch.arange(4, device="cuda"))
+    rk.prefix_attention(b.q, k, v, *a[3:], out=out, lse=lse)
+    rk.prefix_groups(chains, off, 1, *groups)
+    rk.block_tables(tables[0], a[4], i32(2), i32(2), i32(8), 4, None, None, *tables[1:])
+    assert [t._version for t in written] == [x + 1 for x in was]
+    with torch.inference_mode():
+        c = torch.zeros_like(k)
+        rk.kv_write(new, new, c, c.clone(), torch.arange(4, device="cuda"))
+        rk.prefix_attention(b.q, k, v, *a[3:], out=torch.empty_like(out))
+    assert rk.device_status(reset=True) == 0
+
+
 # ------------------------------------------------------------------ together
 
 def test_whole_steps_together(gpu):
