@@ -642,7 +642,13 @@ typedef struct {
     float* lse;
 } rk_attention;
 
-/* Workspace bytes for a call of these sizes on the current device (0 if they are not supported). */
+/*
+ * Workspace bytes for a call of these sizes on the current device (0 if they are not supported).
+ * 34-69 MB for parts of rows, and, with DP = D rounded up to 64, 128, 192 or 256, for rows that may share a prefix
+ *   8 (DP + 2) Hq min(T, 128 min(B, 1024) / (Hq / Hkv)) bytes
+ * (1.1 GB for 16,384 tokens of 1,024 requests on 64 / 8 heads of 128).  A call without groups (group_off NULL) needs
+ * only what T = 0 gives, which has none of these.
+ */
 size_t rk_prefix_attention_workspace_size(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
 
 int rk_prefix_attention(const rk_attention* a /* host */, void* workspace, size_t ws_bytes, void* stream);

@@ -1784,7 +1784,7 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
         return fail(RK_EINVAL, "rk_prefix_attention: NULL array");
     if (((uintptr_t)a->q | (uintptr_t)a->out | (uintptr_t)a->k_cache | (uintptr_t)a->v_cache) % 16)
         return fail(RK_EINVAL, "rk_prefix_attention: an array is not aligned to 16 bytes");
-    const AttendLayout L = attend_layout(a->T, a->B, a->Hq, a->Hkv, a->D);
+    const AttendLayout L = attend_layout(a->group_off ? a->T : 0, a->B, a->Hq, a->Hkv, a->D);       // (no groups: no rows of such)
     if (!workspace || ws_bytes < L.bytes)
         return fail(RK_ENOMEM, "rk_prefix_attention: workspace of %zu bytes, %zu needed", workspace ? ws_bytes : (size_t)0, L.bytes);
     if ((uintptr_t)workspace % 256) return fail(RK_EINVAL, "rk_prefix_attention: workspace is not aligned to 256 bytes");

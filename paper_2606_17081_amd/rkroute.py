@@ -593,6 +593,7 @@ def kv_write(k, v, k_cache, v_cache, slots, stream=None):
 
 
 def prefix_attention_workspace_size(T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
+    """Bytes of workspace for T tokens of B requests in groups; for T = 0, of any number of tokens without groups."""
     return int(lib().rk_prefix_attention_workspace_size(T, B, Hq, Hkv, D))
 
 
@@ -630,7 +631,7 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
         if lse is None and want_lse:
             lse = torch.empty((T, Hq), dtype=torch.float32, device=at)
         if workspace is None:
-            ws_bytes = prefix_attention_workspace_size(T, B, Hq, Hkv, D)
+            ws_bytes = prefix_attention_workspace_size(T if group_off is not None else 0, B, Hq, Hkv, D)
             workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=at)
         elif workspace.get_device() != dev or not workspace.is_contiguous():
             raise RkError(f"workspace must be a contiguous tensor on cuda:{dev}")

@@ -709,6 +709,30 @@ def test_attend_same_bits_each_time(gpu):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("B,new,Hq,Hkv,D", [(3, 500, 8, 2, 128), (600, 1, 4, 1, 64), (700, 5, 2, 1, 80)])
+def test_attend_without_groups_in_a_small_workspace(gpu, B, new, Hq, Hkv, D):
+    """A call without groups keeps to the workspace that T = 0 gives."""
+    torch, rk = gpu
+    rng = rng_of("small", B)
+    kv = new + rng.integers(0, 900, B)
+    b = Batch(torch, rng, kv, [new] * B, Hq, Hkv, D)
+    a, _ = b.args(rk)
+    n = rk.prefix_attention_workspace_size(0, B, Hq, Hkv, D)
+    assert n < rk.prefix_attention_workspace_size(B * new, B, Hq, Hkv, D)
+    ws = torch.full((n + 2 ** 22,), 77, dtype=torch.uint8, device="cuda")
+    out, lse = rk.prefix_attention(*a, want_lse=True, workspace=ws[:n])
+    b.check(out, lse)
+    assert (ws[n:] == 77).all()
+    with pytest.raises(rk.RkError, match="workspace"):
+        rk.prefix_attention(*a, workspace=ws[:n - 1])
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    rk.prefix_attention(*a, out=out)
+    assert torch.cuda.max_memory_allocated() - before < n + 2 ** 21
+    assert rk.device_status(reset=True) == 0
+
+
 def test_attend_two_streams_at_once(gpu):
     torch, rk = gpu
     rng = rng_of("streams")

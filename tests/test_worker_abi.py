@@ -144,6 +144,20 @@ def test_attention_refuses_a_workspace_too_small(L):
     assert L.rk_prefix_attention(C.byref(a), C.c_void_p(4096 + 16), need, None) == rk.RK_EINVAL
 
 
+def test_a_call_without_groups_needs_no_room_for_shared_rows(L):
+    size = rk.prefix_attention_workspace_size
+    least, most = size(0, 1024, 64, 8, 128), size(16384, 1024, 64, 8, 128)
+    assert 0 < least < 1 << 27 and most > 1 << 30
+    a = _attention(T=16384, B=1024, Hq=64, Hkv=8, D=128, q_head=128, out_head=128, q_token=8192, out_token=8192,
+                   ks=rk.CacheStrides(16 * 1024, 1024, 128), vs=rk.CacheStrides(16 * 1024, 1024, 128))
+    odd = C.c_void_p(4096 + 16)                           # refused for its address, but for its size before that
+    assert L.rk_prefix_attention(C.byref(a), odd, most - 1, None) == rk.RK_ENOMEM
+    assert L.rk_prefix_attention(C.byref(a), odd, most, None) == rk.RK_EINVAL
+    a.group_off = a.shared = None
+    assert L.rk_prefix_attention(C.byref(a), odd, least - 1, None) == rk.RK_ENOMEM
+    assert L.rk_prefix_attention(C.byref(a), odd, least, None) == rk.RK_EINVAL
+
+
 def test_workspace_sizes(L):
     size = rk.prefix_attention_workspace_size
     assert size(1, 4097, 8, 2, 64) == size(1, 1, 7, 2, 64) == size(1, 1, 8, 2, 60) == size(-1, 1, 8, 2, 64) == 0
