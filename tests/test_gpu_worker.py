@@ -473,6 +473,27 @@ def test_attend_many_requests(gpu):
     assert gpu[1].device_status(reset=True) == 0
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,D,dtype", [
+    (512, 4, 1, 128, "bf16"), (513, 4, 1, 128, "bf16"), (513, 2, 2, 72, "fp16"), (1024, 2, 1, 128, "fp16"), (1024, 2, 1, 192, "bf16"),
+    (1024, 1, 1, 256, "fp16"), (1025, 2, 1, 256, "bf16"), (700, 3, 1, 200, "bf16")])
+def test_attend_many_requests_of_wide_heads(gpu, B, Hq, Hkv, D, dtype):
+    """On both sides of where what is kept of the requests leaves room for one workgroup a CU, and of a launch's most requests;
+    prompts, single tokens and empty requests, with a group and without."""
+    rng = rng_of("wide heads", B, D)
+    kv = rng.integers(1, 70, B)
+    new = np.where(rng.random(B) < 0.1, kv, np.minimum(1, kv))
+    new[rng.random(B) < 0.05] = 0
+    kv[5] = new[5] = 300
+    attend(gpu, Batch(gpu[0], rng, kv, new, Hq, Hkv, D, dtype))
+    sizes = [B // 2, 3, B - B // 2 - 3]
+    goff = np.concatenate([offsets(sizes), np.full(B - 3, B)]).astype(np.int64)
+    sh = np.zeros(B, np.int32)
+    sh[:3] = 30, 5, 2
+    kv = BLOCK * np.repeat(sh[:3], sizes) + rng.integers(1, 20, B)
+    attend(gpu, Batch(gpu[0], rng, kv, np.ones(B, np.int64), Hq, Hkv, D, dtype, goff=goff, shared=sh))
+    assert gpu[1].device_status(reset=True) == 0
+
+
 def test_attend_long(gpu):
     """Long sequences, cut over many workgroups."""
     rng = rng_of("long")
@@ -511,6 +532,31 @@ def test_attend_not_finite_in_later_tokens(gpu, Hq, new):
             if which:                                                # values: the weights stay what they are
                 assert np.array_equal(np.isnan(o[:new]), np.isnan(host(out)[:new]))
                 assert np.array_equal(np.isinf(o[:new]), np.isinf(host(out)[:new]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 80, 128, 192, 256])
+@pytest.mark.parametrize("Hq,new", [(1, 12), (3, 9), (8, 40), (5, 70)])
+def test_attend_not_finite_at_every_head_size(gpu, Hq, new, D, dtype):
+    """Keys and values that are not finite, in several tokens, heads' places and signs, on narrow tiles of one and two row
+    blocks and wide ones: every row within check()'s bounds, its infinities of the right sign, its log-sum-exp too."""
+    torch, rk = gpu
+    rng = rng_of("not finite", Hq, new, D)
+    kv = [new + 100, 90]
+    for which in (0, 1):
+        b = Batch(torch, rng, kv, [new, 1], Hq, 1, D, dtype, garbage=float("nan"))
+        for value in (float("inf"), float("-inf"), float("nan")):
+            for at in rng.integers(100, 100 + new, 3):              # a new token's own
+                piece = int(rng.integers(0, D // 8)), int(rng.integers(0, 8))
+                slot = int(b.tables[0, at // BLOCK]), int(at % BLOCK)
+                if which:
+                    b.caches[1][slot[0], slot[1], 0, 8 * piece[0] + piece[1]] = value
+                elif at >= 100 + new // 2:                          # so that there are rows without
+                    b.caches[0][slot[0], slot[1], 0, 8 * piece[0] + piece[1]] = value
+        a, _ = b.args(rk)
+        out, lse = rk.prefix_attention(*a, want_lse=True)
+        b.check(out, lse)
+    assert rk.device_status(reset=True) == 0
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
