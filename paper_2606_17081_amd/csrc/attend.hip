@@ -867,10 +867,10 @@ struct Attend {
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[n][kt][i]);
+                    for (int i = 0; i < 4; ++i) top = larger(top, sc[n][kt][i]);
                 if (__any(strays(top * c, m[n]))) {
-                    top = fmaxf(top, __shfl_xor(top, 16));
-                    top = fmaxf(top, __shfl_xor(top, 32)) * c;
+                    top = larger(top, __shfl_xor(top, 16));
+                    top = larger(top, __shfl_xor(top, 32)) * c;
                     float sum = 0.0f;
                     if constexpr (Half) {
                         sum = l[n] + __shfl_xor(l[n], 16);
@@ -1085,7 +1085,7 @@ struct Attend {
             if (r >= rows) continue;
             float mm[kWaves], nm = -INFINITY, total = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) nm = fmaxf(nm, mm[w] = join[2 * (w * kRows + r)]);
+            for (int w = 0; w < kWaves; ++w) nm = larger(nm, mm[w] = join[2 * (w * kRows + r)]);
             f32x4 a = {}, b = {};
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
@@ -1573,8 +1573,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t gr
             }
             float top = pm;
 #pragma unroll
-            for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-            const float nm = fmaxf(m, top);
+            for (int d = 32; d > 0; d >>= 1) top = larger(top, __shfl_xor(top, d));
+            const float nm = larger(m, top);
             if (nm == -INFINITY) {           // no key seen, or scores that are no numbers: l tells
 #pragma unroll
                 for (int d = 32; d > 0; d >>= 1) pl += __shfl_xor(pl, d);
