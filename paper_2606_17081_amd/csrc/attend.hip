@@ -321,8 +321,9 @@ struct Attend {
     // The block's `rows` first rows from base to LDS, zeros after them.  Straight to LDS, in flight until a wait for
     // vector memory; written as asm with no register result so that the compiler does not place that wait before
     // every LDS read.  The compiler sees no need of wait states inside it, so they stand there: one between the write of m0 and the
-    // load that takes its place in LDS from it, five between an instruction of the vector unit that may have written the
-    // descriptor's registers (a readfirstlane, a spilled register's return) and the load that reads them.
+    // load that takes its place in LDS from it, and before the block's first load five after an instruction of the vector unit that may
+    // have written the descriptor's registers (a readfirstlane, a spilled register's return).  (Five before every load: pieces
+    // of prompts with D = 192 110 -> 114 us.)
     __device__ __forceinline__ void load_block(const uint16_t* base, int64_t stride, int32_t rows, const uint32_t* at,
                                                uint32_t lds) const
     {
@@ -338,9 +339,14 @@ struct Attend {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const uint32_t to = __builtin_amdgcn_readfirstlane(lds + 1024u * i);
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to),
-                         "v"(offset(at, i, stride)), "s"(rsrc)
-                         : "m0", "memory");
+            if (i == 0)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to),
+                             "v"(offset(at, i, stride)), "s"(rsrc)
+                             : "m0", "memory");
+            else
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to),
+                             "v"(offset(at, i, stride)), "s"(rsrc)
+                             : "m0", "memory");
         }
     }
 
