@@ -612,7 +612,8 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
  *   q_off       int64 [B+1]  tokens of q of each request
  *   group_off, shared        as in rk_block_tables, or both NULL
  *   lse         float [T * Hq], or NULL
- *   scale       -1e18..1e18
+ *   scale       -1e18..1e18; scores |scale q . k| past 2^23 have too few bits in fp32 for their differences, and may
+ *               end as no number
  * Strides are multiples of 8 elements (>= 0), pointers of 16 bytes; out overlaps no input, nor, by its strides, itself (as the
  * caches of rk_kv_write).
  * workspace: rk_prefix_attention_workspace_size bytes, 256-byte aligned, of any content, for this

@@ -611,6 +611,34 @@ def test_attend_large_scores(gpu):
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("kv,new,Hq", [(70, 1, 2), (3000, 1, 4), (500, 300, 4), (8100, 2, 64)])
+def test_attend_scores_in_the_millions(gpu, kv, new, Hq, dtype):
+    """Scores up to the documented 2^23, thousands apart: each row is the value of its largest."""
+    torch, rk = gpu
+    rng = rng_of("millions", kv, new)
+    b = Batch(torch, rng, [kv], [new], Hq, 1, 64, dtype)
+    b.q.zero_()
+    b.q[..., 0] = 2048.0
+    k, v = b.caches
+    score = np.concatenate([rng.permutation(kv - new), np.arange(kv - new, kv)])      # a new token's own is its largest
+    at = np.arange(kv)
+    block = torch.from_numpy(b.tables[0][at // BLOCK].astype(np.int64)).cuda()
+    coarse, fine = score // 64, score % 64                      # scores are 2^16 * coarse + 2^10 * fine, exactly
+    k[block, at % BLOCK] = 0.0
+    b.q[..., 1] = 32.0
+    k[block, at % BLOCK, 0, 0] = torch.from_numpy(coarse * 32.0).to(k.dtype).cuda()
+    k[block, at % BLOCK, 0, 1] = torch.from_numpy(fine * 32.0).to(k.dtype).cuda()
+    a, _ = b.args(rk)
+    assert score.max() * 2 ** 10 < 2 ** 23
+    out, lse = rk.prefix_attention(*a, scale=1.0, want_lse=True)
+    want = host(v[block, at % BLOCK, 0])[kv - new:]
+    assert np.abs(host(out) - want[:, None]).max() <= 2 * STEP[dtype] * np.abs(want).max()
+    top = score[kv - new:] * 2.0 ** 10
+    assert np.abs(host(lse) - top[:, None]).max() <= 4 * 2.0 ** -24 * top.max()
+    assert rk.device_status(reset=True) == 0
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("others", ["equal", "spread"])
 @pytest.mark.parametrize("kv,new,Hq,Hkv,D,shared", [
     ([3000], [1], 4, 1, 128, 0), ([2500, 40], [4, 1], 8, 1, 80, 0), ([300] * 40, [1] * 40, 8, 8, 64, 0),
