@@ -592,9 +592,9 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
  *   out[t, h] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q[t, h] . k_j)
  *   lse[t, h] = log sum_j w_j
  * with sums and softmax statistics in fp32 and the w_j of a tile rounded to the cache's type for
- * the product with the values: half a step of it, relative; with RK_F16 also 2^-17 of the largest
- * of the 64 positions (or 32) that are worked on together, and 2^-26 of the row's largest for all of them, where a
- * w_j is small against these.  With groups, the first lead entries (as in
+ * the product with the values: half a step of it, relative; with RK_F16 the small ones of the 64
+ * positions (or 32) that are worked on together lose at most 2^-11 of the largest of these between them, and 2^-26 of
+ * the row's largest.  With groups, the first lead entries (as in
  * rk_block_tables) of a group's rows are the same blocks, and where that is the faster way
  * the group's rows attend to them together, read through the row of one of them.
  * No key or value past a token's position has a part in its result, whatever

@@ -10,8 +10,9 @@
 //
 // What bounds it: few rows (a decoding batch) the reading of keys and values, 4 D bytes a key and head for 4 D
 // operations a row; from some hundred rows a key head on (a prompt, or a group on its prefix) the matrix instructions.  So there are tiles of two
-// shapes, wide and narrow, and solo ones for what is short.  128 requests on one prefix of 8,192 tokens (64 / 8 heads of 128):
-// 70 + 10 us; prompts of 2,500-6,000 tokens: 1.15-1.26 ms, 860-940 TFLOP/s; 5 requests of 60,000-131,072 tokens: 198 us, 5.1 TB/s.
+// shapes, wide and narrow, and solo ones for what is short.  Kernels in a trace, the same inputs over and over: 128 requests on
+// one prefix of 8,192 tokens (64 / 8 heads of 128) 66 + 10 us; prompts of 2,500-6,000 tokens 1.15-1.26 ms, 860-940 TFLOP/s;
+// 5 requests of 60,000-131,072 tokens 193-199 us, 5.1 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -442,9 +443,9 @@ struct Attend {
     //
     // Bound by nothing alone: at D = 128 the two wavefronts of a SIMD have 2,048 cycles of matrix instructions a step, their CU's eight
     // 2,048 of LDS reads (32 KB each at 128 B a cycle), and 1,600 of vector instructions, two thirds of them for exponentials and
-    // sums; on whole prompts the matrix units are busy 43% of the time.  Rows of 64 a wavefront would halve the LDS
+    // sums; on whole prompts the matrix units are busy for 43-52% of the cycles.  Rows of 64 a wavefront would halve the LDS
     // reads, but need 300 registers of the 256 that two wavefronts a SIMD have; one a SIMD (as for D > 128) reaches
-    // half the rate: pieces of prompts with D = 192, 104 us for 52 GFLOP.  Conflicts of LDS banks are rare.
+    // half the rate: pieces of prompts with D = 192, 107 us for 52 GFLOP.  Conflicts of LDS banks are rare.
     // One prompt of 8,192 tokens, 64 / 8 heads of 128: 1.12 ms, 975 TFLOP/s.
     __device__ void wide(const Tile& t)
     {
@@ -788,7 +789,7 @@ struct Attend {
     // follow as soon as this step's are in registers.  The wavefronts' results are joined through LDS; of few keys a
     // wavefront does a tile alone.  Measured: 5 requests of 60,000-131,072 tokens, 16 / 4 heads of 128, 198 us for 1.01 GB, 5.1 TB/s; 128 of
     // 2,048 tokens, 8 key heads, 215 us, 5.0 TB/s; one of 8,192 tokens 21 us, of 100 tokens 12 us, both waits one after the
-    // other (lengths, block numbers, keys, join).
+    // other (lengths, block numbers, keys, join).  (Kernels in a trace.)
     template <int NQ, bool Solo>
     __device__ void narrow(const Tile& t)
     {
@@ -1452,10 +1453,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             const int32_t broken = req[m.first].base, f = m.first + (broken & 1);
             if (m.end - f < 2 || (broken & 2) || (broken & (broken & 1 ? 8 : 4)) || i < f) continue;
             // Together where that costs less along the line than each member's own steps over the prefix, a join a member
-            // counted; and only if most members have fewer rows than a wide tile (what the workspace holds).  128 requests on
-            // 8,192 tokens: 80 us together, 507 us each for itself; 200 of 24 groups 62 and 129; pieces of prompts in 3 groups, of 350
-            // tokens each, 117 and 116 (there the matrix instructions bound both); 533 requests that share 5 blocks stay apart, for 141 us, 134
-            // when no groups are named.
+            // counted; and only if most members have fewer rows than a wide tile (what the workspace holds).  Calls one after the
+            // other on the same inputs: 128 requests on 8,192 tokens 80 us together, 507 us each for itself; 200 of 24 groups 62 and 129;
+            // pieces of prompts in 3 groups, of 350 tokens each, 117 and 116 (there the matrix instructions bound both); 533 requests that
+            // share 5 blocks stay apart, for 141 us, 134 when no groups are named.
             const int64_t n = m.end - f, tokens = req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0, rows = tokens * G;
             if (rows == 0 || rows >= kWideRows * n) continue;
             const Segment sg = prefix_segment((int32_t)tokens, m.lent, p);

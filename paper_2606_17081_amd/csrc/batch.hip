@@ -34,8 +34,8 @@ __device__ __forceinline__ int64_t group_incl_sum(int64_t v, int64_t* tmp)
 // request's key (its hash at block min_blocks - 1) is entered with the lowest
 // request number that has it; the requests that are their key's lowest number
 // the groups, by a population count over 64-request masks; a counting sort by
-// group number, 6 bits a pass, gives the stable order.  32 requests: 10 us, 4,096 of 256 groups: 18.5 us and
-// 4.9 us for their common blocks; some ten waits for loads, LDS and the other wavefronts one after the other.
+// group number, 6 bits a pass, gives the stable order.  32 requests: 10 us, 4,096 of 256 groups: 18.8 us and
+// 5.3 us for their common blocks; some ten waits for loads, LDS and the other wavefronts one after the other.
 constexpr int kGroupSlots = 2 * kBatchMax;
 // Batches up to this are done in one launch, their common blocks by this workgroup, 64 requests at a time: calls of 64 and 128
 // requests 11.4 and 12.4 us (14.0 and 13.7 by two launches), of 192 and 512 14.1 and 20.9 us (13.8 and 14.8).
