@@ -517,7 +517,7 @@ int rk_poa_estimate_noalloc(int32_t n_windows, const int64_t* win_off, int32_t n
  *                             can be handed on without their number
  *   shared      int32 [B]     shared_g, 0 from the last group on
  *   n_groups    int32 [1]
- * A hash of 0 is a missing one (rk_hash_chains leaves the end of a chain so whose
+ * A hash of 0 is a missing one (rk_hash_chains leaves 0 at the end of a chain whose
  * tokens were too few) and in common with none.  At block min_blocks - 1 it
  * names no prefix: RK_DEV_ZERO_KEY, the request is a group of its own.
  */
@@ -598,8 +598,9 @@ int rk_kv_write(int64_t T, int32_t Hkv, int32_t D, const void* k, int64_t k_toke
  * rk_block_tables) of a group's rows are the same blocks, and where that is the faster way
  * the group's rows attend to them together, read through the row of one of them.
  * No key or value past a token's position has a part in its result, whatever
- * it holds; the tokens of q behind q_off[B] are not read, and their rows of out and lse stay
- * as they were.
+ * it holds.  A value that is not finite at a position that the token sees makes its result infinite or no
+ * number (perhaps not, where the weight is too small for fp32 or the type).  The tokens of q behind
+ * q_off[B] are not read, and their rows of out and lse stay as they were.
  *   B           requests, 0..RK_MAX_BATCH;  T  tokens that q and out hold
  *   Hq, Hkv     query and key heads, Hq a multiple of Hkv, at most 128 per key head
  *   D           values of a head, a multiple of 8, 8..256
