@@ -655,6 +655,70 @@ size_t rk_prefix_attention_workspace_size(int64_t T, int32_t B, int32_t Hq, int3
 
 int rk_prefix_attention(const rk_attention* a /* host */, void* workspace, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------- a worker's cache in 4 bits
+ * The same cache of 4.25 bits a value, so that a worker keeps 3.76 times the blocks in the same memory and a
+ * decoding batch reads as much less.  rk_prefix_groups and rk_block_tables serve it as they are;
+ *   rk_kv_write_fp4          the new tokens' keys and values into the cache
+ *   rk_kv_read_fp4           tokens of the cache as 16-bit values
+ *   rk_prefix_attention_fp4  the new tokens' attention
+ * take the places of rk_kv_write and rk_prefix_attention; all may be captured into a graph.
+ * Values 32 g .. 32 g + 31 of a head (those of them below D) share a byte s, their scale, and each has a code of 4
+ * bits: a sign and one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7, the sign 8 more).  The value held
+ * is magnitude * 2^(s - 127); with s = 255 all of them are no numbers.  (This is the MXFP4 of the OCP
+ * Microscaling formats: e2m1 elements, e8m0 scales.)
+ * With C = ceil(D / 32), a head's row is 16 C bytes of codes, value 2 i in the low half of byte i, and C bytes of
+ * scales.  What the codes behind D are has no effect.
+ */
+typedef struct {
+    void* codes;              /* uint8 [n_blocks, 16, Hkv, 16 C], aligned to 16 bytes   */
+    rk_cache_strides cs;      /* in bytes, multiples of 16                              */
+    void* scales;             /* uint8 [n_blocks, 16, Hkv, C]                           */
+    rk_cache_strides ss;      /* in bytes                                               */
+} rk_fp4_cache;
+
+/*
+ * rk_kv_write_fp4 -- keys and values of new tokens into a cache in 4 bits.
+ * As rk_kv_write; a group of 32 values whose largest magnitude is a gets the scale s = e + 127, e the least whole
+ * number with a <= 7 * 2^e, and each value the code whose magnitude is nearest to |x| / 2^e, of two the one with the
+ * even code, 6 for all above it.  e is kept within -125..125 for RK_BF16 and -23..13 for RK_F16, so that every value held is
+ * one of the type (and in bf16 no subnormal one); beyond, magnitudes are held as 6 * 2^125 and 49,152, small ones as 0.
+ * A group with a value that is not finite gets s = 255 and codes of 0.  Missing values behind D count, and are held, as 0.
+ * Nothing of the cache but the rows of the slots is read or written.
+ *   T, Hkv, D, k, v, strides, slots   as of rk_kv_write;  dtype  RK_BF16 or RK_F16, of k and v
+ *   k_cache, v_cache   (host) the caches; neither's strides lay two heads' codes, or scales, over each other (RK_EINVAL)
+ */
+int rk_kv_write_fp4(int64_t T, int32_t Hkv, int32_t D, int32_t dtype, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                    int64_t v_token, int64_t v_head, const rk_fp4_cache* k_cache, const rk_fp4_cache* v_cache, int32_t n_blocks,
+                    const int64_t* slots, void* stream);
+
+/*
+ * rk_kv_read_fp4 -- tokens of a cache in 4 bits as 16-bit values.
+ * Row t of k and v gets what the cache holds at slots[t] (a slot may come more than once), rounded to the type: no rounding of
+ * what rk_kv_write_fp4 put there from the same type; bf16's range holds all scales up to 252, beyond it and fp16's values
+ * become infinite.  Rows of negative slots become 0, and those of slots past n_blocks too (RK_DEV_BAD_BLOCK).
+ *   k, v   [T, Hkv, D], strides k_token, k_head, v_token, v_head: multiples of 8 elements (>= 0), pointers of 16 bytes, no two
+ *          rows over each other (RK_EINVAL)
+ */
+int rk_kv_read_fp4(int64_t T, int32_t Hkv, int32_t D, int32_t dtype, const rk_fp4_cache* k_cache, const rk_fp4_cache* v_cache,
+                   int32_t n_blocks, const int64_t* slots, void* k, int64_t k_token, int64_t k_head, void* v, int64_t v_token,
+                   int64_t v_head, void* stream);
+
+/*
+ * rk_prefix_attention_fp4 -- attention of a step's new tokens over a cache in 4 bits.
+ * As rk_prefix_attention in everything, k_j and v_j being the values held, as rk_kv_read_fp4 gives them in the type of q.
+ *   a      as of rk_prefix_attention; its k_cache, ks, v_cache and vs are not read
+ *   k, v   the caches; their token strides at least a row's bytes and < 2^26
+ */
+typedef struct {
+    rk_attention a;
+    rk_fp4_cache k, v;
+} rk_attention_fp4;
+
+/* Workspace bytes, as of rk_prefix_attention_workspace_size. */
+size_t rk_prefix_attention_fp4_workspace_size(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
+
+int rk_prefix_attention_fp4(const rk_attention_fp4* a /* host */, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

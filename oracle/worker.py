@@ -117,3 +117,39 @@ def attention(q, k_cache, v_cache, tables, kv_len, q_off, scale=None):
                     lse[rows, heads] = np.where(none[..., 0], -np.inf, top[..., 0] + np.log(np.where(none, 1, total)[..., 0]))
                     most[rows, heads] = np.where(see[:, None, :], abs(scale) * (np.abs(x) @ np.abs(kk).T), 0).max(-1, initial=0)
     return out, lse, mean, most
+
+
+# ------------------------------------------------------------------ a cache in 4 bits
+
+SHARE = 32
+MAGNITUDES = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+EXPONENTS = {"bf16": (-125, 125), "fp16": (-23, 13)}
+
+
+def fp4_encode(x, dtype):
+    """(codes uint8 [..., 16 C], scales uint8 [..., C]) of values [..., D] in 64 bits: of each group of 32 the least power of
+    two that 7 times holds the largest, and of each value the nearest magnitude, of two the one with the even code."""
+    D = x.shape[-1]
+    C = -(-D // SHARE)
+    x = np.concatenate([np.asarray(x, np.float64), np.zeros((*x.shape[:-1], C * SHARE - D))], -1).reshape(*x.shape[:-1], C, SHARE)
+    good = np.isfinite(x).all(-1)
+    top = np.where(good, np.abs(np.where(np.isfinite(x), x, 0)).max(-1), 0)
+    lo, hi = EXPONENTS[dtype]
+    e = np.full(top.shape, hi)
+    for k in range(hi - 1, lo - 1, -1):
+        e = np.where(top <= 7 * 2.0 ** k, k, e)
+    y = np.abs(np.where(np.isfinite(x), x, 0)) / 2.0 ** e[..., None]
+    far = np.abs(y[..., None] - MAGNITUDES)
+    nearest = far == far.min(-1, keepdims=True)
+    even = nearest & (np.arange(8) % 2 == 0)
+    code = np.where(even.any(-1), even.argmax(-1), nearest.argmax(-1)) + 8 * np.signbit(x)
+    code = np.where(good[..., None], code, 0).reshape(*x.shape[:-2], C * SHARE).astype(np.uint8)
+    return code[..., ::2] | code[..., 1::2] << 4, np.where(good, e + 127, 255).astype(np.uint8)
+
+
+def fp4_decode(codes, scales, D):
+    """The values [..., D] held, in 64 bits."""
+    code = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], 2 * codes.shape[-1])
+    x = np.where(code & 8, -1.0, 1.0) * MAGNITUDES[code & 7]
+    power = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return (x * np.repeat(power, SHARE, -1))[..., :D]

@@ -1,0 +1,193 @@
+// fp4.hip -- a block cache held in 4 bits: writes and reads.
+//
+// 32 neighbouring values of a head (the last of D may be fewer) share a power of two, of which each is a multiple by 0, 0.5, 1,
+// 1.5, 2, 3, 4 or 6 and a sign.  With a the largest of them in magnitude and e the least whole number with a <= 7 2^e,
+// a value is off by at most half the distance of its neighbours on that grid, or by a - 6 2^e <= 2^e.  Everything is exact but the one rounding to
+// that grid, so what the cache holds follows from the values alone.
+#include <hip/hip_runtime.h>
+
+#include "rk_internal.h"
+
+namespace rk {
+
+// The bytes of the powers that a type's caches use: with them all values are the type's own, none of them subnormal in bf16
+// (8 bits of exponent hold 2^-126 and more), none of them past its range.
+template <bool Half>
+constexpr int32_t kLeastPower = Half ? 127 - 23 : 127 - 125;
+template <bool Half>
+constexpr int32_t kMostPower = Half ? 127 + 13 : 127 + 125;
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// The codes of eight values, the first's in the lowest bits.
+template <bool Half>
+__device__ __forceinline__ uint32_t fp4_codes(u32x4 x, float scale)
+{
+    const uint32_t a = x.x, b = x.y, c = x.z, d = x.w;       // (a bit_cast takes no vector's element)
+    uint32_t codes = 0;
+    if constexpr (Half) {
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, __builtin_bit_cast(f16x2, a), scale, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, __builtin_bit_cast(f16x2, b), scale, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, __builtin_bit_cast(f16x2, c), scale, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, __builtin_bit_cast(f16x2, d), scale, 3);
+    } else {
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, a), scale, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, b), scale, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, c), scale, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, d), scale, 3);
+    }
+    return codes;
+}
+
+// Four lanes a group of 32 values, 8 each: whole rows are read and written.  blockIdx.y: keys or values.
+template <bool Half>
+__global__ __launch_bounds__(256) void write_fp4_kernel(int64_t T, int32_t Hkv, int32_t D, const uint16_t* __restrict__ k,
+                                                        int64_t k_token, int64_t k_head, const uint16_t* __restrict__ v,
+                                                        int64_t v_token, int64_t v_head, rk_fp4_cache kc, rk_fp4_cache vc,
+                                                        int32_t n_blocks, const int64_t* __restrict__ slots, int32_t* status)
+{
+    const bool values = blockIdx.y != 0;
+    const uint16_t* __restrict__ src = values ? v : k;
+    const rk_fp4_cache c = values ? vc : kc;
+    const int64_t s_token = values ? v_token : k_token, s_head = values ? v_head : k_head;
+    const uint32_t pieces = ((uint32_t)D + 31) / 32 * 4, per = (uint32_t)Hkv * pieces;       // of a row, of a token
+    const int64_t n = T * per;
+    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
+        const int64_t t = x / per;
+        const uint32_t r = (uint32_t)(x - t * per), h = r / pieces, piece = r - h * pieces;
+        const int64_t slot = slots[t];
+        if (slot < 0) continue;
+        const int64_t block = slot / RK_BLOCK_TOKENS, tok = slot % RK_BLOCK_TOKENS;
+        if (block >= n_blocks) {
+            if (r == 0) atomicOr(status, RK_DEV_BAD_BLOCK);
+            continue;
+        }
+        u32x4 val = {0u, 0u, 0u, 0u};
+        if (8 * piece < (uint32_t)D) val = *reinterpret_cast<const u32x4*>(src + t * s_token + h * s_head + 8 * piece);
+        // the largest magnitude, by its bits
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, val[i] & 0x7fff7fffu));
+        uint32_t top = most.x > most.y ? most.x : most.y;
+#pragma unroll
+        for (int d = 1; d < 4; d <<= 1) {
+            const uint32_t other = __shfl_xor(top, d);
+            top = top > other ? top : other;
+        }
+        const bool finite = top < (Half ? 0x7c00u : 0x7f80u);
+        const uint32_t bits = __float_as_uint(Half ? (float)__builtin_bit_cast(_Float16, (uint16_t)top) : __uint_as_float(top << 16));
+        int32_t power = (int32_t)((bits + 0x1fffffu) >> 23) - 2;     // 1.75 2^n or less: 2^(n-2), else 2^(n-1)
+        power = power < kLeastPower<Half> ? kLeastPower<Half> : power > kMostPower<Half> ? kMostPower<Half> : power;
+        const float scale = __uint_as_float((uint32_t)power << 23);
+        const uint32_t codes = fp4_codes<Half>(val, scale);
+        *reinterpret_cast<uint32_t*>((uint8_t*)c.codes + block * c.cs.block + tok * c.cs.token + h * c.cs.head + 4 * piece) =
+            finite ? codes : 0u;
+        if (piece % 4 == 0)
+            ((uint8_t*)c.scales)[block * c.ss.block + tok * c.ss.token + h * c.ss.head + piece / 4] = finite ? (uint8_t)power : 255;
+    }
+}
+
+// The reverse, with a thread for 8 values too.
+template <bool Half>
+__global__ __launch_bounds__(256) void read_fp4_kernel(int64_t T, int32_t Hkv, int32_t D8, uint16_t* __restrict__ k,
+                                                       int64_t k_token, int64_t k_head, uint16_t* __restrict__ v,
+                                                       int64_t v_token, int64_t v_head, rk_fp4_cache kc, rk_fp4_cache vc,
+                                                       int32_t n_blocks, const int64_t* __restrict__ slots, int32_t* status)
+{
+    const bool values = blockIdx.y != 0;
+    uint16_t* __restrict__ dst = values ? v : k;
+    const rk_fp4_cache c = values ? vc : kc;
+    const int64_t d_token = values ? v_token : k_token, d_head = values ? v_head : k_head;
+    const uint32_t per = (uint32_t)Hkv * (uint32_t)D8;
+    const int64_t n = T * per;
+    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
+        const int64_t t = x / per;
+        const uint32_t r = (uint32_t)(x - t * per), h = r / (uint32_t)D8, piece = r - h * (uint32_t)D8;
+        const int64_t slot = slots[t], block = slot / RK_BLOCK_TOKENS, tok = slot % RK_BLOCK_TOKENS;
+        u32x4 val = {0u, 0u, 0u, 0u};
+        if (slot >= 0 && block < n_blocks) {
+            const uint32_t codes = *reinterpret_cast<const uint32_t*>((const uint8_t*)c.codes + block * c.cs.block +
+                                                                      tok * c.cs.token + h * c.cs.head + 4 * piece);
+            const uint8_t power = ((const uint8_t*)c.scales)[block * c.ss.block + tok * c.ss.token + h * c.ss.head + piece / 4];
+            val = fp4_values<Half>(codes, __uint_as_float((uint32_t)power << 23));
+        } else if (slot >= 0 && r == 0) {
+            atomicOr(status, RK_DEV_BAD_BLOCK);
+        }
+        *reinterpret_cast<u32x4*>(dst + t * d_token + h * d_head + 8 * piece) = val;
+    }
+}
+
+// What the two entry points refuse alike: `k` and `v` are the tokens' rows, [T, Hkv, D].
+static int tokens_arguments(const char* name, int64_t T, int32_t Hkv, int32_t D, int32_t dtype, const void* k, int64_t k_token,
+                            int64_t k_head, const void* v, int64_t v_token, int64_t v_head, const rk_fp4_cache* kc,
+                            const rk_fp4_cache* vc, int32_t n_blocks, const int64_t* slots)
+{
+    if (T < 0 || n_blocks < 0) return fail(RK_EINVAL, "%s: a negative size", name);
+    if (Hkv < 1 || Hkv > 1024) return fail(RK_EUNSUPPORTED, "%s: Hkv outside 1..1024", name);
+    if (D < 8 || D > 256 || D % 8) return fail(RK_EUNSUPPORTED, "%s: D is no multiple of 8 in 8..256", name);
+    if (dtype != RK_BF16 && dtype != RK_F16) return fail(RK_EUNSUPPORTED, "%s: dtype %d", name, dtype);
+    if (!kc || !vc) return fail(RK_EINVAL, "%s: NULL cache", name);
+    for (int64_t x : {k_token, k_head, v_token, v_head})
+        if (x < 0 || x % 8) return fail(RK_EINVAL, "%s: a stride is negative or no multiple of 8", name);
+    for (const rk_fp4_cache& c : {*kc, *vc})
+        if (!fp4_strides(c)) return fail(RK_EINVAL, "%s: a stride is negative, or one of codes no multiple of 16", name);
+    if (T == 0) return RK_OK;
+    if (!k || !v || !slots || (n_blocks > 0 && (!kc->codes || !kc->scales || !vc->codes || !vc->scales)))
+        return fail(RK_EINVAL, "%s: NULL array", name);
+    if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)kc->codes | (uintptr_t)vc->codes) % 16)
+        return fail(RK_EINVAL, "%s: an array is not aligned to 16 bytes", name);
+    return RK_OK;
+}
+
+}  // namespace rk
+
+using namespace rk;
+
+extern "C" {
+
+int rk_kv_write_fp4(int64_t T, int32_t Hkv, int32_t D, int32_t dtype, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                    int64_t v_token, int64_t v_head, const rk_fp4_cache* k_cache, const rk_fp4_cache* v_cache, int32_t n_blocks,
+                    const int64_t* slots, void* stream)
+{
+    const char* name = "rk_kv_write_fp4";
+    if (int rc = tokens_arguments(name, T, Hkv, D, dtype, k, k_token, k_head, v, v_token, v_head, k_cache, v_cache, n_blocks, slots))
+        return rc;
+    const int32_t shares = (D + 31) / 32;
+    for (const rk_fp4_cache& c : {*k_cache, *v_cache})
+        if (!rows_apart({{n_blocks, c.cs.block}, {RK_BLOCK_TOKENS, c.cs.token}, {Hkv, c.cs.head}}, 16 * shares) ||
+            !rows_apart({{n_blocks, c.ss.block}, {RK_BLOCK_TOKENS, c.ss.token}, {Hkv, c.ss.head}}, shares))
+            return fail(RK_EINVAL, "%s: a cache's strides lay heads, tokens or blocks over each other", name);
+    if (T == 0) return RK_OK;
+    int32_t* st = status_word();
+    if (!st) return fail(RK_EHIP, "%s: no status word", name);
+    int64_t blocks = (T * Hkv * shares * 4 + 255) / 256;
+    if (blocks > 16384) blocks = 16384;
+    hipLaunchKernelGGL(dtype == RK_F16 ? write_fp4_kernel<true> : write_fp4_kernel<false>, dim3((unsigned)blocks, 2), dim3(256), 0,
+                       (hipStream_t)stream, T, Hkv, D, (const uint16_t*)k, k_token, k_head, (const uint16_t*)v, v_token, v_head,
+                       *k_cache, *v_cache, n_blocks, slots, st);
+    return hip_check(hipGetLastError(), "rk_kv_write_fp4 launch");
+}
+
+int rk_kv_read_fp4(int64_t T, int32_t Hkv, int32_t D, int32_t dtype, const rk_fp4_cache* k_cache, const rk_fp4_cache* v_cache,
+                   int32_t n_blocks, const int64_t* slots, void* k, int64_t k_token, int64_t k_head, void* v, int64_t v_token,
+                   int64_t v_head, void* stream)
+{
+    const char* name = "rk_kv_read_fp4";
+    if (int rc = tokens_arguments(name, T, Hkv, D, dtype, k, k_token, k_head, v, v_token, v_head, k_cache, v_cache, n_blocks, slots))
+        return rc;
+    if (!rows_apart({{T, k_token}, {Hkv, k_head}}, D) || !rows_apart({{T, v_token}, {Hkv, v_head}}, D))
+        return fail(RK_EINVAL, "%s: an output's strides lay heads or tokens over each other", name);
+    if (T == 0) return RK_OK;
+    int32_t* st = status_word();
+    if (!st) return fail(RK_EHIP, "%s: no status word", name);
+    int64_t blocks = (T * Hkv * (D / 8) + 255) / 256;
+    if (blocks > 16384) blocks = 16384;
+    hipLaunchKernelGGL(dtype == RK_F16 ? read_fp4_kernel<true> : read_fp4_kernel<false>, dim3((unsigned)blocks, 2), dim3(256), 0,
+                       (hipStream_t)stream, T, Hkv, D / 8, (uint16_t*)k, k_token, k_head, (uint16_t*)v, v_token, v_head, *k_cache,
+                       *v_cache, n_blocks, slots, st);
+    return hip_check(hipGetLastError(), "rk_kv_read_fp4 launch");
+}
+
+}  // extern "C"

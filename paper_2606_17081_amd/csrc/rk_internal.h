@@ -407,6 +407,32 @@ struct EpisodeLayout {
 EpisodeLayout episode_layout(int32_t W, int32_t cache_blocks, int32_t max_blocks, int32_t max_conv,
                              int32_t max_routes);
 
+// Of a cache held in 4 bits: no stride below 0, rows of codes at multiples of 16 bytes.
+inline bool fp4_strides(const rk_fp4_cache& c)
+{
+    for (int64_t x : {c.cs.block, c.cs.token, c.cs.head})
+        if (x < 0 || x % 16) return false;
+    for (int64_t x : {c.ss.block, c.ss.token, c.ss.head})
+        if (x < 0) return false;
+    return true;
+}
+
+// Eight codes of 4 bits as 16-bit values; scale: their power of two.
+template <bool Half>
+__device__ __forceinline__ u32x4 fp4_values(uint32_t codes, float scale)
+{
+    if constexpr (Half)
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3))};
+    else
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
+}
+
 // A dimension of an array: how many, and how far apart, in elements.
 struct ArrayDim {
     int64_t n, stride;

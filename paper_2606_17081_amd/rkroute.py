@@ -33,7 +33,8 @@ EXPORTED = ("rk_status_string", "rk_last_error", "rk_device_status", "rk_hash_ch
             "rk_simulate_workspace_size",
             "rk_simulate_episodes", "rk_poa_workspace_size", "rk_poa_estimate",
             "rk_poa_estimate_noalloc", "rk_prefix_groups", "rk_block_tables", "rk_kv_write",
-            "rk_prefix_attention_workspace_size", "rk_prefix_attention")
+            "rk_prefix_attention_workspace_size", "rk_prefix_attention", "rk_kv_write_fp4", "rk_kv_read_fp4",
+            "rk_prefix_attention_fp4_workspace_size", "rk_prefix_attention_fp4")
 RK_POA_NOALLOC_BYTES = 64 << 20
 
 
@@ -91,6 +92,14 @@ class Attention(C.Structure):
                 ("tables", C.c_void_p), ("kv_len", C.c_void_p), ("q_off", C.c_void_p),
                 ("group_off", C.c_void_p), ("shared", C.c_void_p),
                 ("out", C.c_void_p), ("out_token", C.c_int64), ("out_head", C.c_int64), ("lse", C.c_void_p)]
+
+
+class Fp4Cache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("cs", CacheStrides), ("scales", C.c_void_p), ("ss", CacheStrides)]
+
+
+class AttentionFp4(C.Structure):
+    _fields_ = [("a", Attention), ("k", Fp4Cache), ("v", Fp4Cache)]
 
 
 # rk_episode_params, 104 bytes, as a numpy record
@@ -161,6 +170,14 @@ def lib():
             L.rk_prefix_attention_workspace_size.argtypes = [i64, i32, i32, i32, i32]
             L.rk_prefix_attention.restype = C.c_int
             L.rk_prefix_attention.argtypes = [vp, vp, sz, vp]
+            L.rk_kv_write_fp4.restype = C.c_int
+            L.rk_kv_write_fp4.argtypes = [i64, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, i32, vp, vp]
+            L.rk_kv_read_fp4.restype = C.c_int
+            L.rk_kv_read_fp4.argtypes = [i64, i32, i32, i32, vp, vp, i32, vp, vp, i64, i64, vp, i64, i64, vp]
+            L.rk_prefix_attention_fp4_workspace_size.restype = sz
+            L.rk_prefix_attention_fp4_workspace_size.argtypes = [i64, i32, i32, i32, i32]
+            L.rk_prefix_attention_fp4.restype = C.c_int
+            L.rk_prefix_attention_fp4.argtypes = [vp, vp, sz, vp]
             _lib = L
     return _lib
 
@@ -609,14 +626,21 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
     dev = _where("q", q)
     _no_gradient("prefix_attention", q, k_cache, v_cache, out, lse)
     dtype, shape = _heads("q", q, 3)
-    T, Hq, D = shape
-    q_token, q_head = _rows("q", q, dev, dtype, shape)
     if k_cache.dim() != 4:
         raise RkError("k_cache must be [blocks, 16, heads, D]")
     blocks, _, Hkv, _ = k_cache.shape
-    cache = (blocks, RK_BLOCK_TOKENS, Hkv, D)
+    cache = (blocks, RK_BLOCK_TOKENS, Hkv, shape[2])
     ks = _cache_strides("k_cache", k_cache, dev, dtype, cache)
     vs = _cache_strides("v_cache", v_cache, dev, dtype, cache)
+    return _attend("rk_prefix_attention", dev, q, dtype, shape, blocks, Hkv, (k_cache.data_ptr(), *ks, v_cache.data_ptr(), *vs),
+                   b"", tables, kv_len, q_off, group_off, shared, scale, out, lse, want_lse, workspace, stream)
+
+
+def _attend(name, dev, q, dtype, shape, blocks, Hkv, caches, more, tables, kv_len, q_off, group_off, shared, scale, out, lse,
+            want_lse, workspace, stream):
+    """The call `name`; caches: pointers and strides of 16-bit caches, more: what follows the rk_attention."""
+    T, Hq, D = shape
+    q_token, q_head = _rows("q", q, dev, dtype, shape)
     with _On(dev, stream) as st:
         torch = _found_torch
         i32, i64 = torch.int32, torch.int64
@@ -630,8 +654,9 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
             out_token, out_head = _rows("out", out, dev, dtype, shape)
         if lse is None and want_lse:
             lse = torch.empty((T, Hq), dtype=torch.float32, device=at)
+        L = lib()
         if workspace is None:
-            ws_bytes = prefix_attention_workspace_size(T if group_off is not None else 0, B, Hq, Hkv, D)
+            ws_bytes = getattr(L, name + "_workspace_size")(T if group_off is not None else 0, B, Hq, Hkv, D)
             workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=at)
         elif workspace.get_device() != dev or not workspace.is_contiguous():
             raise RkError(f"workspace must be a contiguous tensor on cuda:{dev}")
@@ -639,11 +664,96 @@ def prefix_attention(q, k_cache, v_cache, tables, kv_len, q_off, group_off=None,
             ws_bytes = workspace.numel() * workspace.element_size()
         a = _attention_struct.pack(
             B, Hq, Hkv, D, _NARROW[dtype], blocks, stride, max(D, 1) ** -0.5 if scale is None else scale, T, q.data_ptr(),
-            q_token, q_head, k_cache.data_ptr(), *ks, v_cache.data_ptr(), *vs, _flat("tables", tables, i32, dev, 0),
+            q_token, q_head, *caches, _flat("tables", tables, i32, dev, 0),
             _flat("kv_len", kv_len, i32, dev, B), _flat("q_off", q_off, i64, dev, B + 1),
             _flat("group_off", group_off, i64, dev, B + 1) or 0, _flat("shared", shared, i32, dev, B) or 0,
-            out.data_ptr(), out_token, out_head, _flat("lse", lse, torch.float32, dev, T * Hq) or 0)
-        _check(lib().rk_prefix_attention(a, workspace.data_ptr(), ws_bytes, st), "rk_prefix_attention")
+            out.data_ptr(), out_token, out_head, _flat("lse", lse, torch.float32, dev, T * Hq) or 0) + more
+        _check(getattr(L, name)(a, workspace.data_ptr(), ws_bytes, st), name)
         if given:
             _changed(*given)
     return out, lse
+
+
+# ------------------------------------------------------------------ a worker's cache in 4 bits
+
+_fp4_struct = struct.Struct("@P3qP3q")
+assert _fp4_struct.size == C.sizeof(Fp4Cache) and C.sizeof(AttentionFp4) == _attention_struct.size + 2 * _fp4_struct.size
+
+
+def _fp4_cache(which, codes, scales, dev, blocks, Hkv, D):
+    """A cache in 4 bits as the ABI's struct: codes [blocks, 16, Hkv, 16 C], scales [blocks, 16, Hkv, C], C = ceil(D / 32)."""
+    u8, C_ = _found_torch.uint8, -(-D // 32)
+    shape = (blocks, RK_BLOCK_TOKENS, Hkv)
+    return _fp4_struct.pack(codes.data_ptr(), *_cache_strides(which + "_cache", codes, dev, u8, (*shape, 16 * C_)),
+                            scales.data_ptr(), *_cache_strides(which + "_scales", scales, dev, u8, (*shape, C_)))
+
+
+def kv_write_fp4(k, v, k_cache, v_cache, k_scales, v_scales, slots, stream=None):
+    """Keys and values [T, Hkv, D] of new tokens into a cache in 4 bits (rk_kv_write_fp4): codes uint8 [blocks, 16, Hkv, 16 C],
+    scales uint8 [blocks, 16, Hkv, C], C = ceil(D / 32)."""
+    dev = _where("k", k)
+    _no_gradient("kv_write_fp4", k, v)
+    dtype, shape = _heads("k", k, 3)
+    T, Hkv, D = shape
+    k_token, k_head = _rows("k", k, dev, dtype, shape)
+    v_token, v_head = _rows("v", v, dev, dtype, shape)
+    if k_cache.dim() != 4:
+        raise RkError("k_cache must be [blocks, 16, heads, 16 ceil(D / 32)]")
+    blocks = k_cache.shape[0]
+    kc, vc = _fp4_cache("k", k_cache, k_scales, dev, blocks, Hkv, D), _fp4_cache("v", v_cache, v_scales, dev, blocks, Hkv, D)
+    with _On(dev, stream) as st:
+        _check(lib().rk_kv_write_fp4(T, Hkv, D, _NARROW[dtype], k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, kc, vc,
+                                     blocks, _flat("slots", slots, _found_torch.int64, dev, T), st), "rk_kv_write_fp4")
+        _changed(k_cache, v_cache, k_scales, v_scales)
+
+
+def kv_read_fp4(k_cache, v_cache, k_scales, v_scales, slots, D=None, dtype=None, k=None, v=None, stream=None):
+    """Tokens of a cache in 4 bits as 16-bit values (rk_kv_read_fp4): (k, v), [tokens, Hkv, D] each.  D defaults to the k that is
+    given, or to 2 bytes' worth of a row of codes each (32 C); dtype to the k that is given, or to bfloat16."""
+    dev = _where("k_cache", k_cache)
+    torch = _found_torch or _torch()
+    _no_gradient("kv_read_fp4", k, v)
+    if k_cache.dim() != 4:
+        raise RkError("k_cache must be [blocks, 16, heads, 16 ceil(D / 32)]")
+    blocks, _, Hkv, row = k_cache.shape
+    T = slots.numel()
+    given = [t for t in (k, v) if t is not None]
+    if D is None:
+        D = 2 * row if not given else given[0].shape[-1]
+    if dtype is None:
+        dtype = given[0].dtype if given else torch.bfloat16
+    with _On(dev, stream) as st:
+        shape = (T, Hkv, D)
+        if k is None:
+            k = torch.empty(shape, dtype=dtype, device=k_cache.device)
+        if v is None:
+            v = torch.empty(shape, dtype=dtype, device=k_cache.device)
+        _heads("k", k, 3)
+        k_token, k_head = _rows("k", k, dev, dtype, shape)
+        v_token, v_head = _rows("v", v, dev, dtype, shape)
+        kc, vc = _fp4_cache("k", k_cache, k_scales, dev, blocks, Hkv, D), _fp4_cache("v", v_cache, v_scales, dev, blocks, Hkv, D)
+        _check(lib().rk_kv_read_fp4(T, Hkv, D, _NARROW[dtype], kc, vc, blocks, _flat("slots", slots, torch.int64, dev, T),
+                                    k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, st), "rk_kv_read_fp4")
+        if given:
+            _changed(*given)
+    return k, v
+
+
+def prefix_attention_fp4_workspace_size(T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
+    """As prefix_attention_workspace_size, of prefix_attention_fp4."""
+    return int(lib().rk_prefix_attention_fp4_workspace_size(T, B, Hq, Hkv, D))
+
+
+def prefix_attention_fp4(q, k_cache, v_cache, k_scales, v_scales, tables, kv_len, q_off, group_off=None, shared=None, scale=None,
+                         out=None, lse=None, want_lse=False, workspace=None, stream=None):
+    """prefix_attention over a cache in 4 bits (rk_prefix_attention_fp4): (out, lse or None)."""
+    dev = _where("q", q)
+    _no_gradient("prefix_attention_fp4", q, out, lse)
+    dtype, shape = _heads("q", q, 3)
+    if k_cache.dim() != 4:
+        raise RkError("k_cache must be [blocks, 16, heads, 16 ceil(D / 32)]")
+    blocks, _, Hkv, _ = k_cache.shape
+    more = (_fp4_cache("k", k_cache, k_scales, dev, blocks, Hkv, shape[2]) +
+            _fp4_cache("v", v_cache, v_scales, dev, blocks, Hkv, shape[2]))
+    return _attend("rk_prefix_attention_fp4", dev, q, dtype, shape, blocks, Hkv, (0,) * 8, more, tables, kv_len, q_off, group_off,
+                   shared, scale, out, lse, want_lse, workspace, stream)
