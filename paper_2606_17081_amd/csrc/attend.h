@@ -32,8 +32,11 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int32_t kLaunch = 1024;                    // requests of a launch: what is known of each is kept in LDS
 constexpr int kWideRows = 128, kWideKeys = 64;       // a wide step: 32 rows a wavefront, 64 keys
-constexpr int kNarrowRows = 32, kNarrowKeys = 128;   // a narrow step: 32 keys a wavefront
-constexpr int kSoloKeys = 32, kSoloMost = 512;       // a narrow tile of so few keys is one wavefront's: 32 a step
+constexpr int kNarrowRows = 32;
+// Keys of a wavefront in a narrow step.  In 4 bits a key is a quarter of the bytes, and as many should be under way.
+template <bool Fp4>
+constexpr int kNarrowKeys = Fp4 ? 64 : 32;
+constexpr int kSoloMost = 512;                       // a narrow tile of so few keys is one wavefront's
 
 // Kinds of tiles, each on a line of its own.
 enum Kind { kWide, kNarrow, kSolo };
@@ -45,7 +48,9 @@ enum Kind { kWide, kNarrow, kSolo };
 constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
 constexpr uint32_t kLeast = 4;
 static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
-constexpr int kKeysOf[3] = {kWideKeys, kNarrowKeys, kSoloKeys};
+// Keys of a tile's step.
+template <bool Fp4>
+constexpr int kKeysOf[3] = {kWideKeys, kWaves * kNarrowKeys<Fp4>, kNarrowKeys<Fp4>};
 constexpr int kJoinCost = 2;                         // of a request whose prefix and own keys are joined
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 
@@ -197,6 +202,7 @@ __device__ __forceinline__ Memory memory(const uint8_t* from, int32_t bytes)
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, bytes, 0x00027000);
 }
 __device__ __forceinline__ u32x4 load16(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b128(m, at, 0, 0); }
+__device__ __forceinline__ u32x2 load8(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b64(m, at, 0, 0); }
 __device__ __forceinline__ uint8_t load1(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b8(m, at, 0, 0); }
 
 // x, in a way that what is computed from it stays where it is used: hoisted out of the loop over tiles, the
@@ -264,6 +270,7 @@ struct Tile {
 template <int DP, bool Half, bool Fp4>
 struct Attend {
     static constexpr int kHead = DP;
+    static constexpr bool kFp4 = Fp4;
     static constexpr int NC = DP / 8;                 // 16-byte pieces of a row
     static constexpr int NI = NC / 4;                 // loads of 64 pieces that bring a block
     static constexpr uint32_t kRow = DP * 2;          // bytes of a row in LDS
@@ -289,7 +296,10 @@ struct Attend {
     const uint32_t last_piece;                        // of a row: the bytes before it
     // the pieces of a block that the lane loads: whole rows a load, or not
     static constexpr bool kEven = 64 % NC == 0;
-    static constexpr int kShares = DP / 32, kRounds = (RK_BLOCK_TOKENS * kShares + 63) / 64;    // of a cache in 4 bits: 32 values a lane
+    // Of a cache in 4 bits a lane loads a quarter of a row of a block: in each round a share, in the last (of a DP that is no
+    // multiple of 128) half a share.
+    static constexpr int kShares = DP / 32, kRounds = (kShares + 3) / 4;
+    static constexpr bool kHalfRound = kShares % 4 != 0;
     static constexpr int kPlaces = Fp4 ? kRounds : kEven ? 2 : NI;
     uint32_t k_at[kPlaces], v_at[kPlaces], ks_at[Fp4 ? kRounds : 1], vs_at[Fp4 ? kRounds : 1];
 
@@ -302,12 +312,8 @@ struct Attend {
         if constexpr (Fp4) {
 #pragma unroll
             for (int i = 0; i < kRounds; ++i) {
-                const uint32_t x = 64 * i + lane, r = x / kShares, share = x % kShares;
-                const bool there = r < RK_BLOCK_TOKENS && 32 * share < (uint32_t)p.a.D;
-                k_at[i] = there ? r * (uint32_t)p.kc.cs.token + 16 * share : 0x80000000u;
-                v_at[i] = there ? r * (uint32_t)p.vc.cs.token + 16 * share : 0x80000000u;
-                ks_at[i] = there ? r * (uint32_t)p.kc.ss.token + share : 0x80000000u;
-                vs_at[i] = there ? r * (uint32_t)p.vc.ss.token + share : 0x80000000u;
+                codes_at(p.kc, i, lane & 15, lane >> 4, k_at[i], ks_at[i]);
+                codes_at(p.vc, i, lane >> 2, lane & 3, v_at[i], vs_at[i]);
             }
         } else if constexpr (kEven) {
             const uint32_t r = lane / NC;
@@ -374,24 +380,61 @@ struct Attend {
         }
     }
 
-    // The same of a block held in 4 bits, as 16-bit values, which hold them exactly: 32 of one power of two a lane.
-    __device__ __forceinline__ void load_codes(const rk_fp4_cache& c, int32_t head, int32_t id, int32_t rows, const uint32_t* at,
-                                               const uint32_t* scale_at, uint32_t lds) const
+    // What a lane loads of a block held in 4 bits: quarter j of row r, the codes and the powers of two.
+    struct Codes {
+        u32x4 w[kRounds];
+        uint32_t power[kRounds];
+        // the lane's ks-th eight values in 16 bits, which hold them exactly
+        template <bool H>
+        __device__ __forceinline__ u32x4 values(int ks) const
+        {
+            return fp4_values<H>(w[ks / 4][ks % 4], __uint_as_float(power[ks / 4] << 23));
+        }
+    };
+    static constexpr int kPieces = DP / 32;                            // of 8 values, a lane's of a row
+    // which of a row's pieces of 8 values quarter j has as its ks-th
+    static __device__ __forceinline__ int piece_of(int ks, int j)
     {
-        const int32_t shares = (p.a.D + 31) / 32, last = rows - 1;
-        const Memory codes = memory((const uint8_t*)c.codes + id * c.cs.block + head * c.cs.head,
+        if (kHalfRound && ks / 4 == kRounds - 1) return 4 * (ks / 4 * 4 + j / 2) + 2 * (j & 1) + ks % 4;
+        return 4 * (ks / 4 * 4 + j) + ks % 4;
+    }
+    // Byte offsets in a block of round i's codes and power of two of the row's quarter.
+    __device__ __forceinline__ void codes_at(const rk_fp4_cache& c, int i, uint32_t r, uint32_t j, uint32_t& at, uint32_t& scale_at) const
+    {
+        const bool half = kHalfRound && i == kRounds - 1;
+        const uint32_t share = 4 * i + (half ? j / 2 : j);
+        const bool there = 32 * share < (uint32_t)p.a.D;
+        at = there ? r * (uint32_t)c.cs.token + 16 * share + (half ? 8 * (j & 1) : 0) : 0x80000000u;
+        scale_at = there ? r * (uint32_t)c.ss.token + share : 0x80000000u;
+    }
+    __device__ __forceinline__ Codes codes_of(const rk_fp4_cache& c, const Tile& t, int32_t b, int32_t id, const uint32_t* at,
+                                              const uint32_t* scale_at) const
+    {
+        const int32_t rows = rows_of(t, b, id), block = rows > 0 ? id : 0, shares = (p.a.D + 31) / 32, last = rows - 1;
+        const Memory codes = memory((const uint8_t*)c.codes + block * c.cs.block + t.head * c.cs.head,
                                     rows > 0 ? last * (int32_t)c.cs.token + 16 * shares : 0);
-        const Memory scales = memory((const uint8_t*)c.scales + id * c.ss.block + head * c.ss.head,
+        const Memory scales = memory((const uint8_t*)c.scales + block * c.ss.block + t.head * c.ss.head,
                                      rows > 0 ? last * (int32_t)c.ss.token + shares : 0);
+        Codes x;
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
-            const uint32_t x = 64 * i + (threadIdx.x & 63), r = x / kShares, share = x % kShares;
-            const u32x4 w = load16(codes, at[i]);
-            const float scale = __uint_as_float((uint32_t)load1(scales, scale_at[i]) << 23);
-            if (RK_BLOCK_TOKENS * kShares % 64 != 0 && r >= RK_BLOCK_TOKENS) break;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) lds_write16(lds + r * kRow + (((4 * share + k) ^ turn(r)) << 4), fp4_values<Half>(w[k], scale));
+            if (kHalfRound && i == kRounds - 1) {
+                const u32x2 w = load8(codes, at[i]);
+                x.w[i] = u32x4{w.x, w.y, 0u, 0u};
+            } else {
+                x.w[i] = load16(codes, at[i]);
+            }
+            x.power[i] = load1(scales, scale_at[i]);
         }
+        return x;
+    }
+    // A lane's quarter (of row lane / 4) as 16-bit values to LDS.
+    __device__ __forceinline__ void place_values(const Codes& x, uint32_t lds) const
+    {
+        const uint32_t lane = threadIdx.x & 63, r = lane >> 2;
+#pragma unroll
+        for (int ks = 0; ks < kPieces; ++ks)
+            lds_write16(lds + r * kRow + (((uint32_t)piece_of(ks, lane & 3) ^ turn(r)) << 4), x.template values<Half>(ks));
     }
 
     // Block number `b`'s block of the segment's sequence, keys to k_lds, values to v_lds (either may be left out).
@@ -408,21 +451,27 @@ struct Attend {
     }
     __device__ __forceinline__ void load_keys(const Tile& t, int32_t b, int32_t id, uint32_t lds) const
     {
-        const int32_t rows = rows_of(t, b, id);
-        if constexpr (Fp4)
-            load_codes(p.kc, t.head, rows > 0 ? id : 0, rows, k_at, ks_at, lds);
-        else
+        if constexpr (Fp4) {
+            const int lane = threadIdx.x & 63;
+            uint32_t at[kRounds], scale_at[kRounds];
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) codes_at(p.kc, i, lane >> 2, lane & 3, at[i], scale_at[i]);
+            place_values(codes_of(p.kc, t, b, id, at, scale_at), lds);
+        } else {
+            const int32_t rows = rows_of(t, b, id);
             load_block((const uint16_t*)p.a.k_cache + (rows > 0 ? (int64_t)id * p.a.ks.block : 0) + t.head * p.a.ks.head,
                        p.a.ks.token, rows, k_at, lds);
+        }
     }
     __device__ __forceinline__ void load_values(const Tile& t, int32_t b, int32_t id, uint32_t lds) const
     {
-        const int32_t rows = rows_of(t, b, id);
-        if constexpr (Fp4)
-            load_codes(p.vc, t.head, rows > 0 ? id : 0, rows, v_at, vs_at, lds);
-        else
+        if constexpr (Fp4) {
+            place_values(codes_of(p.vc, t, b, id, v_at, vs_at), lds);
+        } else {
+            const int32_t rows = rows_of(t, b, id);
             load_block((const uint16_t*)p.a.v_cache + (rows > 0 ? (int64_t)id * p.a.vs.block : 0) + t.head * p.a.vs.head,
                        p.a.vs.token, rows, v_at, lds);
+        }
     }
     // a block whose number is outside the cache
     __device__ __forceinline__ bool bad_block(int32_t id) const { return (uint32_t)id >= (uint32_t)p.a.n_blocks; }
@@ -842,7 +891,7 @@ struct Attend {
     template <int NQ, bool Solo>
     __device__ void narrow(const Tile& t)
     {
-        constexpr int KS = DP / 32, DT = DP / 16;
+        constexpr int KS = DP / 32, DT = DP / 16, NB = kNarrowKeys<Fp4> / RK_BLOCK_TOKENS;    // blocks of a step
         const int lane = afresh(threadIdx.x & 63);
         const int g = lane >> 4, col = lane & 15;
         u32x4 q[NQ][KS];
@@ -851,7 +900,7 @@ struct Attend {
         for (int n = 0; n < NQ; ++n) {
             const int32_t r = 16 * n + col;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query(t, r, 4 * ks + g);
+            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query(t, r, Fp4 ? piece_of(ks, g) : 4 * ks + g);
             last[n] = t.keys_end - 1;
             if (t.mask) {
                 const int32_t pos = t.pos + token_of(r);
@@ -877,51 +926,60 @@ struct Attend {
             for (int x = 0; x < kTurn / 2; ++x)
                 v_read[x] = vr * kRow + (((2 * x + ((lane & 3) >> 1)) ^ turn(vr)) << 4) + 8 * (lane & 1);
         }
-        const uint32_t keys = tile + wave * (64 * kRow), vals = keys + 32 * kRow;
-        // this wavefront's steps: 32 keys at 128 s + 32 wave, or all of them
-        constexpr int kKeys = Solo ? kSoloKeys : kNarrowKeys, kBlocks = kKeys / RK_BLOCK_TOKENS;
-        const int32_t first_block = t.block0 + (Solo ? 0 : 2 * wave);
+        // (of a cache in 4 bits keys stay in registers, and all of the wavefront's LDS is the values')
+        const uint32_t keys = tile + wave * (64 * kRow), vals = Fp4 ? keys : keys + 32 * kRow;
+        // this wavefront's steps: of each 4 NB blocks (of a workgroup's tile) NB from NB wave on, or all of them
+        constexpr int kKeys = kKeysOf<Fp4>[Solo ? kSolo : kNarrow], kBlocks = kKeys / RK_BLOCK_TOKENS;
+        const int32_t first_block = t.block0 + (Solo ? 0 : NB * wave);
         int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kKeys - 1) / kKeys;
         s1 = s1 < t.s1 ? s1 : t.s1;
-        int32_t s = t.s0, id[2], later[2];
+        int32_t s = t.s0, id[NB], later[NB];
         auto ids = [&](int32_t* to, int32_t x) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) to[b] = block_id(t, first_block + kBlocks * x + b);
+            for (int b = 0; b < NB; ++b) to[b] = block_id(t, first_block + kBlocks * x + b);
         };
         uint32_t bad = 0, next_bad = 0;
+        Codes k_raw[Fp4 ? NB : 1], v_raw[Fp4 ? NB : 1];
         auto issue_keys = [&](int32_t x) {
             next_bad = 0;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                load_keys(t, first_block + kBlocks * x + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
+            for (int b = 0; b < NB; ++b) {
+                if constexpr (Fp4) k_raw[b] = codes_of(p.kc, t, first_block + kBlocks * x + b, id[b], k_at, ks_at);
+                else load_keys(t, first_block + kBlocks * x + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
                 next_bad |= (bad_block(id[b]) ? 1u : 0u) << b;
             }
+            if constexpr (Fp4) __builtin_amdgcn_sched_barrier(0);
         };
-        auto issue_values = [&](int32_t x) {
+        auto issue_values = [&](int32_t x, const int32_t* which) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-                load_values(t, first_block + kBlocks * x + b, id[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+            for (int b = 0; b < NB; ++b) {
+                if constexpr (Fp4) v_raw[b] = codes_of(p.vc, t, first_block + kBlocks * x + b, which[b], v_at, vs_at);
+                else load_values(t, first_block + kBlocks * x + b, which[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+            }
+            if constexpr (Fp4) __builtin_amdgcn_sched_barrier(0);
         };
-        auto scores = [&](f32x4 (*sc)[2]) {
+        auto scores = [&](f32x4 (*sc)[NB]) {
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
+            for (int kt = 0; kt < NB; ++kt) {
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) sc[n][kt] = f32x4{};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const u32x4 k = lds_read16(keys + k_read[ks % (kTurn / 4)] +
-                                               (uint32_t)(kt * 16 * kRow + ks / (kTurn / 4) * (16 * kTurn)));
+                    u32x4 k;
+                    if constexpr (Fp4) k = k_raw[kt].template values<Half>(ks);
+                    else k = lds_read16(keys + k_read[ks % (kTurn / 4)] +
+                                        (uint32_t)(kt * 16 * kRow + ks / (kTurn / 4) * (16 * kTurn)));
 #pragma unroll
                     for (int n = 0; n < NQ; ++n) sc[n][kt] = mfma16<Half>(k, q[n][ks], sc[n][kt]);
                 }
             }
         };
-        auto weights = [&](f32x4 (*sc)[2], u32x4* w) {
+        auto weights = [&](f32x4 (*sc)[NB], u32x4 (*w)[NB / 2]) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 float top = sc[n][0][0];
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+                for (int kt = 0; kt < NB; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) top = larger(top, sc[n][kt][i]);
                 if (__any(strays(top * c, m[n]))) {
@@ -941,73 +999,85 @@ struct Attend {
                 }
                 const float base = m[n] == -INFINITY ? 0.0f : -m[n];
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+                for (int kt = 0; kt < NB; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; i += 2) {
                         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i], c, base));
                         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i + 1], c, base));
                         l[n] += x + y;
-                        w[n][2 * kt + (i >> 1)] = pack16<Half>(x, y);
+                        w[n][kt / 2][2 * (kt % 2) + (i >> 1)] = pack16<Half>(x, y);
                     }
             }
         };
-        auto values = [&](int d) {
-            const uint32_t x = vals + v_read[d % (kTurn / 2)] + (uint32_t)(d / (kTurn / 2) * (16 * kTurn));
+        auto values = [&](int d, int c) {
+            const uint32_t x = vals + c * (32 * kRow) + v_read[d % (kTurn / 2)] + (uint32_t)(d / (kTurn / 2) * (16 * kTurn));
             const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
             return u32x4{lo.x, lo.y, up.x, up.y};
         };
         // (vector memory operations end in the order of their issue: the step's keys are there when only its values'
         // loads are under way, its values when only the next keys' are)
-        auto wait_keys = [&]() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory"); };
+        auto wait_keys = [&]() {
+            if constexpr (!Fp4) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
+        };
         auto keys_read = [&]() {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the keys are in registers
+            if constexpr (!Fp4) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the keys are in registers
             bad = next_bad;
             if (s + 1 < s1) {
-                id[0] = later[0];
-                id[1] = later[1];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) id[b] = later[b];
                 issue_keys(s + 1);
                 ids(later, s + 2);
             }
         };
         auto wait_values = [&]() {
-            if (s + 1 < s1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if constexpr (Fp4) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) place_values(v_raw[b], vals + b * (RK_BLOCK_TOKENS * kRow));
+                if (s + 1 < s1) issue_values(s + 1, id);
+            } else if (s + 1 < s1) {
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
         };
         auto values_read = [&]() {
+            if constexpr (Fp4) return;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the values are in registers
-            if (s + 1 < s1) issue_values(s + 1);
+            if (s + 1 < s1) issue_values(s + 1, id);
         };
         if constexpr (Solo) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the LDS is the last tile's until here
         else __syncthreads();
         if (s < s1) {
             ids(id, s);
             issue_keys(s);
-            issue_values(s);
+            issue_values(s, id);
             ids(later, s + 1);
         }
-        const int32_t seen = all_see + 1 - first_block * RK_BLOCK_TOKENS - 32;       // the last step's first key that all see
+        const int32_t seen = all_see + 1 - first_block * RK_BLOCK_TOKENS - kNarrowKeys<Fp4>;       // the last step's first key that all see
         const int32_t open = seen < 0 ? 0 : seen / kKeys + 1, s_open = open < s1 ? open : s1;
         for (; s < s_open && !next_bad; ++s) {
-            f32x4 sc[NQ][2];
-            u32x4 w[NQ];
+            f32x4 sc[NQ][NB];
+            u32x4 w[NQ][NB / 2];
             wait_keys();
             scores(sc);
             keys_read();
             weights(sc, w);
             wait_values();
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const u32x4 v = values(d);
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
-            }
+                for (int c = 0; c < NB / 2; ++c) {
+                    const u32x4 v = values(d, c);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
+                }
             values_read();
         }
         for (; s < s1; ++s) {
             const int32_t key0 = (first_block + kBlocks * s) * RK_BLOCK_TOKENS;
-            const bool masked = key0 + 31 > all_see;
-            f32x4 sc[NQ][2];
-            u32x4 w[NQ];
+            const bool masked = key0 + kNarrowKeys<Fp4> - 1 > all_see;
+            f32x4 sc[NQ][NB];
+            u32x4 w[NQ][NB / 2];
             wait_keys();
             scores(sc);
             keys_read();
@@ -1015,7 +1085,7 @@ struct Attend {
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+                for (int kt = 0; kt < NB; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
@@ -1024,10 +1094,10 @@ struct Attend {
             if (masked && t.mask && t.tokens > 1) {                      // (as for wide tiles, of values of the wavefront's own)
                 u16x2 most = {0, 0};
 #pragma unroll 4
-                for (int x = lane; x < 32 * NC; x += 64) most = without_sign(most, lds_read16(vals + 16 * x));
+                for (int x = lane; x < kNarrowKeys<Fp4> * NC; x += 64) most = without_sign(most, lds_read16(vals + 16 * x));
                 if (__any(not_finite<Half>(__builtin_bit_cast(uint32_t, most)))) {
 #pragma unroll 1
-                    for (int x = 0; x < 32; ++x)
+                    for (int x = 0; x < kNarrowKeys<Fp4>; ++x)
 #pragma unroll
                         for (int d = 0; d < DT; ++d) {
                             __builtin_amdgcn_sched_barrier(0);
@@ -1042,7 +1112,7 @@ struct Attend {
                                 o[n][d][3] += only_odd<Half>(sees, v.y >> 16);
                             }
                         }
-                    for (int x = lane; x < 32 * NC; x += 64) {
+                    for (int x = lane; x < kNarrowKeys<Fp4> * NC; x += 64) {
                         const u32x4 v = lds_read16(vals + 16 * x);
                         lds_write16(vals + 16 * x, u32x4{finite_or_zero<Half>(v.x), finite_or_zero<Half>(v.y),
                                                          finite_or_zero<Half>(v.z), finite_or_zero<Half>(v.w)});
@@ -1051,11 +1121,13 @@ struct Attend {
                 }
             }
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const u32x4 v = values(d);
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n], o[n][d]);
-            }
+                for (int c = 0; c < NB / 2; ++c) {
+                    const u32x4 v = values(d, c);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
+                }
             values_read();
         }
         constexpr int kRows = 16 * NQ;
@@ -1191,9 +1263,10 @@ struct Segment {
     uint64_t pair, cost;                     // cost of a pair (or tile), and in all
 };
 
+template <bool Fp4>
 __device__ __forceinline__ int32_t steps_for(int64_t keys, int kind)
 {
-    const int32_t per = kind == kWide ? kKeysOf[kWide] : kind == kNarrow ? kKeysOf[kNarrow] : kKeysOf[kSolo];
+    const int32_t per = kind == kWide ? kKeysOf<Fp4>[kWide] : kind == kNarrow ? kKeysOf<Fp4>[kNarrow] : kKeysOf<Fp4>[kSolo];
     return keys > 0 ? (int32_t)((keys + per - 1) / per) : 1;
 }
 
@@ -1213,6 +1286,7 @@ __device__ __forceinline__ int32_t steps_before(uint64_t length, int32_t steps)
     return n < (uint64_t)steps ? (int32_t)n : steps;
 }
 
+template <bool Fp4>
 __device__ __forceinline__ Segment own_segment(const Request& r, const AttendArgs& p)
 {
     Segment s{};
@@ -1224,18 +1298,19 @@ __device__ __forceinline__ Segment own_segment(const Request& r, const AttendArg
     if (s.tokens == 0) return s;
     s.tiles = (s.tokens + s.per - 1) / s.per;
     if (s.tiles == 1) {
-        s.steps0 = steps_for(own, s.kind);
+        s.steps0 = steps_for<Fp4>(own, s.kind);
         s.pair = s.cost = extent(s.steps0, s.kind);
     } else {
         s.grows = true;
-        s.steps0 = steps_for(own - s.tokens + s.per, kWide);
-        const int32_t last = steps_for(own - s.tokens + (int64_t)s.tiles * s.per, kWide);
+        s.steps0 = steps_for<Fp4>(own - s.tokens + s.per, kWide);
+        const int32_t last = steps_for<Fp4>(own - s.tokens + (int64_t)s.tiles * s.per, kWide);
         s.pair = extent(s.steps0, kWide) + extent(last, kWide) + 2 * kStepCost[kWide];
         s.cost = s.pair * ((s.tiles + 1) / 2);
     }
     return s;
 }
 
+template <bool Fp4>
 __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks, const AttendArgs& p)
 {
     Segment s{};
@@ -1244,7 +1319,7 @@ __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks
     s.kind = s.rows > kNarrowRows ? kWide : blocks * RK_BLOCK_TOKENS > p.solo_most ? kNarrow : kSolo;
     s.per = s.kind == kWide ? p.wide_tokens : s.tokens;
     s.tiles = (s.tokens + s.per - 1) / s.per;
-    s.steps0 = steps_for((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
+    s.steps0 = steps_for<Fp4>((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
     s.pair = extent(s.steps0, s.kind);
     s.cost = s.pair * s.tiles;
     return s;
@@ -1274,12 +1349,12 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         bool prefix = false;
         uint64_t before = 0;
         if (r.end) {
-            sg = prefix_segment(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, p);
+            sg = prefix_segment<A::kFp4>(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, p);
             before = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             prefix = off < before;
         }
         if (!prefix) {
-            sg = own_segment(r, p);
+            sg = own_segment<A::kFp4>(r, p);
             const uint64_t own = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             off -= before;
             if (off >= own) {                // on to the next request
@@ -1298,7 +1373,7 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         if (K == kWide && sg.grows) {
             auto steps_of = [&](int32_t k) {
                 const int64_t seen = (int64_t)(k + 1) * sg.per < sg.tokens ? (int64_t)(k + 1) * sg.per : sg.tokens;
-                return steps_for((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWide);
+                return steps_for<A::kFp4>((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWide);
             };
             const int32_t k = sg.tiles - 1 - j;
             const uint64_t first = extent(steps_of(j), kWide);
@@ -1508,7 +1583,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             // share 5 blocks stay apart, for 141 us, 134 when no groups are named.
             const int64_t n = m.end - f, tokens = req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0, rows = tokens * G;
             if (rows == 0 || rows >= kWideRows * n) continue;
-            const Segment sg = prefix_segment((int32_t)tokens, m.lent, p);
+            const Segment sg = prefix_segment<Fp4>((int32_t)tokens, m.lent, p);
             const int64_t apart = n * m.lent * (rows > kNarrowRows * n ? 2 : 1), costs = sg.kind == kSolo ? 1 : 4;    // in quarters
             if ((int64_t)sg.cost * costs + 4 * kJoinCost * n >= apart) continue;
             req[i].shared = m.lent;
@@ -1527,10 +1602,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 #pragma unroll
             for (int k = 0; k < 3; ++k) x.of[k] += sg.kind == k ? sg.cost * (uint64_t)a.Hkv : 0;
         };
-        add(own_segment(req[i], p));
+        add(own_segment<Fp4>(req[i], p));
         if (req[i].end) {
             const Request& l = req[req[i].end - 1];
-            add(prefix_segment(l.q0 + l.tokens - req[i].q0, req[i].shared, p));
+            add(prefix_segment<Fp4>(l.q0 + l.tokens - req[i].q0, req[i].shared, p));
         }
     };
     uint32_t together = 0;
