@@ -18,6 +18,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "rk_internal.h"
 
 namespace rk {
@@ -33,9 +35,6 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int32_t kLaunch = 1024;                    // requests of a launch: what is known of each is kept in LDS
 constexpr int kWideRows = 128, kWideKeys = 64;       // a wide step: 32 rows a wavefront, 64 keys
 constexpr int kNarrowRows = 32;
-// Keys of a wavefront in a narrow step.  In 4 bits a key is a quarter of the bytes, and as many should be under way.
-template <bool Fp4>
-constexpr int kNarrowKeys = Fp4 ? 64 : 32;
 constexpr int kSoloMost = 512;                       // a narrow tile of so few keys is one wavefront's
 
 // Kinds of tiles, each on a line of its own.
@@ -48,9 +47,9 @@ enum Kind { kWide, kNarrow, kSolo };
 constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
 constexpr uint32_t kLeast = 4;
 static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
-// Keys of a tile's step.
-template <bool Fp4>
-constexpr int kKeysOf[3] = {kWideKeys, kWaves * kNarrowKeys<Fp4>, kNarrowKeys<Fp4>};
+// Keys of a tile's step; A: the class of the tiles, whose kNarrowKeys are a wavefront's in a narrow step.
+template <class A>
+constexpr int kKeysOf[3] = {kWideKeys, kWaves * A::kNarrowKeys, A::kNarrowKeys};
 constexpr int kJoinCost = 2;                         // of a request whose prefix and own keys are joined
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 
@@ -267,10 +266,10 @@ struct Tile {
     float *part, *part_ml;                   // where the result goes; NULL: to out and lse
 };
 
-template <int DP, bool Half, bool Fp4>
-struct Attend {
+// What tiles of all kinds of caches have in common.
+template <int DP, bool Half>
+struct AttendBase {
     static constexpr int kHead = DP;
-    static constexpr bool kFp4 = Fp4;
     static constexpr int NC = DP / 8;                 // 16-byte pieces of a row
     static constexpr int NI = NC / 4;                 // loads of 64 pieces that bring a block
     static constexpr uint32_t kRow = DP * 2;          // bytes of a row in LDS
@@ -293,148 +292,11 @@ struct Attend {
     const int32_t G;                                  // query heads of a key head
     const uint32_t g_inverse;                         // (exact quotients of a tile's rows: fewer than 2^7)
     const float c;                                    // |scale| log2(e)
-    const uint32_t last_piece;                        // of a row: the bytes before it
-    // the pieces of a block that the lane loads: whole rows a load, or not
-    static constexpr bool kEven = 64 % NC == 0;
-    // Of a cache in 4 bits a lane loads a quarter of a row of a block: in each round a share, in the last (of a DP that is no
-    // multiple of 128) half a share.
-    static constexpr int kShares = DP / 32, kRounds = (kShares + 3) / 4;
-    static constexpr bool kHalfRound = kShares % 4 != 0;
-    static constexpr int kPlaces = Fp4 ? kRounds : kEven ? 2 : NI;
-    uint32_t k_at[kPlaces], v_at[kPlaces], ks_at[Fp4 ? kRounds : 1], vs_at[Fp4 ? kRounds : 1];
 
-    __device__ __forceinline__ Attend(const AttendArgs& args, uint32_t lds, float* j, float scale)
+    __device__ __forceinline__ AttendBase(const AttendArgs& args, uint32_t lds, float* j, float scale)
         : p(args), tile(lds), join(j), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), G(args.G),
-          g_inverse(args.g_inverse), c(scale),
-          last_piece(2 * args.a.D - 16)
+          g_inverse(args.g_inverse), c(scale)
     {
-        const int lane = threadIdx.x & 63;
-        if constexpr (Fp4) {
-#pragma unroll
-            for (int i = 0; i < kRounds; ++i) {
-                codes_at(p.kc, i, lane & 15, lane >> 4, k_at[i], ks_at[i]);
-                codes_at(p.vc, i, lane >> 2, lane & 3, v_at[i], vs_at[i]);
-            }
-        } else if constexpr (kEven) {
-            const uint32_t r = lane / NC;
-            k_at[0] = r * (uint32_t)p.a.ks.token * 2;
-            v_at[0] = r * (uint32_t)p.a.vs.token * 2;
-            k_at[1] = v_at[1] = 16 * ((uint32_t)(lane % NC) ^ turn(r));
-        } else {
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const uint32_t x = 64 * i + lane, r = x / NC, piece = 16 * ((x % NC) ^ turn(r));
-                k_at[i] = place(r * (uint32_t)p.a.ks.token * 2, piece);
-                v_at[i] = place(r * (uint32_t)p.a.vs.token * 2, piece);
-            }
-        }
-    }
-
-    // The byte offset of a row's piece, or, of a piece behind D (of rows that D does not fill), one past any block's end, whose load
-    // brings zeros: the query's are 0 there, and a product with anything that is not finite would not be.
-    __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece) const
-    {
-        return piece <= last_piece ? row + piece : 0x80000000u;
-    }
-
-    // The byte offset in a block of the piece that the lane loads i-th.
-    __device__ __forceinline__ uint32_t offset(const uint32_t* at, int i, int64_t token) const
-    {
-        if constexpr (!kEven) {
-            return at[i];
-        } else {
-            const uint32_t piece = at[1] ^ (16 * turn((uint32_t)i * (64 / NC)));
-            return place(at[0] + (uint32_t)(i * (64 / NC)) * (uint32_t)token * 2, piece);
-        }
-    }
-
-    // The block's `rows` first rows from base to LDS, zeros after them.  Straight to LDS, in flight until a wait for
-    // vector memory; written as asm with no register result so that the compiler does not place that wait before
-    // every LDS read.  The compiler sees no need of wait states inside it, so they stand there: one between the write of m0 and the
-    // load that takes its place in LDS from it, and before the block's first load five after an instruction of the vector unit that may
-    // have written the descriptor's registers (a readfirstlane, a spilled register's return).  (Five before every load: pieces
-    // of prompts with D = 192 110 -> 114 us.)
-    __device__ __forceinline__ void load_block(const uint16_t* base, int64_t stride, int32_t rows, const uint32_t* at,
-                                               uint32_t lds) const
-    {
-        const uint64_t b = (uint64_t)base;
-        u32x4 rsrc;
-        rsrc.x = (uint32_t)b;
-        rsrc.y = (uint32_t)(b >> 32) & 0xffffu;
-        rsrc.z = rows > 0 ? (uint32_t)((rows - 1) * (int32_t)stride * 2 + p.a.D * 2) : 0u;
-        rsrc.w = 0x00027000u;
-        rsrc.x = __builtin_amdgcn_readfirstlane(rsrc.x);
-        rsrc.y = __builtin_amdgcn_readfirstlane(rsrc.y);
-        rsrc.z = __builtin_amdgcn_readfirstlane(rsrc.z);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + 1024u * i);
-            if (i == 0)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to),
-                             "v"(offset(at, i, stride)), "s"(rsrc)
-                             : "m0", "memory");
-            else
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to),
-                             "v"(offset(at, i, stride)), "s"(rsrc)
-                             : "m0", "memory");
-        }
-    }
-
-    // What a lane loads of a block held in 4 bits: quarter j of row r, the codes and the powers of two.
-    struct Codes {
-        u32x4 w[kRounds];
-        uint32_t power[kRounds];
-        // the lane's ks-th eight values in 16 bits, which hold them exactly
-        template <bool H>
-        __device__ __forceinline__ u32x4 values(int ks) const
-        {
-            return fp4_values<H>(w[ks / 4][ks % 4], __uint_as_float(power[ks / 4] << 23));
-        }
-    };
-    static constexpr int kPieces = DP / 32;                            // of 8 values, a lane's of a row
-    // which of a row's pieces of 8 values quarter j has as its ks-th
-    static __device__ __forceinline__ int piece_of(int ks, int j)
-    {
-        if (kHalfRound && ks / 4 == kRounds - 1) return 4 * (ks / 4 * 4 + j / 2) + 2 * (j & 1) + ks % 4;
-        return 4 * (ks / 4 * 4 + j) + ks % 4;
-    }
-    // Byte offsets in a block of round i's codes and power of two of the row's quarter.
-    __device__ __forceinline__ void codes_at(const rk_fp4_cache& c, int i, uint32_t r, uint32_t j, uint32_t& at, uint32_t& scale_at) const
-    {
-        const bool half = kHalfRound && i == kRounds - 1;
-        const uint32_t share = 4 * i + (half ? j / 2 : j);
-        const bool there = 32 * share < (uint32_t)p.a.D;
-        at = there ? r * (uint32_t)c.cs.token + 16 * share + (half ? 8 * (j & 1) : 0) : 0x80000000u;
-        scale_at = there ? r * (uint32_t)c.ss.token + share : 0x80000000u;
-    }
-    __device__ __forceinline__ Codes codes_of(const rk_fp4_cache& c, const Tile& t, int32_t b, int32_t id, const uint32_t* at,
-                                              const uint32_t* scale_at) const
-    {
-        const int32_t rows = rows_of(t, b, id), block = rows > 0 ? id : 0, shares = (p.a.D + 31) / 32, last = rows - 1;
-        const Memory codes = memory((const uint8_t*)c.codes + block * c.cs.block + t.head * c.cs.head,
-                                    rows > 0 ? last * (int32_t)c.cs.token + 16 * shares : 0);
-        const Memory scales = memory((const uint8_t*)c.scales + block * c.ss.block + t.head * c.ss.head,
-                                     rows > 0 ? last * (int32_t)c.ss.token + shares : 0);
-        Codes x;
-#pragma unroll
-        for (int i = 0; i < kRounds; ++i) {
-            if (kHalfRound && i == kRounds - 1) {
-                const u32x2 w = load8(codes, at[i]);
-                x.w[i] = u32x4{w.x, w.y, 0u, 0u};
-            } else {
-                x.w[i] = load16(codes, at[i]);
-            }
-            x.power[i] = load1(scales, scale_at[i]);
-        }
-        return x;
-    }
-    // A lane's quarter (of row lane / 4) as 16-bit values to LDS.
-    __device__ __forceinline__ void place_values(const Codes& x, uint32_t lds) const
-    {
-        const uint32_t lane = threadIdx.x & 63, r = lane >> 2;
-#pragma unroll
-        for (int ks = 0; ks < kPieces; ++ks)
-            lds_write16(lds + r * kRow + (((uint32_t)piece_of(ks, lane & 3) ^ turn(r)) << 4), x.template values<Half>(ks));
     }
 
     // Block number `b`'s block of the segment's sequence, keys to k_lds, values to v_lds (either may be left out).
@@ -448,30 +310,6 @@ struct Attend {
     {
         const int32_t n = t.keys_end - b * RK_BLOCK_TOKENS;
         return (uint32_t)id < (uint32_t)p.a.n_blocks ? (n < RK_BLOCK_TOKENS ? n : RK_BLOCK_TOKENS) : 0;
-    }
-    __device__ __forceinline__ void load_keys(const Tile& t, int32_t b, int32_t id, uint32_t lds) const
-    {
-        if constexpr (Fp4) {
-            const int lane = threadIdx.x & 63;
-            uint32_t at[kRounds], scale_at[kRounds];
-#pragma unroll
-            for (int i = 0; i < kRounds; ++i) codes_at(p.kc, i, lane >> 2, lane & 3, at[i], scale_at[i]);
-            place_values(codes_of(p.kc, t, b, id, at, scale_at), lds);
-        } else {
-            const int32_t rows = rows_of(t, b, id);
-            load_block((const uint16_t*)p.a.k_cache + (rows > 0 ? (int64_t)id * p.a.ks.block : 0) + t.head * p.a.ks.head,
-                       p.a.ks.token, rows, k_at, lds);
-        }
-    }
-    __device__ __forceinline__ void load_values(const Tile& t, int32_t b, int32_t id, uint32_t lds) const
-    {
-        if constexpr (Fp4) {
-            place_values(codes_of(p.vc, t, b, id, v_at, vs_at), lds);
-        } else {
-            const int32_t rows = rows_of(t, b, id);
-            load_block((const uint16_t*)p.a.v_cache + (rows > 0 ? (int64_t)id * p.a.vs.block : 0) + t.head * p.a.vs.head,
-                       p.a.vs.token, rows, v_at, lds);
-        }
     }
     // a block whose number is outside the cache
     __device__ __forceinline__ bool bad_block(int32_t id) const { return (uint32_t)id >= (uint32_t)p.a.n_blocks; }
@@ -533,302 +371,11 @@ struct Attend {
                 l == 0.0f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
     }
 
-    // ---------------------------------------------------------------- up to 128 rows, 32 a wavefront
-    //
-    // Scores are computed transposed, keys x rows: a lane then holds 32 of the 64 scores of one row (lane
-    // % 32) in registers, in the order in which the product with the values takes them: the row of
-    // the value that lane half h multiplies with its j-th weight is the key whose score it holds.
-    //
-    // Bound by nothing alone: at D = 128 the two wavefronts of a SIMD have 2,048 cycles of matrix instructions a step, their CU's eight
-    // 2,048 of LDS reads (32 KB each at 128 B a cycle), and 1,600 of vector instructions, two thirds of them for exponentials and
-    // sums; on whole prompts the matrix units are busy for 43-52% of the cycles.  Rows of 64 a wavefront would halve the LDS
-    // reads, but need 300 registers of the 256 that two wavefronts a SIMD have; one a SIMD (as for D > 128) reaches
-    // half the rate: pieces of prompts with D = 192, 107 us for 52 GFLOP.  Conflicts of LDS banks are rare.
-    // One prompt of 8,192 tokens, 64 / 8 heads of 128: 1.12 ms, 975 TFLOP/s.
-    __device__ void wide(const Tile& t)
+    // A wide tile's results: o transposed, values x rows, of row r of the tile, m and l (the lane's half of the sum).
+    template <int DT>
+    __device__ __forceinline__ void wide_out(const Tile& t, const f32x16 (&o)[DT], float m, float l, int r, int lane) const
     {
-        constexpr int KS = DP / 16, DT = DP / 32;
-        const int lane = afresh(threadIdx.x & 63);
-        const int hi = lane >> 5, r = 32 * wave + (lane & 31);
-        int32_t last = t.keys_end - 1;               // the last position that the row sees
-        if (t.mask) {
-            const int32_t pos = t.pos + token_of(r);
-            last = pos < last ? pos : last;
-        }
-        const int32_t all_see = t.mask ? (t.pos < t.keys_end - 1 ? t.pos : t.keys_end - 1) : t.keys_end - 1;
-        f32x16 o[DT];
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-        float m = -INFINITY, l = 0.0f;               // m: log2 of the weights' common divisor
-        // LDS addresses in a stage, less what the unrolled loops add
-        uint32_t k_read[kTurn / 2], v_read[kTurn / 4];
-        {
-            const uint32_t row = lane & 31, vr = 4 * hi + ((lane & 15) >> 2), vp = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-#pragma unroll
-            for (int x = 0; x < kTurn / 2; ++x) k_read[x] = row * kRow + (((2 * x + hi) ^ turn(row & 15)) << 4);
-#pragma unroll
-            for (int x = 0; x < kTurn / 4; ++x) v_read[x] = vr * kRow + (((4 * x + vp) ^ turn(vr)) << 4) + 8 * (lane & 1);
-        }
-        constexpr uint32_t kKeys = kWideKeys * kRow;   // bytes of a step's keys; two of them, then two steps' values
-        // Keys come two steps ahead, values one: while a step's weights are computed, the products of the next step's
-        // scores run beside them (whole prompts 1,440 -> 1,360 us).  Pieces are read from LDS kAhead products before the one that
-        // takes them: 3 are as good, 6 spill registers (whole prompts 1,230 -> 1,500 us).
-        constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
-        struct Step {
-            int32_t own;                             // this wavefront's block
-            uint32_t bad;                            // of the four blocks, those outside the cache
-        };
-        auto look = [&](int32_t x) {
-            const int32_t b = t.block0 + 4 * x;
-            const int32_t b0 = block_id(t, b), b1 = block_id(t, b + 1), b2 = block_id(t, b + 2), b3 = block_id(t, b + 3);
-            Step e;
-            e.own = uniform(wave < 2 ? (wave == 0 ? b0 : b1) : (wave == 2 ? b2 : b3));
-            e.bad = (bad_block(b0) ? 1u : 0u) | (bad_block(b1) ? 2u : 0u) | (bad_block(b2) ? 4u : 0u) | (bad_block(b3) ? 8u : 0u);
-            return e;
-        };
-        auto keys_at = [&](int32_t x) { return tile + ((x - t.s0) & 1) * kKeys; };
-        auto values_at = [&](int32_t x) { return tile + 2 * kKeys + ((x - t.s0) & 1) * kKeys; };
-        auto issue_keys = [&](int32_t x, const Step& e) {
-            load_keys(t, t.block0 + 4 * x + wave, e.own, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow));
-        };
-        auto issue_values = [&](int32_t x, const Step& e) {
-            load_values(t, t.block0 + 4 * x + wave, e.own, values_at(x) + wave * (RK_BLOCK_TOKENS * kRow));
-        };
-        // the x-th product's piece of the keys, or values, in a stage; what differs by constants is added by the reads
-        struct Keys {
-            uint32_t at[kTurn / 2];
-        };
-        struct Values {
-            uint32_t at[kTurn / 4], at8[kTurn / 4];  // (of rows 8 further, less those rows)
-        };
-        auto keys_in = [&](uint32_t at) {
-            Keys k;
-#pragma unroll
-            for (int x = 0; x < kTurn / 2; ++x) k.at[x] = at + k_read[x];
-            return k;
-        };
-        auto values_in = [&](uint32_t at) {
-            Values v;
-#pragma unroll
-            for (int x = 0; x < kTurn / 4; ++x) {
-                v.at[x] = at + v_read[x];
-                v.at8[x] = v.at[x] ^ 16 * turn(8);
-            }
-            return v;
-        };
-        auto key_piece = [&](const Keys& k, int x) {
-            const int kt = x & 1, ks = x >> 1;
-            return lds_read16(k.at[ks % (kTurn / 2)] + (uint32_t)(kt * 32 * kRow + ks / (kTurn / 2) * (16 * kTurn)));
-        };
-        auto value_piece = [&](const Values& v, int x) {
-            constexpr int n = kTurn / 4;
-            const int d = x % DT, kk = x / DT;
-            const uint32_t y = (uint32_t)(d / n * (16 * kTurn) + 16 * kk * kRow);
-            const u32x2 lo = lds_read_columns(v.at[d % n] + y), up = lds_read_columns(v.at8[d % n] + y + 8 * kRow);
-            return u32x4{lo.x, lo.y, up.x, up.y};
-        };
-        u32x4 q[KS];
-        auto scores = [&](uint32_t stage, f32x16* sc) {
-            const Keys at = keys_in(stage);
-            u32x4 k[kAhead];
-            sc[0] = sc[1] = f32x16{};
-#pragma unroll
-            for (int x = 0; x < kAhead; ++x) k[x] = key_piece(at, x);
-#pragma unroll
-            for (int x = 0; x < 2 * KS; ++x) {
-                sc[x & 1] = mfma32<Half>(k[x % kAhead], q[x >> 1], sc[x & 1]);
-                if (x + kAhead < 2 * KS) k[x % kAhead] = key_piece(at, x + kAhead);
-            }
-        };
-        auto highest = [&](const f32x16* sc) {
-            float top = sc[0][0];
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = larger(top, sc[kt][i]);
-            return top;
-        };
-        auto follow = [&](float top) {
-            if (__any(strays(top * c, m))) {
-                top = larger(top, __shfl_xor(top, 32)) * c;
-                const float nm = divisor(top, m, Half ? l + __shfl_xor(l, 32) : 0.0f);
-                const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - nm);
-                m = nm;
-                l *= keep;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= keep;
-            }
-            return m == -INFINITY ? 0.0f : -m;
-        };
-        auto exponent = [&](const f32x16* sc, int x, int e, float base) {
-            return __builtin_fmaf(sc[x >> 3][2 * (x & 7) + e], c, base);
-        };
-        auto weight = [&](u32x4* w, int x, float a, float b) {
-            l += a + b;
-            w[x >> 2][x & 3] = pack16<Half>(a, b);
-        };
-        // A step whose keys every row sees: sc its scores, top their largest; the next step's into nx.
-        auto open_step = [&](int32_t x, const f32x16* sc, f32x16* nx, float& top) {
-            const float base = follow(top);
-            const Keys ka = keys_in(keys_at(x + 1));
-            constexpr int n = 2 * KS;
-            u32x4 k[kAhead], w[4];
-            nx[0] = nx[1] = f32x16{};
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) k[u] = key_piece(ka, u);
-            float fa = exponent(sc, 0, 0, base), fb = exponent(sc, 0, 1, base), ea = 0.0f, eb = 0.0f;
-#pragma unroll
-            for (int u = 0; u < n; ++u) {
-                __builtin_amdgcn_sched_barrier(0);
-                nx[u & 1] = mfma32<Half>(k[u % kAhead], q[u >> 1], nx[u & 1]);
-                if (u + kAhead < n) k[u % kAhead] = key_piece(ka, u + kAhead);
-#pragma unroll
-                for (int y = u * kPairs / n; y < (u + 1) * kPairs / n; ++y) {
-                    const float na = __builtin_amdgcn_exp2f(fa), nb = __builtin_amdgcn_exp2f(fb);
-                    if (y + 1 < kPairs) {
-                        fa = exponent(sc, y + 1, 0, base);
-                        fb = exponent(sc, y + 1, 1, base);
-                    }
-                    if (y > 0) weight(w, y - 1, ea, eb);
-                    ea = na;
-                    eb = nb;
-                }
-            }
-            // (a wavefront in this product goes first: the other on its SIMD has its weights to compute meanwhile;
-            // whole prompts 1,251 -> 1,214 us)
-            __builtin_amdgcn_s_setprio(1);
-            const Values va = values_in(values_at(x));
-            u32x4 v[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
-            weight(w, kPairs - 1, ea, eb);
-            top = nx[0][0];
-#pragma unroll
-            for (int u = 0; u < 4 * DT; ++u) {
-                __builtin_amdgcn_sched_barrier(0);
-                o[u % DT] = mfma32<Half>(v[u % kAhead], w[u / DT], o[u % DT]);
-                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(va, u + kAhead);
-#pragma unroll
-                for (int y = u * 32 / (4 * DT); y < (u + 1) * 32 / (4 * DT); ++y) top = larger(top, nx[y >> 4][y & 15]);
-            }
-            __builtin_amdgcn_s_setprio(0);
-        };
-        int32_t s = t.s0;
-        Step now, next, then;
-        // Step s + 1's keys and step s's values are there, and everyone has read what came before; the loads of those
-        // after them begin.
-        auto arrive = [&]() {
-            __builtin_amdgcn_s_waitcnt(0);
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (s + 1 < t.s1) {
-                issue_values(s + 1, next);
-                if (s + 2 < t.s1) issue_keys(s + 2, then);
-            }
-        };
-        auto advance = [&]() {
-            ++s;
-            now = next;
-            next = then;
-            then = look(s + 2);
-        };
-        now = look(s);
-        next = look(s + 1);
-        then = look(s + 2);
-        __syncthreads();                             // the LDS is the last tile's until here
-        issue_keys(s, now);
-        issue_values(s, now);
-        if (s + 1 < t.s1) issue_keys(s + 1, next);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = query(t, r, 2 * ks + hi);
-        __builtin_amdgcn_s_waitcnt(0);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        f32x16 sa[2], sb[2];
-        scores(keys_at(s), sa);
-        // the steps whose keys every row sees, if their blocks are good, but the last
-        const int32_t open = (all_see + 1 - t.block0 * RK_BLOCK_TOKENS) / kWideKeys, s_open = open < t.s1 - 1 ? open : t.s1 - 1;
-        float top = highest(sa);
-        while (s + 1 < s_open && !(now.bad | next.bad)) {
-            arrive();
-            open_step(s, sa, sb, top);
-            advance();
-            arrive();
-            open_step(s, sb, sa, top);
-            advance();
-        }
-        for (;;) {
-            arrive();
-            const int32_t key0 = (t.block0 + 4 * s) * RK_BLOCK_TOKENS;
-            const bool masked = key0 + kWideKeys - 1 > all_see;
-            if (masked || now.bad) {
-                if (now.bad) report_bad();
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int x = 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3);
-                        if (key0 + x > last || ((now.bad >> (x >> 4)) & 1)) sa[kt][i] = -INFINITY;
-                    }
-            }
-            const float base = follow(highest(sa));
-            u32x4 w[4];
-#pragma unroll
-            for (int x = 0; x < kPairs; ++x)
-                weight(w, x, __builtin_amdgcn_exp2f(exponent(sa, x, 0, base)), __builtin_amdgcn_exp2f(exponent(sa, x, 1, base)));
-            const uint32_t va = values_at(s);
-            if (masked && t.mask) {
-                // A value that is not finite must not meet the weight of 0 of a row that does not see it: such values
-                // are added to the rows that do, and are 0 in the product.  (All wavefronts decide alike.)
-                u16x2 most = {0, 0};
-#pragma unroll 4
-                for (int x = lane; x < kWideKeys * NC; x += 64) most = without_sign(most, lds_read16(va + 16 * x));
-                if (__any(not_finite<Half>(__builtin_bit_cast(uint32_t, most)))) {
-#pragma unroll 1
-                    for (int x = 0; x < kWideKeys; ++x) {
-                        const bool sees = key0 + x <= last;
-#pragma unroll
-                        for (int d = 0; d < DT; ++d)
-#pragma unroll
-                            for (int g = 0; g < 4; ++g) {
-                                __builtin_amdgcn_sched_barrier(0);
-                                const uint32_t piece = (uint32_t)(4 * d + g) ^ turn(x & 15);
-                                const u32x2 v = lds_read8(va + x * kRow + (piece << 4) + 8 * hi);
-                                o[d][4 * g] += only_odd<Half>(sees, v.x & 0xffffu);
-                                o[d][4 * g + 1] += only_odd<Half>(sees, v.x >> 16);
-                                o[d][4 * g + 2] += only_odd<Half>(sees, v.y & 0xffffu);
-                                o[d][4 * g + 3] += only_odd<Half>(sees, v.y >> 16);
-                            }
-                    }
-                    __builtin_amdgcn_s_waitcnt(0xc07f);              // (lgkmcnt 0: loads to LDS stay under way)
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                    for (int x = 64 * wave + lane; x < kWideKeys * NC; x += kThreads) {
-                        const u32x4 v = lds_read16(va + 16 * x);
-                        lds_write16(va + 16 * x, u32x4{finite_or_zero<Half>(v.x), finite_or_zero<Half>(v.y),
-                                                       finite_or_zero<Half>(v.z), finite_or_zero<Half>(v.w)});
-                    }
-                    __builtin_amdgcn_s_waitcnt(0xc07f);
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                }
-            }
-            const Values vs = values_in(va);
-            u32x4 v[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(vs, u);
-#pragma unroll
-            for (int u = 0; u < 4 * DT; ++u) {
-                __builtin_amdgcn_sched_barrier(0);
-                o[u % DT] = mfma32<Half>(v[u % kAhead], w[u / DT], o[u % DT]);
-                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(vs, u + kAhead);
-            }
-            if (s + 1 >= t.s1) break;
-            scores(keys_at(s + 1), sa);
-            advance();
-        }
+        const int hi = lane >> 5;
         l += __shfl_xor(l, 32);
         // Out through LDS, so that whole rows are written: a lane's own pieces of a row are 8 or 16 bytes each, of 32 rows at a
         // time.  The keys' stages are free: everyone has read the last keys.
@@ -880,256 +427,11 @@ struct Attend {
         }
     }
 
-    // ---------------------------------------------------------------- up to 16 NQ rows, 32 keys a wavefront
-    //
-    // What bounds few rows is the reading of keys and values, so each wavefront takes keys of its own, with no
-    // barrier: while it computes on the keys of a step its values are still under way, and the next step's keys
-    // follow as soon as this step's are in registers.  The wavefronts' results are joined through LDS; of few keys a
-    // wavefront does a tile alone.  Measured: 5 requests of 60,000-131,072 tokens, 16 / 4 heads of 128, 198 us for 1.01 GB, 5.1 TB/s; 128 of
-    // 2,048 tokens, 8 key heads, 215 us, 5.0 TB/s; one of 8,192 tokens 21 us, of 100 tokens 12 us, both waits one after the
-    // other (lengths, block numbers, keys, join).  (Kernels in a trace.)
-    template <int NQ, bool Solo>
-    __device__ void narrow(const Tile& t)
+    // A narrow tile's results, the wavefronts' joined, or a solo one's; keys: where the wavefront's own LDS begins.
+    template <int NQ, bool Solo, int DT>
+    __device__ __forceinline__ void narrow_out(const Tile& t, f32x4 (&o)[NQ][DT], float (&m)[NQ], float (&l)[NQ], uint32_t keys, int lane) const
     {
-        constexpr int KS = DP / 32, DT = DP / 16, NB = kNarrowKeys<Fp4> / RK_BLOCK_TOKENS;    // blocks of a step
-        const int lane = afresh(threadIdx.x & 63);
         const int g = lane >> 4, col = lane & 15;
-        u32x4 q[NQ][KS];
-        int32_t last[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            const int32_t r = 16 * n + col;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query(t, r, Fp4 ? piece_of(ks, g) : 4 * ks + g);
-            last[n] = t.keys_end - 1;
-            if (t.mask) {
-                const int32_t pos = t.pos + token_of(r);
-                last[n] = pos < last[n] ? pos : last[n];
-            }
-        }
-        const int32_t all_see = t.mask ? (t.pos < t.keys_end - 1 ? t.pos : t.keys_end - 1) : t.keys_end - 1;
-        f32x4 o[NQ][DT];
-        float m[NQ], l[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[n][d] = f32x4{};
-            m[n] = -INFINITY;
-            l[n] = 0.0f;
-        }
-        uint32_t k_read[kTurn / 4], v_read[kTurn / 2];
-#pragma unroll
-        for (int x = 0; x < kTurn / 4; ++x) k_read[x] = col * kRow + (((4 * x + g) ^ turn(col)) << 4);
-        {
-            const uint32_t vr = 4 * g + (col >> 2);
-#pragma unroll
-            for (int x = 0; x < kTurn / 2; ++x)
-                v_read[x] = vr * kRow + (((2 * x + ((lane & 3) >> 1)) ^ turn(vr)) << 4) + 8 * (lane & 1);
-        }
-        // (of a cache in 4 bits keys stay in registers, and all of the wavefront's LDS is the values')
-        const uint32_t keys = tile + wave * (64 * kRow), vals = Fp4 ? keys : keys + 32 * kRow;
-        // this wavefront's steps: of each 4 NB blocks (of a workgroup's tile) NB from NB wave on, or all of them
-        constexpr int kKeys = kKeysOf<Fp4>[Solo ? kSolo : kNarrow], kBlocks = kKeys / RK_BLOCK_TOKENS;
-        const int32_t first_block = t.block0 + (Solo ? 0 : NB * wave);
-        int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kKeys - 1) / kKeys;
-        s1 = s1 < t.s1 ? s1 : t.s1;
-        int32_t s = t.s0, id[NB], later[NB];
-        auto ids = [&](int32_t* to, int32_t x) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) to[b] = block_id(t, first_block + kBlocks * x + b);
-        };
-        uint32_t bad = 0, next_bad = 0;
-        Codes k_raw[Fp4 ? NB : 1], v_raw[Fp4 ? NB : 1];
-        auto issue_keys = [&](int32_t x) {
-            next_bad = 0;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                if constexpr (Fp4) k_raw[b] = codes_of(p.kc, t, first_block + kBlocks * x + b, id[b], k_at, ks_at);
-                else load_keys(t, first_block + kBlocks * x + b, id[b], keys + b * (RK_BLOCK_TOKENS * kRow));
-                next_bad |= (bad_block(id[b]) ? 1u : 0u) << b;
-            }
-            if constexpr (Fp4) __builtin_amdgcn_sched_barrier(0);
-        };
-        auto issue_values = [&](int32_t x, const int32_t* which) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                if constexpr (Fp4) v_raw[b] = codes_of(p.vc, t, first_block + kBlocks * x + b, which[b], v_at, vs_at);
-                else load_values(t, first_block + kBlocks * x + b, which[b], vals + b * (RK_BLOCK_TOKENS * kRow));
-            }
-            if constexpr (Fp4) __builtin_amdgcn_sched_barrier(0);
-        };
-        auto scores = [&](f32x4 (*sc)[NB]) {
-#pragma unroll
-            for (int kt = 0; kt < NB; ++kt) {
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) sc[n][kt] = f32x4{};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    u32x4 k;
-                    if constexpr (Fp4) k = k_raw[kt].template values<Half>(ks);
-                    else k = lds_read16(keys + k_read[ks % (kTurn / 4)] +
-                                        (uint32_t)(kt * 16 * kRow + ks / (kTurn / 4) * (16 * kTurn)));
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) sc[n][kt] = mfma16<Half>(k, q[n][ks], sc[n][kt]);
-                }
-            }
-        };
-        auto weights = [&](f32x4 (*sc)[NB], u32x4 (*w)[NB / 2]) {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                float top = sc[n][0][0];
-#pragma unroll
-                for (int kt = 0; kt < NB; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) top = larger(top, sc[n][kt][i]);
-                if (__any(strays(top * c, m[n]))) {
-                    top = larger(top, __shfl_xor(top, 16));
-                    top = larger(top, __shfl_xor(top, 32)) * c;
-                    float sum = 0.0f;
-                    if constexpr (Half) {
-                        sum = l[n] + __shfl_xor(l[n], 16);
-                        sum += __shfl_xor(sum, 32);
-                    }
-                    const float nm = divisor(top, m[n], sum);
-                    const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[n] - nm);
-                    m[n] = nm;
-                    l[n] *= keep;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
-                }
-                const float base = m[n] == -INFINITY ? 0.0f : -m[n];
-#pragma unroll
-                for (int kt = 0; kt < NB; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i], c, base));
-                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i + 1], c, base));
-                        l[n] += x + y;
-                        w[n][kt / 2][2 * (kt % 2) + (i >> 1)] = pack16<Half>(x, y);
-                    }
-            }
-        };
-        auto values = [&](int d, int c) {
-            const uint32_t x = vals + c * (32 * kRow) + v_read[d % (kTurn / 2)] + (uint32_t)(d / (kTurn / 2) * (16 * kTurn));
-            const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
-            return u32x4{lo.x, lo.y, up.x, up.y};
-        };
-        // (vector memory operations end in the order of their issue: the step's keys are there when only its values'
-        // loads are under way, its values when only the next keys' are)
-        auto wait_keys = [&]() {
-            if constexpr (!Fp4) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
-        };
-        auto keys_read = [&]() {
-            if constexpr (!Fp4) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the keys are in registers
-            bad = next_bad;
-            if (s + 1 < s1) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) id[b] = later[b];
-                issue_keys(s + 1);
-                ids(later, s + 2);
-            }
-        };
-        auto wait_values = [&]() {
-            if constexpr (Fp4) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) place_values(v_raw[b], vals + b * (RK_BLOCK_TOKENS * kRow));
-                if (s + 1 < s1) issue_values(s + 1, id);
-            } else if (s + 1 < s1) {
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
-            } else {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            }
-        };
-        auto values_read = [&]() {
-            if constexpr (Fp4) return;
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the values are in registers
-            if (s + 1 < s1) issue_values(s + 1, id);
-        };
-        if constexpr (Solo) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the LDS is the last tile's until here
-        else __syncthreads();
-        if (s < s1) {
-            ids(id, s);
-            issue_keys(s);
-            issue_values(s, id);
-            ids(later, s + 1);
-        }
-        const int32_t seen = all_see + 1 - first_block * RK_BLOCK_TOKENS - kNarrowKeys<Fp4>;       // the last step's first key that all see
-        const int32_t open = seen < 0 ? 0 : seen / kKeys + 1, s_open = open < s1 ? open : s1;
-        for (; s < s_open && !next_bad; ++s) {
-            f32x4 sc[NQ][NB];
-            u32x4 w[NQ][NB / 2];
-            wait_keys();
-            scores(sc);
-            keys_read();
-            weights(sc, w);
-            wait_values();
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int c = 0; c < NB / 2; ++c) {
-                    const u32x4 v = values(d, c);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
-                }
-            values_read();
-        }
-        for (; s < s1; ++s) {
-            const int32_t key0 = (first_block + kBlocks * s) * RK_BLOCK_TOKENS;
-            const bool masked = key0 + kNarrowKeys<Fp4> - 1 > all_see;
-            f32x4 sc[NQ][NB];
-            u32x4 w[NQ][NB / 2];
-            wait_keys();
-            scores(sc);
-            keys_read();
-            if (bad) report_bad();
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int kt = 0; kt < NB; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
-            weights(sc, w);
-            wait_values();
-            if (masked && t.mask && t.tokens > 1) {                      // (as for wide tiles, of values of the wavefront's own)
-                u16x2 most = {0, 0};
-#pragma unroll 4
-                for (int x = lane; x < kNarrowKeys<Fp4> * NC; x += 64) most = without_sign(most, lds_read16(vals + 16 * x));
-                if (__any(not_finite<Half>(__builtin_bit_cast(uint32_t, most)))) {
-#pragma unroll 1
-                    for (int x = 0; x < kNarrowKeys<Fp4>; ++x)
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            __builtin_amdgcn_sched_barrier(0);
-                            const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ turn(x & 15);
-                            const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
-#pragma unroll
-                            for (int n = 0; n < NQ; ++n) {
-                                const bool sees = key0 + x <= last[n];
-                                o[n][d][0] += only_odd<Half>(sees, v.x & 0xffffu);
-                                o[n][d][1] += only_odd<Half>(sees, v.x >> 16);
-                                o[n][d][2] += only_odd<Half>(sees, v.y & 0xffffu);
-                                o[n][d][3] += only_odd<Half>(sees, v.y >> 16);
-                            }
-                        }
-                    for (int x = lane; x < kNarrowKeys<Fp4> * NC; x += 64) {
-                        const u32x4 v = lds_read16(vals + 16 * x);
-                        lds_write16(vals + 16 * x, u32x4{finite_or_zero<Half>(v.x), finite_or_zero<Half>(v.y),
-                                                         finite_or_zero<Half>(v.z), finite_or_zero<Half>(v.w)});
-                    }
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                }
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int c = 0; c < NB / 2; ++c) {
-                    const u32x4 v = values(d, c);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
-                }
-            values_read();
-        }
         constexpr int kRows = 16 * NQ;
         if constexpr (Solo) {
             // out through LDS, as of wide tiles; all of it is free
@@ -1263,10 +565,10 @@ struct Segment {
     uint64_t pair, cost;                     // cost of a pair (or tile), and in all
 };
 
-template <bool Fp4>
+template <class A>
 __device__ __forceinline__ int32_t steps_for(int64_t keys, int kind)
 {
-    const int32_t per = kind == kWide ? kKeysOf<Fp4>[kWide] : kind == kNarrow ? kKeysOf<Fp4>[kNarrow] : kKeysOf<Fp4>[kSolo];
+    const int32_t per = kind == kWide ? kKeysOf<A>[kWide] : kind == kNarrow ? kKeysOf<A>[kNarrow] : kKeysOf<A>[kSolo];
     return keys > 0 ? (int32_t)((keys + per - 1) / per) : 1;
 }
 
@@ -1286,7 +588,7 @@ __device__ __forceinline__ int32_t steps_before(uint64_t length, int32_t steps)
     return n < (uint64_t)steps ? (int32_t)n : steps;
 }
 
-template <bool Fp4>
+template <class A>
 __device__ __forceinline__ Segment own_segment(const Request& r, const AttendArgs& p)
 {
     Segment s{};
@@ -1298,19 +600,19 @@ __device__ __forceinline__ Segment own_segment(const Request& r, const AttendArg
     if (s.tokens == 0) return s;
     s.tiles = (s.tokens + s.per - 1) / s.per;
     if (s.tiles == 1) {
-        s.steps0 = steps_for<Fp4>(own, s.kind);
+        s.steps0 = steps_for<A>(own, s.kind);
         s.pair = s.cost = extent(s.steps0, s.kind);
     } else {
         s.grows = true;
-        s.steps0 = steps_for<Fp4>(own - s.tokens + s.per, kWide);
-        const int32_t last = steps_for<Fp4>(own - s.tokens + (int64_t)s.tiles * s.per, kWide);
+        s.steps0 = steps_for<A>(own - s.tokens + s.per, kWide);
+        const int32_t last = steps_for<A>(own - s.tokens + (int64_t)s.tiles * s.per, kWide);
         s.pair = extent(s.steps0, kWide) + extent(last, kWide) + 2 * kStepCost[kWide];
         s.cost = s.pair * ((s.tiles + 1) / 2);
     }
     return s;
 }
 
-template <bool Fp4>
+template <class A>
 __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks, const AttendArgs& p)
 {
     Segment s{};
@@ -1319,7 +621,7 @@ __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks
     s.kind = s.rows > kNarrowRows ? kWide : blocks * RK_BLOCK_TOKENS > p.solo_most ? kNarrow : kSolo;
     s.per = s.kind == kWide ? p.wide_tokens : s.tokens;
     s.tiles = (s.tokens + s.per - 1) / s.per;
-    s.steps0 = steps_for<Fp4>((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
+    s.steps0 = steps_for<A>((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
     s.pair = extent(s.steps0, s.kind);
     s.cost = s.pair * s.tiles;
     return s;
@@ -1349,12 +651,12 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         bool prefix = false;
         uint64_t before = 0;
         if (r.end) {
-            sg = prefix_segment<A::kFp4>(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, p);
+            sg = prefix_segment<A>(uniform(req[r.end - 1].q0 + req[r.end - 1].tokens) - r.q0, r.shared, p);
             before = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             prefix = off < before;
         }
         if (!prefix) {
-            sg = own_segment<A::kFp4>(r, p);
+            sg = own_segment<A>(r, p);
             const uint64_t own = sg.kind == K ? sg.cost * (uint64_t)a.Hkv : 0;
             off -= before;
             if (off >= own) {                // on to the next request
@@ -1373,7 +675,7 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
         if (K == kWide && sg.grows) {
             auto steps_of = [&](int32_t k) {
                 const int64_t seen = (int64_t)(k + 1) * sg.per < sg.tokens ? (int64_t)(k + 1) * sg.per : sg.tokens;
-                return steps_for<A::kFp4>((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWide);
+                return steps_for<A>((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWide);
             };
             const int32_t k = sg.tiles - 1 - j;
             const uint64_t first = extent(steps_of(j), kWide);
@@ -1456,14 +758,13 @@ __device__ __forceinline__ bool spread(uint32_t& at, uint32_t n, uint32_t of)
 // that only the device knows: 4-6 us, as long as another launch that told them would take.  Each kind has a line of its own, so
 // that a workgroup keeps to one kind's code; workgroups of different kinds lie side by side on a CU, where one waits for memory while the other
 // computes (128 requests on one prefix 86 -> 83 us, groups of 200 64 -> 62 us against kind after kind).
-template <int DP, bool Half, bool Fp4>
-__global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(AttendArgs p)
+template <class A>
+__global__ __launch_bounds__(kThreads, A::kHead <= 128 ? 2 : 1) void attend_kernel(AttendArgs p)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
     __shared__ float s_join[2 * kWaves * kNarrowRows];
     __shared__ uint64_t s_tmp[4 * kWaves], s_off[kWaves];
     __shared__ int32_t s_i[kWaves], s_bad;
-    using A = Attend<DP, Half, Fp4>;
     const rk_attention& a = p.a;
     const int tid = threadIdx.x;
     const int32_t B = p.n, G = p.G;
@@ -1583,7 +884,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
             // share 5 blocks stay apart, for 141 us, 134 when no groups are named.
             const int64_t n = m.end - f, tokens = req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0, rows = tokens * G;
             if (rows == 0 || rows >= kWideRows * n) continue;
-            const Segment sg = prefix_segment<Fp4>((int32_t)tokens, m.lent, p);
+            const Segment sg = prefix_segment<A>((int32_t)tokens, m.lent, p);
             const int64_t apart = n * m.lent * (rows > kNarrowRows * n ? 2 : 1), costs = sg.kind == kSolo ? 1 : 4;    // in quarters
             if ((int64_t)sg.cost * costs + 4 * kJoinCost * n >= apart) continue;
             req[i].shared = m.lent;
@@ -1602,10 +903,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 #pragma unroll
             for (int k = 0; k < 3; ++k) x.of[k] += sg.kind == k ? sg.cost * (uint64_t)a.Hkv : 0;
         };
-        add(own_segment<Fp4>(req[i], p));
+        add(own_segment<A>(req[i], p));
         if (req[i].end) {
             const Request& l = req[req[i].end - 1];
-            add(prefix_segment<Fp4>(l.q0 + l.tokens - req[i].q0, req[i].shared, p));
+            add(prefix_segment<A>(l.q0 + l.tokens - req[i].q0, req[i].shared, p));
         }
     };
     uint32_t together = 0;
@@ -1684,7 +985,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attend_kernel(Att
 // lane.  The parts' weights come first, a lane each; then their values, several loads under way at a time.  Waiting for
 // loads is all that bounds it (4 us with nothing to join, 8-10 us for decoding batches), but of the rows of whole prompts'
 // 500 cut tiles (30 us for 100 MB).
-template <int DP, bool Half, bool Fp4>
+template <class A, int DP, bool Half>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks, int32_t shared_chunks)
 {
     const rk_attention& a = p.a;
@@ -1827,7 +1128,7 @@ inline AttendLayout attend_layout(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
     return L;
 }
 
-template <int DP, bool Half, bool Fp4>
+template <class A, int DP, bool Half>
 static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
 {
     const int64_t rows = p.a.T * p.G;
@@ -1838,11 +1139,11 @@ static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
         // With few tiles, one wavefront with all of a tile's keys would be what the others wait for (16 requests of 300 tokens
         // on 2 key heads 25 us, 21 by workgroups; 64 of 128 on 8 22 us, 27 by workgroups).
         p.solo_most = (int64_t)p.n * p.a.Hkv > grid / 2 ? kSoloMost : 0;
-        hipLaunchKernelGGL((attend_kernel<DP, Half, Fp4>), dim3((unsigned)grid), dim3(kThreads), lds_bytes(DP, p.n), s, p);
+        hipLaunchKernelGGL((attend_kernel<A>), dim3((unsigned)grid), dim3(kThreads), lds_bytes(DP, p.n), s, p);
         int rc = hip_check(hipGetLastError(), "rk_prefix_attention launch");
         if (rc) return rc;
         const int64_t blocks = (int64_t)grid * chunks + (p.a.group_off ? (int64_t)p.n * p.a.Hkv * shared_chunks : 0);
-        hipLaunchKernelGGL((join_kernel<DP, Half, Fp4>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, grid, chunks,
+        hipLaunchKernelGGL((join_kernel<A, DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, grid, chunks,
                            shared_chunks);
         rc = hip_check(hipGetLastError(), "rk_prefix_attention join launch");
         if (rc) return rc;
@@ -1850,14 +1151,14 @@ static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
     return RK_OK;
 }
 
-template <bool Half, bool Fp4>
+template <template <int, bool> class Tiles, bool Half>
 static int launch_of(AttendArgs& p, int32_t grid, hipStream_t s)
 {
     switch (head_size(p.a.D)) {
-    case 64: return launch<64, Half, Fp4>(p, grid, s);
-    case 128: return launch<128, Half, Fp4>(p, grid, s);
-    case 192: return launch<192, Half, Fp4>(p, grid, s);
-    default: return launch<256, Half, Fp4>(p, grid, s);
+    case 64: return launch<Tiles<64, Half>, 64, Half>(p, grid, s);
+    case 128: return launch<Tiles<128, Half>, 128, Half>(p, grid, s);
+    case 192: return launch<Tiles<192, Half>, 192, Half>(p, grid, s);
+    default: return launch<Tiles<256, Half>, 256, Half>(p, grid, s);
     }
 }
 
@@ -1898,8 +1199,8 @@ inline bool attention_arrays(const rk_attention& a)
     return a.q && a.out && a.kv_len && a.q_off && (a.table_stride == 0 || a.tables);
 }
 
-// The call whose arguments hold; kc, vc: the caches, where they are held in 4 bits.
-template <bool Fp4>
+// The call whose arguments hold; Tiles: the class of its tiles; kc, vc: the caches, where they are held in 4 bits, or NULL.
+template <template <int, bool> class Tiles>
 static int attention_call(const rk_attention& a, const rk_fp4_cache* kc, const rk_fp4_cache* vc, void* workspace, size_t ws_bytes,
                           void* stream, const char* name)
 {
@@ -1910,7 +1211,7 @@ static int attention_call(const rk_attention& a, const rk_fp4_cache* kc, const r
     uint8_t* ws = (uint8_t*)workspace;
     AttendArgs p{};
     p.a = a;
-    if (Fp4) {
+    if (kc) {
         p.kc = *kc;
         p.vc = *vc;
     }
@@ -1926,7 +1227,7 @@ static int attention_call(const rk_attention& a, const rk_fp4_cache* kc, const r
     p.g_inverse = (uint32_t)((65535 + p.G) / p.G);
     p.shared_rows = L.shared_rows;
     p.shared_tokens = L.shared_tokens;
-    return a.dtype == RK_F16 ? launch_of<true, Fp4>(p, L.grid, (hipStream_t)stream) : launch_of<false, Fp4>(p, L.grid, (hipStream_t)stream);
+    return a.dtype == RK_F16 ? launch_of<Tiles, true>(p, L.grid, (hipStream_t)stream) : launch_of<Tiles, false>(p, L.grid, (hipStream_t)stream);
 }
 
 }  // namespace rk

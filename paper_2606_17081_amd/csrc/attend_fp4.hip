@@ -1,6 +1,664 @@
 // attend_fp4.hip -- rk_prefix_attention_fp4: the entry points, and the kernels of caches held in 4 bits.
 #include "attend.h"
 
+namespace rk {
+
+// Tiles over a cache in 4 bits.
+template <int DP, bool Half>
+struct AttendFp4 : AttendBase<DP, Half> {
+    using Base = AttendBase<DP, Half>;
+    using Base::NC, Base::kRow, Base::kTurn, Base::turn, Base::p, Base::tile, Base::join, Base::wave, Base::G, Base::c;
+    using Base::block_id, Base::rows_of, Base::bad_block, Base::report_bad, Base::token_of, Base::strays, Base::divisor;
+    // Keys of a wavefront in a narrow step: a key is a quarter of the bytes of a 16-bit one, and as many should be under way.
+    static constexpr int kNarrowKeys = DP <= 128 ? 64 : 32;
+
+    using Base::Base;
+
+    // A lane loads a quarter of a row of a block: in each round a share (32 values of one power of two), in the last, of a DP that is
+    // no multiple of 128, half a share.
+    static constexpr int kShares = DP / 32, kRounds = (kShares + 3) / 4, kPieces = DP / 32;   // (kPieces: of 8 values, a lane's)
+    static constexpr bool kHalfRound = kShares % 4 != 0;
+    static constexpr uint32_t kNowhere = 0x80000000u;        // past any block's end: what is loaded there is 0
+
+    // Which of a row's pieces of 8 values quarter j has as its ks-th.
+    static __device__ __forceinline__ int piece_of(int ks, int j)
+    {
+        if (kHalfRound && ks / 4 == kRounds - 1) return 4 * (ks / 4 * 4 + j / 2) + 2 * (j & 1) + ks % 4;
+        return 4 * (ks / 4 * 4 + j) + ks % 4;
+    }
+
+    // Byte offsets in a block of what a lane loads of it, quarter j of row r: codes and powers of two.
+    struct Places {
+        uint32_t codes[kRounds], powers[kRounds];
+    };
+    __device__ __forceinline__ Places places(const rk_fp4_cache& cache, uint32_t r, uint32_t j) const
+    {
+        Places at;
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const bool half = kHalfRound && i == kRounds - 1;
+            const uint32_t share = 4 * i + (half ? j / 2 : j);
+            const bool there = 32 * share < (uint32_t)p.a.D;
+            at.codes[i] = there ? r * (uint32_t)cache.cs.token + 16 * share + (half ? 8 * (j & 1) : 0) : kNowhere;
+            at.powers[i] = there ? r * (uint32_t)cache.ss.token + share : kNowhere;
+        }
+        return at;
+    }
+
+    // Piece x of the row's query, its sign turned with the scale's; rows that are not there and pieces behind D are 0.  The load is made
+    // in any case, from a place that is there: with a branch around each of a row's loads, values that two of them share were
+    // computed for the lanes of one side alone (D = 256, 17 rows: results of no meaning).
+    __device__ __forceinline__ u32x4 query_of(const Tile& t, int32_t r, int32_t piece) const
+    {
+        const int32_t tok = token_of(r), head = r - tok * G;
+        const bool there = tok < t.tokens && 8 * piece < p.a.D;
+        const uint32_t mask = there ? 0xffffffffu : 0u, sign = p.a.scale < 0.0f ? 0x80008000u & mask : 0u;
+        const u32x4 q = *reinterpret_cast<const u32x4*>((const uint16_t*)p.a.q + (t.token + (int64_t)(there ? tok : 0)) * p.a.q_token +
+                                                        (t.head * G + (there ? head : 0)) * p.a.q_head + (there ? 8 * piece : 0));
+        return (q & mask) ^ sign;
+    }
+
+    struct Codes {
+        u32x4 w[kRounds];
+        uint32_t power[kRounds];
+        // the lane's ks-th piece in 16 bits, which hold the values exactly
+        __device__ __forceinline__ u32x4 values(int ks) const
+        {
+            return fp4_values<Half>(w[ks / 4][ks % 4], __uint_as_float(power[ks / 4] << 23));
+        }
+    };
+    // The lane's part of block number b of the tile's sequence, block `id` of the cache; 0 in rows behind the tile's keys.
+    __device__ __forceinline__ Codes codes_of(const rk_fp4_cache& cache, const Tile& t, int32_t b, int32_t id, const Places& at) const
+    {
+        const int32_t rows = rows_of(t, b, id), block = rows > 0 ? id : 0, shares = (p.a.D + 31) / 32, last = rows - 1;
+        const Memory codes = memory((const uint8_t*)cache.codes + block * cache.cs.block + t.head * cache.cs.head,
+                                    rows > 0 ? last * (int32_t)cache.cs.token + 16 * shares : 0);
+        const Memory scales = memory((const uint8_t*)cache.scales + block * cache.ss.block + t.head * cache.ss.head,
+                                     rows > 0 ? last * (int32_t)cache.ss.token + shares : 0);
+        Codes x;
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            if (kHalfRound && i == kRounds - 1) {
+                const u32x2 w = load8(codes, at.codes[i]);
+                x.w[i] = u32x4{w.x, w.y, 0u, 0u};
+            } else {
+                x.w[i] = load16(codes, at.codes[i]);
+            }
+            x.power[i] = load1(scales, at.powers[i]);
+        }
+        return x;
+    }
+    // The ks-th piece of a lane's quarter (lane % 4) of row lane / 4, and all of them, as 16-bit values to a block's place in LDS.
+    __device__ __forceinline__ void place_piece(const Codes& x, int ks, uint32_t lds, uint32_t lane) const
+    {
+        const uint32_t r = lane >> 2;
+        lds_write16(lds + r * kRow + (((uint32_t)piece_of(ks, lane & 3) ^ turn(r)) << 4), x.values(ks));
+    }
+    __device__ __forceinline__ void place_values(const Codes& x, uint32_t lds, uint32_t lane) const
+    {
+#pragma unroll
+        for (int ks = 0; ks < kPieces; ++ks) place_piece(x, ks, lds, lane);
+    }
+
+    // ---------------------------------------------------------------- up to 128 rows, 32 a wavefront
+    //
+    // As over 16-bit caches: scores are computed transposed, keys x rows, and the weights lie in registers in the order in which the
+    // product with the values takes them.
+    __device__ void wide(const Tile& t)
+    {
+        constexpr int KS = DP / 16, DT = DP / 32;
+        const int lane = afresh(threadIdx.x & 63);
+        const int hi = lane >> 5, r = 32 * wave + (lane & 31);
+        int32_t last = t.keys_end - 1;               // the last position that the row sees
+        if (t.mask) {
+            const int32_t pos = t.pos + token_of(r);
+            last = pos < last ? pos : last;
+        }
+        const int32_t all_see = t.mask ? (t.pos < t.keys_end - 1 ? t.pos : t.keys_end - 1) : t.keys_end - 1;
+        f32x16 o[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+        float m = -INFINITY, l = 0.0f;               // m: log2 of the weights' common divisor
+        // LDS addresses in a stage, less what the unrolled loops add
+        uint32_t k_read[kTurn / 2], v_read[kTurn / 4];
+        {
+            const uint32_t row = lane & 31, vr = 4 * hi + ((lane & 15) >> 2), vp = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+            for (int x = 0; x < kTurn / 2; ++x) k_read[x] = row * kRow + (((2 * x + hi) ^ turn(row & 15)) << 4);
+#pragma unroll
+            for (int x = 0; x < kTurn / 4; ++x) v_read[x] = vr * kRow + (((4 * x + vp) ^ turn(vr)) << 4) + 8 * (lane & 1);
+        }
+        constexpr uint32_t kKeys = kWideKeys * kRow;   // bytes of a step's keys; two of them, then two steps' values
+        // Keys come two steps ahead, values one: while a step's weights are computed, the products of the next step's
+        // scores run beside them (whole prompts 1,440 -> 1,360 us).  Pieces are read from LDS kAhead products before the one that
+        // takes them: 3 are as good, 6 spill registers (whole prompts 1,230 -> 1,500 us).
+        constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
+        struct Step {
+            int32_t own;                             // this wavefront's block
+            uint32_t bad;                            // of the four blocks, those outside the cache
+        };
+        auto look = [&](int32_t x) {
+            const int32_t b = t.block0 + 4 * x;
+            const int32_t b0 = block_id(t, b), b1 = block_id(t, b + 1), b2 = block_id(t, b + 2), b3 = block_id(t, b + 3);
+            Step e;
+            e.own = uniform(wave < 2 ? (wave == 0 ? b0 : b1) : (wave == 2 ? b2 : b3));
+            e.bad = (bad_block(b0) ? 1u : 0u) | (bad_block(b1) ? 2u : 0u) | (bad_block(b2) ? 4u : 0u) | (bad_block(b3) ? 8u : 0u);
+            return e;
+        };
+        auto keys_at = [&](int32_t x) { return tile + ((x - t.s0) & 1) * kKeys; };
+        auto values_at = [&](int32_t x) { return tile + 2 * kKeys + ((x - t.s0) & 1) * kKeys; };
+        // Of a cache in 4 bits the codes of keys three steps ahead and of values two are under way to registers; they are
+        // converted into the stages of keys two steps ahead and values one beside the second product, which leaves the vector units idle.
+        Codes k_raw, v_raw;
+        const Places k_at = places(p.kc, lane >> 2, lane & 3), v_at = places(p.vc, lane >> 2, lane & 3);
+        auto issue_keys = [&](int32_t x, const Step& e) {
+            k_raw = codes_of(p.kc, t, t.block0 + 4 * x + wave, e.own, k_at);
+        };
+        auto issue_values = [&](int32_t x, const Step& e) {
+            v_raw = codes_of(p.vc, t, t.block0 + 4 * x + wave, e.own, v_at);
+        };
+        auto put_keys = [&](int32_t x) { place_values(k_raw, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
+        auto put_values = [&](int32_t x) { place_values(v_raw, values_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
+        // the x-th product's piece of the keys, or values, in a stage; what differs by constants is added by the reads
+        struct Keys {
+            uint32_t at[kTurn / 2];
+        };
+        struct Values {
+            uint32_t at[kTurn / 4], at8[kTurn / 4];  // (of rows 8 further, less those rows)
+        };
+        auto keys_in = [&](uint32_t at) {
+            Keys k;
+#pragma unroll
+            for (int x = 0; x < kTurn / 2; ++x) k.at[x] = at + k_read[x];
+            return k;
+        };
+        auto values_in = [&](uint32_t at) {
+            Values v;
+#pragma unroll
+            for (int x = 0; x < kTurn / 4; ++x) {
+                v.at[x] = at + v_read[x];
+                v.at8[x] = v.at[x] ^ 16 * turn(8);
+            }
+            return v;
+        };
+        auto key_piece = [&](const Keys& k, int x) {
+            const int kt = x & 1, ks = x >> 1;
+            return lds_read16(k.at[ks % (kTurn / 2)] + (uint32_t)(kt * 32 * kRow + ks / (kTurn / 2) * (16 * kTurn)));
+        };
+        auto value_piece = [&](const Values& v, int x) {
+            constexpr int n = kTurn / 4;
+            const int d = x % DT, kk = x / DT;
+            const uint32_t y = (uint32_t)(d / n * (16 * kTurn) + 16 * kk * kRow);
+            const u32x2 lo = lds_read_columns(v.at[d % n] + y), up = lds_read_columns(v.at8[d % n] + y + 8 * kRow);
+            return u32x4{lo.x, lo.y, up.x, up.y};
+        };
+        u32x4 q[KS];
+        auto scores = [&](uint32_t stage, f32x16* sc) {
+            const Keys at = keys_in(stage);
+            u32x4 k[kAhead];
+            sc[0] = sc[1] = f32x16{};
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) k[x] = key_piece(at, x);
+#pragma unroll
+            for (int x = 0; x < 2 * KS; ++x) {
+                sc[x & 1] = mfma32<Half>(k[x % kAhead], q[x >> 1], sc[x & 1]);
+                if (x + kAhead < 2 * KS) k[x % kAhead] = key_piece(at, x + kAhead);
+            }
+        };
+        auto highest = [&](const f32x16* sc) {
+            float top = sc[0][0];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = larger(top, sc[kt][i]);
+            return top;
+        };
+        auto follow = [&](float top) {
+            if (__any(strays(top * c, m))) {
+                top = larger(top, __shfl_xor(top, 32)) * c;
+                const float nm = divisor(top, m, Half ? l + __shfl_xor(l, 32) : 0.0f);
+                const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - nm);
+                m = nm;
+                l *= keep;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= keep;
+            }
+            return m == -INFINITY ? 0.0f : -m;
+        };
+        auto exponent = [&](const f32x16* sc, int x, int e, float base) {
+            return __builtin_fmaf(sc[x >> 3][2 * (x & 7) + e], c, base);
+        };
+        auto weight = [&](u32x4* w, int x, float a, float b) {
+            l += a + b;
+            w[x >> 2][x & 3] = pack16<Half>(a, b);
+        };
+        // A step whose keys every row sees: sc its scores, top their largest; the next step's into nx; e2, e3: the blocks of steps
+        // x + 2 and x + 3.
+        auto open_step = [&](int32_t x, const f32x16* sc, f32x16* nx, float& top, const Step& e2, const Step& e3) {
+            const float base = follow(top);
+            const Keys ka = keys_in(keys_at(x + 1));
+            constexpr int n = 2 * KS;
+            u32x4 k[kAhead], w[4];
+            nx[0] = nx[1] = f32x16{};
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) k[u] = key_piece(ka, u);
+            float fa = exponent(sc, 0, 0, base), fb = exponent(sc, 0, 1, base), ea = 0.0f, eb = 0.0f;
+#pragma unroll
+            for (int u = 0; u < n; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                nx[u & 1] = mfma32<Half>(k[u % kAhead], q[u >> 1], nx[u & 1]);
+                if (u + kAhead < n) k[u % kAhead] = key_piece(ka, u + kAhead);
+#pragma unroll
+                for (int y = u * kPairs / n; y < (u + 1) * kPairs / n; ++y) {
+                    const float na = __builtin_amdgcn_exp2f(fa), nb = __builtin_amdgcn_exp2f(fb);
+                    if (y + 1 < kPairs) {
+                        fa = exponent(sc, y + 1, 0, base);
+                        fb = exponent(sc, y + 1, 1, base);
+                    }
+                    if (y > 0) weight(w, y - 1, ea, eb);
+                    ea = na;
+                    eb = nb;
+                }
+            }
+            // (a wavefront in this product goes first: the other on its SIMD has its weights to compute meanwhile;
+            // whole prompts 1,251 -> 1,214 us)
+            __builtin_amdgcn_s_setprio(1);
+            const Values va = values_in(values_at(x));
+            u32x4 v[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
+            weight(w, kPairs - 1, ea, eb);
+            top = nx[0][0];
+#pragma unroll
+            for (int u = 0; u < 4 * DT; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                o[u % DT] = mfma32<Half>(v[u % kAhead], w[u / DT], o[u % DT]);
+                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(va, u + kAhead);
+#pragma unroll
+                for (int y = u * 32 / (4 * DT); y < (u + 1) * 32 / (4 * DT); ++y) top = larger(top, nx[y >> 4][y & 15]);
+                if (u % 2 == 0 && u / 2 < kPieces) place_piece(v_raw, u / 2, values_at(x + 1) + wave * (RK_BLOCK_TOKENS * kRow), lane);
+                if (u % 2 == 0 && u / 2 >= kPieces) place_piece(k_raw, u / 2 - kPieces, keys_at(x + 2) + wave * (RK_BLOCK_TOKENS * kRow), lane);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            issue_values(x + 2, e2);         // (past the tile's end they bring zeros, to a stage that is not read again)
+            issue_keys(x + 3, e3);
+        };
+        int32_t s = t.s0;
+        uint32_t any_bad = 0;
+        Step now, next, then, far;
+        // Step s + 1's keys and step s's values are there, and everyone has read what came before.
+        auto arrive = [&]() {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        auto advance = [&]() {
+            ++s;
+            now = next;
+            next = then;
+            then = far;
+            far = look(s + 3);
+        };
+        now = look(s);
+        next = look(s + 1);
+        then = look(s + 2);
+        far = look(s + 3);
+        __syncthreads();                             // the LDS is the last tile's until here
+        issue_keys(s, now);
+        issue_values(s, now);
+        put_keys(s);
+        issue_keys(s + 1, next);
+        put_values(s);
+        issue_values(s + 1, next);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = query_of(t, r, 2 * ks + hi);
+        put_keys(s + 1);
+        issue_keys(s + 2, then);
+        arrive();
+        f32x16 sa[2], sb[2];
+        scores(keys_at(s), sa);
+        // the steps whose keys every row sees, if their blocks are good, but the last
+        const int32_t open = (all_see + 1 - t.block0 * RK_BLOCK_TOKENS) / kWideKeys, s_open = open < t.s1 - 1 ? open : t.s1 - 1;
+        float top = highest(sa);
+        while (s + 1 < s_open && !(now.bad | next.bad)) {
+            arrive();
+            open_step(s, sa, sb, top, then, far);
+            advance();
+            arrive();
+            open_step(s, sb, sa, top, then, far);
+            advance();
+        }
+        for (;;) {
+            arrive();
+            const int32_t key0 = (t.block0 + 4 * s) * RK_BLOCK_TOKENS;
+            const bool masked = key0 + kWideKeys - 1 > all_see;
+            if (masked || now.bad) {
+                any_bad |= now.bad;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int x = 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3);
+                        if (key0 + x > last || ((now.bad >> (x >> 4)) & 1)) sa[kt][i] = -INFINITY;
+                    }
+            }
+            const float base = follow(highest(sa));
+            u32x4 w[4];
+#pragma unroll
+            for (int x = 0; x < kPairs; ++x)
+                weight(w, x, __builtin_amdgcn_exp2f(exponent(sa, x, 0, base)), __builtin_amdgcn_exp2f(exponent(sa, x, 1, base)));
+            const uint32_t va = values_at(s);
+            if (masked && t.mask) {
+                // A value that is not finite must not meet the weight of 0 of a row that does not see it: such values
+                // are added to the rows that do, and are 0 in the product.  (All wavefronts decide alike.)
+                u16x2 most = {0, 0};
+#pragma unroll 4
+                for (int x = lane; x < kWideKeys * NC; x += 64) most = without_sign(most, lds_read16(va + 16 * x));
+                if (__any(not_finite<Half>(__builtin_bit_cast(uint32_t, most)))) {
+#pragma unroll 1
+                    for (int x = 0; x < kWideKeys; ++x) {
+                        const bool sees = key0 + x <= last;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) {
+                                __builtin_amdgcn_sched_barrier(0);
+                                const uint32_t piece = (uint32_t)(4 * d + g) ^ turn(x & 15);
+                                const u32x2 v = lds_read8(va + x * kRow + (piece << 4) + 8 * hi);
+                                o[d][4 * g] += only_odd<Half>(sees, v.x & 0xffffu);
+                                o[d][4 * g + 1] += only_odd<Half>(sees, v.x >> 16);
+                                o[d][4 * g + 2] += only_odd<Half>(sees, v.y & 0xffffu);
+                                o[d][4 * g + 3] += only_odd<Half>(sees, v.y >> 16);
+                            }
+                    }
+                    __builtin_amdgcn_s_waitcnt(0xc07f);              // (lgkmcnt 0: loads to LDS stay under way)
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    for (int x = 64 * wave + lane; x < kWideKeys * NC; x += kThreads) {
+                        const u32x4 v = lds_read16(va + 16 * x);
+                        lds_write16(va + 16 * x, u32x4{finite_or_zero<Half>(v.x), finite_or_zero<Half>(v.y),
+                                                       finite_or_zero<Half>(v.z), finite_or_zero<Half>(v.w)});
+                    }
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                }
+            }
+            const Values vs = values_in(va);
+            u32x4 v[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v[u] = value_piece(vs, u);
+#pragma unroll
+            for (int u = 0; u < 4 * DT; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                o[u % DT] = mfma32<Half>(v[u % kAhead], w[u / DT], o[u % DT]);
+                if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(vs, u + kAhead);
+            }
+            if (s + 1 >= t.s1) break;
+            put_values(s + 1);               // (not in the last step: then others write their results there)
+            put_keys(s + 2);
+            issue_values(s + 2, then);
+            issue_keys(s + 3, far);
+            scores(keys_at(s + 1), sa);
+            advance();
+        }
+        this->template wide_out<DT>(t, o, m, l, r, lane);
+        if (any_bad) report_bad();
+    }
+
+    // ---------------------------------------------------------------- up to 16 NQ rows, kNarrowKeys keys a wavefront
+    //
+    // What bounds few rows is the reading of keys and values: each wavefront takes keys of its own, with no barrier.  The codes of
+    // kSets steps are under way to registers, keys in the order in which the product takes them, so that they are converted
+    // there; values pass LDS once they are 16 bits, since the second product takes them by columns.
+    template <int NQ, bool Solo>
+    __device__ void narrow(const Tile& t)
+    {
+        constexpr int KS = DP / 32, DT = DP / 16, NB = kNarrowKeys / RK_BLOCK_TOKENS;     // blocks of a step
+        constexpr int kSets = NQ == 1 || DP < 128 ? 2 : 1;      // steps whose codes are under way or in registers
+        const int lane = afresh(threadIdx.x & 63);
+        const int g = lane >> 4, col = lane & 15;
+        u32x4 q[NQ][KS];
+        int32_t last[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int32_t r = 16 * n + col;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query_of(t, r, piece_of(ks, g));
+            last[n] = t.keys_end - 1;
+            if (t.mask) {
+                const int32_t pos = t.pos + token_of(r);
+                last[n] = pos < last[n] ? pos : last[n];
+            }
+        }
+        const int32_t all_see = t.mask ? (t.pos < t.keys_end - 1 ? t.pos : t.keys_end - 1) : t.keys_end - 1;
+        f32x4 o[NQ][DT];
+        float m[NQ], l[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[n][d] = f32x4{};
+            m[n] = -INFINITY;
+            l[n] = 0.0f;
+        }
+        const Places k_at = places(p.kc, col, g), v_at = places(p.vc, lane >> 2, lane & 3);
+        uint32_t v_read[kTurn / 2];
+        {
+            const uint32_t vr = 4 * g + (col >> 2);
+#pragma unroll
+            for (int x = 0; x < kTurn / 2; ++x)
+                v_read[x] = vr * kRow + (((2 * x + ((lane & 3) >> 1)) ^ turn(vr)) << 4) + 8 * (lane & 1);
+        }
+        const uint32_t vals = tile + wave * (64 * kRow);
+        // this wavefront's steps: of each 4 NB blocks (of a workgroup's tile) NB from NB wave on, or all of them
+        constexpr int kKeys = Solo ? kNarrowKeys : kWaves * kNarrowKeys, kBlocks = kKeys / RK_BLOCK_TOKENS;
+        const int32_t first_block = t.block0 + (Solo ? 0 : NB * wave);
+        int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kKeys - 1) / kKeys;
+        s1 = s1 < t.s1 ? s1 : t.s1;
+        int32_t s = t.s0, id[NB], later[NB];
+        auto ids = [&](int32_t* to, int32_t x) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) to[b] = block_id(t, first_block + kBlocks * x + b);
+        };
+        uint32_t bad = 0, any_bad = 0, next_bad[kSets] = {};
+        Codes k_raw[kSets][NB], v_raw[kSets][NB];
+        auto issue_keys = [&](auto u, int32_t x) {
+            next_bad[u] = 0;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                k_raw[u][b] = codes_of(p.kc, t, first_block + kBlocks * x + b, id[b], k_at);
+                next_bad[u] |= (bad_block(id[b]) ? 1u : 0u) << b;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto issue_values = [&](auto u, int32_t x) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                v_raw[u][b] = codes_of(p.vc, t, first_block + kBlocks * x + b, id[b], v_at);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto scores = [&](auto u, f32x4 (*sc)[NB]) {
+#pragma unroll
+            for (int kt = 0; kt < NB; ++kt) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) sc[n][kt] = f32x4{};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const u32x4 k = k_raw[u][kt].values(ks);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) sc[n][kt] = mfma16<Half>(k, q[n][ks], sc[n][kt]);
+                }
+            }
+        };
+        auto weights = [&](f32x4 (*sc)[NB], u32x4 (*w)[NB / 2]) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                float top = sc[n][0][0];
+#pragma unroll
+                for (int kt = 0; kt < NB; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = larger(top, sc[n][kt][i]);
+                if (__any(strays(top * c, m[n]))) {
+                    top = larger(top, __shfl_xor(top, 16));
+                    top = larger(top, __shfl_xor(top, 32)) * c;
+                    float sum = 0.0f;
+                    if constexpr (Half) {
+                        sum = l[n] + __shfl_xor(l[n], 16);
+                        sum += __shfl_xor(sum, 32);
+                    }
+                    const float nm = divisor(top, m[n], sum);
+                    const float keep = nm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[n] - nm);
+                    m[n] = nm;
+                    l[n] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+                }
+                const float base = m[n] == -INFINITY ? 0.0f : -m[n];
+#pragma unroll
+                for (int kt = 0; kt < NB; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i], c, base));
+                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kt][i + 1], c, base));
+                        l[n] += x + y;
+                        w[n][kt / 2][2 * (kt % 2) + (i >> 1)] = pack16<Half>(x, y);
+                    }
+            }
+        };
+        auto values = [&](int d, int c) {
+            const uint32_t x = vals + c * (32 * kRow) + v_read[d % (kTurn / 2)] + (uint32_t)(d / (kTurn / 2) * (16 * kTurn));
+            const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
+            return u32x4{lo.x, lo.y, up.x, up.y};
+        };
+        auto keys_read = [&](auto u) {
+            bad = next_bad[u];
+            if (s + kSets < s1) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) id[b] = later[b];
+                issue_keys(u, s + kSets);
+                ids(later, s + kSets + 1);
+            }
+        };
+        auto put_values = [&](auto u) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) place_values(v_raw[u][b], vals + b * (RK_BLOCK_TOKENS * kRow), lane);
+            if (s + kSets < s1) issue_values(u, s + kSets);
+        };
+        constexpr std::integral_constant<int, 0> first{};
+        constexpr std::integral_constant<int, kSets - 1> second{};
+        if constexpr (Solo) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the LDS is the last tile's until here
+        else __syncthreads();
+        if (s < s1) {
+            ids(id, s);
+            issue_keys(first, s);
+            issue_values(first, s);
+            if (kSets > 1 && s + 1 < s1) {
+                ids(id, s + 1);
+                issue_keys(second, s + 1);
+                issue_values(second, s + 1);
+            }
+            ids(later, s + kSets);
+        }
+        const int32_t seen = all_see + 1 - first_block * RK_BLOCK_TOKENS - kNarrowKeys;       // the last step's first key that all see
+        const int32_t open = seen < 0 ? 0 : seen / kKeys + 1, s_open = open < s1 ? open : s1;
+        auto open_step = [&](auto u) {           // a step whose keys every row sees
+            f32x4 sc[NQ][NB];
+            u32x4 w[NQ][NB / 2];
+            scores(u, sc);
+            keys_read(u);
+            weights(sc, w);
+            put_values(u);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int c = 0; c < NB / 2; ++c) {
+                    const u32x4 v = values(d, c);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
+                }
+        };
+        auto any_step = [&](auto u) {
+            const int32_t key0 = (first_block + kBlocks * s) * RK_BLOCK_TOKENS;
+            const bool masked = key0 + kNarrowKeys - 1 > all_see;
+            f32x4 sc[NQ][NB];
+            u32x4 w[NQ][NB / 2];
+            scores(u, sc);
+            keys_read(u);
+            any_bad |= bad;
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int kt = 0; kt < NB; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
+            weights(sc, w);
+            put_values(u);
+            if (masked && t.mask && t.tokens > 1) {                      // (as for wide tiles, of values of the wavefront's own)
+                u16x2 most = {0, 0};
+#pragma unroll 4
+                for (int x = lane; x < kNarrowKeys * NC; x += 64) most = without_sign(most, lds_read16(vals + 16 * x));
+                if (__any(not_finite<Half>(__builtin_bit_cast(uint32_t, most)))) {
+#pragma unroll 1
+                    for (int x = 0; x < kNarrowKeys; ++x)
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            const uint32_t piece = (uint32_t)(2 * d + (g >> 1)) ^ turn(x & 15);
+                            const u32x2 v = lds_read8(vals + x * kRow + (piece << 4) + 8 * (g & 1));
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n) {
+                                const bool sees = key0 + x <= last[n];
+                                o[n][d][0] += only_odd<Half>(sees, v.x & 0xffffu);
+                                o[n][d][1] += only_odd<Half>(sees, v.x >> 16);
+                                o[n][d][2] += only_odd<Half>(sees, v.y & 0xffffu);
+                                o[n][d][3] += only_odd<Half>(sees, v.y >> 16);
+                            }
+                        }
+                    for (int x = lane; x < kNarrowKeys * NC; x += 64) {
+                        const u32x4 v = lds_read16(vals + 16 * x);
+                        lds_write16(vals + 16 * x, u32x4{finite_or_zero<Half>(v.x), finite_or_zero<Half>(v.y),
+                                                         finite_or_zero<Half>(v.z), finite_or_zero<Half>(v.w)});
+                    }
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int c = 0; c < NB / 2; ++c) {
+                    const u32x4 v = values(d, c);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
+                }
+        };
+        if constexpr (kSets == 1) {
+            for (; s < s_open && !next_bad[0]; ++s) open_step(first);
+            for (; s < s1; ++s) any_step(first);
+        } else {
+            while (s + 1 < s_open && !(next_bad[0] | next_bad[1])) {
+                open_step(first);
+                ++s;
+                open_step(second);
+                ++s;
+            }
+            while (s < s1) {
+                any_step(first);
+                if (++s == s1) break;
+                any_step(second);
+                ++s;
+            }
+        }
+        this->template narrow_out<NQ, Solo, DT>(t, o, m, l, vals, lane);
+        if (any_bad) report_bad();
+    }
+};
+
+}  // namespace rk
+
 using namespace rk;
 
 extern "C" {
@@ -29,7 +687,7 @@ int rk_prefix_attention_fp4(const rk_attention_fp4* a4, void* workspace, size_t 
         return fail(RK_EINVAL, "%s: NULL array", name);
     if (((uintptr_t)a.q | (uintptr_t)a.out | (uintptr_t)a4->k.codes | (uintptr_t)a4->v.codes) % 16)
         return fail(RK_EINVAL, "%s: an array is not aligned to 16 bytes", name);
-    return attention_call<true>(a, &a4->k, &a4->v, workspace, ws_bytes, stream, name);
+    return attention_call<AttendFp4>(a, &a4->k, &a4->v, workspace, ws_bytes, stream, name);
 }
 
 }  // extern "C"
