@@ -8,11 +8,22 @@ template <int DP, bool Half>
 struct AttendFp4 : AttendBase<DP, Half> {
     using Base = AttendBase<DP, Half>;
     using Base::NC, Base::kRow, Base::kTurn, Base::turn, Base::p, Base::tile, Base::join, Base::wave, Base::G, Base::c;
-    using Base::block_id, Base::rows_of, Base::bad_block, Base::report_bad, Base::token_of, Base::strays, Base::divisor;
+    using Base::block_id, Base::report_bad, Base::token_of, Base::strays, Base::divisor;
     // Keys of a wavefront in a narrow step: a key is a quarter of the bytes of a 16-bit one, and as many should be under way.
     static constexpr int kNarrowKeys = DP <= 128 ? 64 : 32;
 
     using Base::Base;
+
+    // The kernel's arguments, to be read where they are used: what is read through `p` is read at the kernel's beginning and kept in
+    // scalar registers through all tiles, more than there are.
+    typedef const __attribute__((address_space(4))) AttendArgs Args;
+    static __device__ __forceinline__ Args& args()
+    {
+        Args* a = (Args*)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(a));
+        return *a;
+    }
+    typedef const __attribute__((address_space(4))) rk_fp4_cache Cache;
 
     // A lane loads a quarter of a row of a block: in each round a share (32 values of one power of two), in the last, of a DP that is
     // no multiple of 128, half a share.
@@ -31,14 +42,14 @@ struct AttendFp4 : AttendBase<DP, Half> {
     struct Places {
         uint32_t codes[kRounds], powers[kRounds];
     };
-    __device__ __forceinline__ Places places(const rk_fp4_cache& cache, uint32_t r, uint32_t j) const
+    static __device__ __forceinline__ Places places(const Cache& cache, int32_t D, uint32_t r, uint32_t j)
     {
         Places at;
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
             const bool half = kHalfRound && i == kRounds - 1;
             const uint32_t share = 4 * i + (half ? j / 2 : j);
-            const bool there = 32 * share < (uint32_t)p.a.D;
+            const bool there = 32 * share < (uint32_t)D;
             at.codes[i] = there ? r * (uint32_t)cache.cs.token + 16 * share + (half ? 8 * (j & 1) : 0) : kNowhere;
             at.powers[i] = there ? r * (uint32_t)cache.ss.token + share : kNowhere;
         }
@@ -48,13 +59,13 @@ struct AttendFp4 : AttendBase<DP, Half> {
     // Piece x of the row's query, its sign turned with the scale's; rows that are not there and pieces behind D are 0.  The load is made
     // in any case, from a place that is there: with a branch around each of a row's loads, values that two of them share were
     // computed for the lanes of one side alone (D = 256, 17 rows: results of no meaning).
-    __device__ __forceinline__ u32x4 query_of(const Tile& t, int32_t r, int32_t piece) const
+    __device__ __forceinline__ u32x4 query_of(Args& a, const Tile& t, int32_t r, int32_t piece) const
     {
         const int32_t tok = token_of(r), head = r - tok * G;
-        const bool there = tok < t.tokens && 8 * piece < p.a.D;
-        const uint32_t mask = there ? 0xffffffffu : 0u, sign = p.a.scale < 0.0f ? 0x80008000u & mask : 0u;
-        const u32x4 q = *reinterpret_cast<const u32x4*>((const uint16_t*)p.a.q + (t.token + (int64_t)(there ? tok : 0)) * p.a.q_token +
-                                                        (t.head * G + (there ? head : 0)) * p.a.q_head + (there ? 8 * piece : 0));
+        const bool there = tok < t.tokens && 8 * piece < a.a.D;
+        const uint32_t mask = there ? 0xffffffffu : 0u, sign = a.a.scale < 0.0f ? 0x80008000u & mask : 0u;
+        const u32x4 q = *reinterpret_cast<const u32x4*>((const uint16_t*)a.a.q + (t.token + (int64_t)(there ? tok : 0)) * a.a.q_token +
+                                                        (t.head * G + (there ? head : 0)) * a.a.q_head + (there ? 8 * piece : 0));
         return (q & mask) ^ sign;
     }
 
@@ -67,14 +78,26 @@ struct AttendFp4 : AttendBase<DP, Half> {
             return fp4_values<Half>(w[ks / 4][ks % 4], __uint_as_float(power[ks / 4] << 23));
         }
     };
-    // The lane's part of block number b of the tile's sequence, block `id` of the cache; 0 in rows behind the tile's keys.
-    __device__ __forceinline__ Codes codes_of(const rk_fp4_cache& cache, const Tile& t, int32_t b, int32_t id, const Places& at) const
+    // A key head's keys or values: where they begin, and how many bytes a whole block of them spans.
+    struct Side {
+        const uint8_t *codes, *powers;
+        uint32_t code_block, power_block;    // bytes from block to block (below 2^32)
+        int32_t code_token, power_token, code_bytes, power_bytes;
+    };
+    static __device__ __forceinline__ Side side(const Cache& c, int32_t D, int32_t head)
     {
-        const int32_t rows = rows_of(t, b, id), block = rows > 0 ? id : 0, shares = (p.a.D + 31) / 32, last = rows - 1;
-        const Memory codes = memory((const uint8_t*)cache.codes + block * cache.cs.block + t.head * cache.cs.head,
-                                    rows > 0 ? last * (int32_t)cache.cs.token + 16 * shares : 0);
-        const Memory scales = memory((const uint8_t*)cache.scales + block * cache.ss.block + t.head * cache.ss.head,
-                                     rows > 0 ? last * (int32_t)cache.ss.token + shares : 0);
+        const int32_t shares = (D + 31) / 32, last = RK_BLOCK_TOKENS - 1;
+        return Side{(const uint8_t*)c.codes + head * c.cs.head, (const uint8_t*)c.scales + head * c.ss.head, (uint32_t)c.cs.block,
+                    (uint32_t)c.ss.block, (int32_t)c.cs.token, (int32_t)c.ss.token, last * (int32_t)c.cs.token + 16 * shares,
+                    last * (int32_t)c.ss.token + shares};
+    }
+    // The lane's part of block `id`'s first `rows` rows; 0 behind them (rows = 0: nothing is read).
+    static __device__ __forceinline__ Codes codes_of(const Side& from, int32_t id, int32_t rows, const Places& at)
+    {
+        const int32_t less = RK_BLOCK_TOKENS - rows;
+        const uint64_t block = rows > 0 ? (uint32_t)id : 0u;
+        const Memory codes = memory(from.codes + block * from.code_block, rows > 0 ? from.code_bytes - less * from.code_token : 0);
+        const Memory powers = memory(from.powers + block * from.power_block, rows > 0 ? from.power_bytes - less * from.power_token : 0);
         Codes x;
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
@@ -84,15 +107,37 @@ struct AttendFp4 : AttendBase<DP, Half> {
             } else {
                 x.w[i] = load16(codes, at.codes[i]);
             }
-            x.power[i] = load1(scales, at.powers[i]);
+            x.power[i] = load1(powers, at.powers[i]);
         }
         return x;
     }
-    // The ks-th piece of a lane's quarter (lane % 4) of row lane / 4, and all of them, as 16-bit values to a block's place in LDS.
+    // Rows of block number b of the tile's sequence.
+    static __device__ __forceinline__ int32_t rows_of(const Tile& t, int32_t b)
+    {
+        const int32_t n = t.keys_end - b * RK_BLOCK_TOKENS;
+        return n < 0 ? 0 : n < RK_BLOCK_TOKENS ? n : RK_BLOCK_TOKENS;
+    }
+    // Of N blocks of the tile's sequence from number b on, with the numbers `id` in the cache.  Most are whole and in the cache, which
+    // spares half of the scalar instructions.
+    template <int N>
+    static __device__ __forceinline__ void codes_of(Codes (&x)[N], const Side& from, const Tile& t, int32_t b, const int32_t (&id)[N],
+                                                    uint32_t bad, const Places& at)
+    {
+        if (!bad && (b + N) * RK_BLOCK_TOKENS <= t.keys_end) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = codes_of(from, id[k], RK_BLOCK_TOKENS, at);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = codes_of(from, id[k], bad >> k & 1 ? 0 : rows_of(t, b + k), at);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // The ks-th piece of a lane's quarter (lane / 16) of row lane % 16, and all of them, as 16-bit values to a block's place in LDS.
+    // (16 lanes' pieces, of 16 rows, fill the banks once; a row by four lanes beside each other, four times: decoding batches.)
     __device__ __forceinline__ void place_piece(const Codes& x, int ks, uint32_t lds, uint32_t lane) const
     {
-        const uint32_t r = lane >> 2;
-        lds_write16(lds + r * kRow + (((uint32_t)piece_of(ks, lane & 3) ^ turn(r)) << 4), x.values(ks));
+        const uint32_t r = lane & 15;
+        lds_write16(lds + r * kRow + (((uint32_t)piece_of(ks, lane >> 4) ^ turn(r)) << 4), x.values(ks));
     }
     __device__ __forceinline__ void place_values(const Codes& x, uint32_t lds, uint32_t lane) const
     {
@@ -133,6 +178,11 @@ struct AttendFp4 : AttendBase<DP, Half> {
         // scores run beside them (whole prompts 1,440 -> 1,360 us).  Pieces are read from LDS kAhead products before the one that
         // takes them: 3 are as good, 6 spill registers (whole prompts 1,230 -> 1,500 us).
         constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
+        Args& a = args();
+        const int32_t n_blocks = a.a.n_blocks;
+        const Side k_side = side(a.kc, a.a.D, t.head), v_side = side(a.vc, a.a.D, t.head);
+        const Places k_at = places(a.kc, a.a.D, lane & 15, lane >> 4), v_at = places(a.vc, a.a.D, lane & 15, lane >> 4);
+        auto bad_block = [&](int32_t id) { return (uint32_t)id >= (uint32_t)n_blocks; };
         struct Step {
             int32_t own;                             // this wavefront's block
             uint32_t bad;                            // of the four blocks, those outside the cache
@@ -150,12 +200,12 @@ struct AttendFp4 : AttendBase<DP, Half> {
         // Of a cache in 4 bits the codes of keys three steps ahead and of values two are under way to registers; they are
         // converted into the stages of keys two steps ahead and values one beside the second product, which leaves the vector units idle.
         Codes k_raw, v_raw;
-        const Places k_at = places(p.kc, lane >> 2, lane & 3), v_at = places(p.vc, lane >> 2, lane & 3);
+        auto own_rows = [&](int32_t x, const Step& e) { return bad_block(e.own) ? 0 : rows_of(t, t.block0 + 4 * x + wave); };
         auto issue_keys = [&](int32_t x, const Step& e) {
-            k_raw = codes_of(p.kc, t, t.block0 + 4 * x + wave, e.own, k_at);
+            k_raw = codes_of(k_side, e.own, own_rows(x, e), k_at);
         };
         auto issue_values = [&](int32_t x, const Step& e) {
-            v_raw = codes_of(p.vc, t, t.block0 + 4 * x + wave, e.own, v_at);
+            v_raw = codes_of(v_side, e.own, own_rows(x, e), v_at);
         };
         auto put_keys = [&](int32_t x) { place_values(k_raw, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
         auto put_values = [&](int32_t x) { place_values(v_raw, values_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
@@ -313,7 +363,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         put_values(s);
         issue_values(s + 1, next);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = query_of(t, r, 2 * ks + hi);
+        for (int ks = 0; ks < KS; ++ks) q[ks] = query_of(a, t, r, 2 * ks + hi);
         put_keys(s + 1);
         issue_keys(s + 2, then);
         arrive();
@@ -420,13 +470,14 @@ struct AttendFp4 : AttendBase<DP, Half> {
         constexpr int kSets = NQ == 1 || DP < 128 ? 2 : 1;      // steps whose codes are under way or in registers
         const int lane = afresh(threadIdx.x & 63);
         const int g = lane >> 4, col = lane & 15;
+        Args& a = args();
         u32x4 q[NQ][KS];
         int32_t last[NQ];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int32_t r = 16 * n + col;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query_of(t, r, piece_of(ks, g));
+            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query_of(a, t, r, piece_of(ks, g));
             last[n] = t.keys_end - 1;
             if (t.mask) {
                 const int32_t pos = t.pos + token_of(r);
@@ -443,7 +494,9 @@ struct AttendFp4 : AttendBase<DP, Half> {
             m[n] = -INFINITY;
             l[n] = 0.0f;
         }
-        const Places k_at = places(p.kc, col, g), v_at = places(p.vc, lane >> 2, lane & 3);
+        const int32_t n_blocks = a.a.n_blocks;
+        const Side k_side = side(a.kc, a.a.D, t.head), v_side = side(a.vc, a.a.D, t.head);
+        const Places k_at = places(a.kc, a.a.D, col, g), v_at = places(a.vc, a.a.D, col, g);
         uint32_t v_read[kTurn / 2];
         {
             const uint32_t vr = 4 * g + (col >> 2);
@@ -467,18 +520,11 @@ struct AttendFp4 : AttendBase<DP, Half> {
         auto issue_keys = [&](auto u, int32_t x) {
             next_bad[u] = 0;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                k_raw[u][b] = codes_of(p.kc, t, first_block + kBlocks * x + b, id[b], k_at);
-                next_bad[u] |= (bad_block(id[b]) ? 1u : 0u) << b;
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            for (int b = 0; b < NB; ++b) next_bad[u] |= ((uint32_t)id[b] >= (uint32_t)n_blocks ? 1u : 0u) << b;
+            codes_of<NB>(k_raw[u], k_side, t, first_block + kBlocks * x, id, next_bad[u], k_at);
         };
         auto issue_values = [&](auto u, int32_t x) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                v_raw[u][b] = codes_of(p.vc, t, first_block + kBlocks * x + b, id[b], v_at);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            codes_of<NB>(v_raw[u], v_side, t, first_block + kBlocks * x, id, next_bad[u], v_at);
         };
         auto scores = [&](auto u, f32x4 (*sc)[NB]) {
 #pragma unroll
@@ -681,6 +727,7 @@ int rk_prefix_attention_fp4(const rk_attention_fp4* a4, void* workspace, size_t 
         if (!fp4_strides(c)) return fail(RK_EINVAL, "%s: a stride is negative, or one of codes no multiple of 16", name);
         if (c.cs.token < 16 * shares || c.ss.token < shares || c.cs.token >= 1 << 26 || c.ss.token >= 1 << 26)
             return fail(RK_EINVAL, "%s: a cache's token stride is below a row or past 2^26", name);
+        if (a.n_blocks > 1 && (c.cs.block >> 32 || c.ss.block >> 32)) return fail(RK_EUNSUPPORTED, "%s: a block stride past 2^32 bytes", name);
     }
     if (a.B == 0 || a.T == 0) return RK_OK;
     if (!attention_arrays(a) || (a.n_blocks > 0 && (!a4->k.codes || !a4->k.scales || !a4->v.codes || !a4->v.scales)))
