@@ -78,26 +78,25 @@ struct AttendFp4 : AttendBase<DP, Half> {
             return fp4_values<Half>(w[ks / 4][ks % 4], __uint_as_float(power[ks / 4] << 23));
         }
     };
-    // A key head's keys or values: where they begin, and how many bytes a whole block of them spans.
+    // A key head's keys or values: where they begin, and how many bytes a block of them spans (0: there is none).
     struct Side {
         const uint8_t *codes, *powers;
         uint32_t code_block, power_block;    // bytes from block to block (below 2^32)
-        int32_t code_token, power_token, code_bytes, power_bytes;
+        int32_t code_bytes, power_bytes;
     };
-    static __device__ __forceinline__ Side side(const Cache& c, int32_t D, int32_t head)
+    static __device__ __forceinline__ Side side(const Cache& c, Args& a, int32_t head)
     {
-        const int32_t shares = (D + 31) / 32, last = RK_BLOCK_TOKENS - 1;
+        const int32_t shares = (a.a.D + 31) / 32, last = RK_BLOCK_TOKENS - 1;
+        const bool some = a.a.n_blocks > 0;
         return Side{(const uint8_t*)c.codes + head * c.cs.head, (const uint8_t*)c.scales + head * c.ss.head, (uint32_t)c.cs.block,
-                    (uint32_t)c.ss.block, (int32_t)c.cs.token, (int32_t)c.ss.token, last * (int32_t)c.cs.token + 16 * shares,
-                    last * (int32_t)c.ss.token + shares};
+                    (uint32_t)c.ss.block, some ? last * (int32_t)c.cs.token + 16 * shares : 0, some ? last * (int32_t)c.ss.token + shares : 0};
     }
-    // The lane's part of block `id`'s first `rows` rows; 0 behind them (rows = 0: nothing is read).
-    static __device__ __forceinline__ Codes codes_of(const Side& from, int32_t id, int32_t rows, const Places& at)
+    // The lane's part of block `id` of the cache.  All of the block is loaded: a key behind a sequence's end gets no weight, and
+    // of values there only what is no number could show.
+    static __device__ __forceinline__ Codes codes_of(const Side& from, int32_t id, const Places& at)
     {
-        const int32_t less = RK_BLOCK_TOKENS - rows;
-        const uint64_t block = rows > 0 ? (uint32_t)id : 0u;
-        const Memory codes = memory(from.codes + block * from.code_block, rows > 0 ? from.code_bytes - less * from.code_token : 0);
-        const Memory powers = memory(from.powers + block * from.power_block, rows > 0 ? from.power_bytes - less * from.power_token : 0);
+        const Memory codes = memory(from.codes + (uint64_t)(uint32_t)id * from.code_block, from.code_bytes);
+        const Memory powers = memory(from.powers + (uint64_t)(uint32_t)id * from.power_block, from.power_bytes);
         Codes x;
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
@@ -111,26 +110,13 @@ struct AttendFp4 : AttendBase<DP, Half> {
         }
         return x;
     }
-    // Rows of block number b of the tile's sequence.
-    static __device__ __forceinline__ int32_t rows_of(const Tile& t, int32_t b)
+    // The least power in the place of those of rows (lane % 16) that block number b of the tile's sequence does not have: what weights of
+    // 0 are multiplied with is a number then.
+    static __device__ __forceinline__ void only_rows(Codes& x, const Tile& t, int32_t b, bool bad, uint32_t lane)
     {
-        const int32_t n = t.keys_end - b * RK_BLOCK_TOKENS;
-        return n < 0 ? 0 : n < RK_BLOCK_TOKENS ? n : RK_BLOCK_TOKENS;
-    }
-    // Of N blocks of the tile's sequence from number b on, with the numbers `id` in the cache.  Most are whole and in the cache, which
-    // spares half of the scalar instructions.
-    template <int N>
-    static __device__ __forceinline__ void codes_of(Codes (&x)[N], const Side& from, const Tile& t, int32_t b, const int32_t (&id)[N],
-                                                    uint32_t bad, const Places& at)
-    {
-        if (!bad && (b + N) * RK_BLOCK_TOKENS <= t.keys_end) {
+        const bool there = !bad && (int32_t)(lane & 15) < t.keys_end - b * RK_BLOCK_TOKENS;
 #pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = codes_of(from, id[k], RK_BLOCK_TOKENS, at);
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = codes_of(from, id[k], bad >> k & 1 ? 0 : rows_of(t, b + k), at);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < kRounds; ++i) x.power[i] = there ? x.power[i] : 0u;
     }
     // The ks-th piece of a lane's quarter (lane / 16) of row lane % 16, and all of them, as 16-bit values to a block's place in LDS.
     // (16 lanes' pieces, of 16 rows, fill the banks once; a row by four lanes beside each other, four times: decoding batches.)
@@ -144,6 +130,49 @@ struct AttendFp4 : AttendBase<DP, Half> {
 #pragma unroll
         for (int ks = 0; ks < kPieces; ++ks) place_piece(x, ks, lds, lane);
     }
+
+    // The numbers of the blocks that a tile's steps load, N of each step, 64 at a time in the lanes of a register, the next 64 under way.
+    // (Scalar loads of each step's would be waited for with the LDS operations beside them, the memory's whole time in every step:
+    // decoding batches.)
+    template <int N>
+    struct Numbers {
+        static constexpr int kSteps = 64 / N;
+        const __attribute__((address_space(4))) int32_t* row;
+        int32_t from, per, last, n_blocks, end;      // step x, below `end`, loads the entries from + per x .. + N - 1, of which `last` is the last there is
+        int32_t base, now, next;             // `now` has those of the steps from `base` on
+        uint64_t bad;                        // of `now`, those outside the cache (and 0 there)
+        __device__ __forceinline__ int32_t load(int32_t step, uint32_t lane) const
+        {
+            const int32_t b = from + per * (step + (int32_t)(lane / N)) + (int32_t)(lane % N);
+            return row[b < last ? b : last];
+        }
+        __device__ __forceinline__ Numbers(const Tile& t, int32_t from_, int32_t per_, int32_t n, int32_t step, uint32_t lane)
+            : row(t.row), from(from_), per(per_), last((t.keys_end - 1) / RK_BLOCK_TOKENS), n_blocks(n), end(t.s1), base(step)
+        {
+            now = load(step, lane);
+            next = load(step + kSteps, lane);
+            check();
+        }
+        __device__ __forceinline__ void check()
+        {
+            const bool outside = (uint32_t)now >= (uint32_t)n_blocks;
+            bad = __ballot(outside);
+            now = outside ? 0 : now;
+        }
+        // Makes those of step x, no more than a step behind the last one asked for, readable; returns the place of its first.
+        __device__ __forceinline__ int32_t turn_to(int32_t x, uint32_t lane)
+        {
+            if (x - base >= kSteps) {
+                now = next;
+                base += kSteps;
+                check();
+                if (base + kSteps < end) next = load(base + kSteps, lane);
+            }
+            return (x - base) * N;
+        }
+        __device__ __forceinline__ int32_t at(int32_t place) const { return __builtin_amdgcn_readlane(now, place); }
+        __device__ __forceinline__ uint32_t bad_at(int32_t place) const { return (uint32_t)(bad >> place) & ((1u << N) - 1u); }
+    };
 
     // ---------------------------------------------------------------- up to 128 rows, 32 a wavefront
     //
@@ -180,35 +209,34 @@ struct AttendFp4 : AttendBase<DP, Half> {
         constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
         Args& a = args();
         const int32_t n_blocks = a.a.n_blocks;
-        const Side k_side = side(a.kc, a.a.D, t.head), v_side = side(a.vc, a.a.D, t.head);
+        const Side k_side = side(a.kc, a, t.head), v_side = side(a.vc, a, t.head);
         const Places k_at = places(a.kc, a.a.D, lane & 15, lane >> 4), v_at = places(a.vc, a.a.D, lane & 15, lane >> 4);
-        auto bad_block = [&](int32_t id) { return (uint32_t)id >= (uint32_t)n_blocks; };
         struct Step {
             int32_t own;                             // this wavefront's block
             uint32_t bad;                            // of the four blocks, those outside the cache
         };
+        Numbers<4> numbers(t, t.block0, 4, n_blocks, t.s0, lane);
         auto look = [&](int32_t x) {
-            const int32_t b = t.block0 + 4 * x;
-            const int32_t b0 = block_id(t, b), b1 = block_id(t, b + 1), b2 = block_id(t, b + 2), b3 = block_id(t, b + 3);
-            Step e;
-            e.own = uniform(wave < 2 ? (wave == 0 ? b0 : b1) : (wave == 2 ? b2 : b3));
-            e.bad = (bad_block(b0) ? 1u : 0u) | (bad_block(b1) ? 2u : 0u) | (bad_block(b2) ? 4u : 0u) | (bad_block(b3) ? 8u : 0u);
-            return e;
+            const int32_t place = numbers.turn_to(x, lane);
+            return Step{numbers.at(place + wave), numbers.bad_at(place)};
         };
         auto keys_at = [&](int32_t x) { return tile + ((x - t.s0) & 1) * kKeys; };
         auto values_at = [&](int32_t x) { return tile + 2 * kKeys + ((x - t.s0) & 1) * kKeys; };
         // Of a cache in 4 bits the codes of keys three steps ahead and of values two are under way to registers; they are
         // converted into the stages of keys two steps ahead and values one beside the second product, which leaves the vector units idle.
         Codes k_raw, v_raw;
-        auto own_rows = [&](int32_t x, const Step& e) { return bad_block(e.own) ? 0 : rows_of(t, t.block0 + 4 * x + wave); };
         auto issue_keys = [&](int32_t x, const Step& e) {
-            k_raw = codes_of(k_side, e.own, own_rows(x, e), k_at);
+            k_raw = codes_of(k_side, e.own, k_at);
         };
         auto issue_values = [&](int32_t x, const Step& e) {
-            v_raw = codes_of(v_side, e.own, own_rows(x, e), v_at);
+            v_raw = codes_of(v_side, e.own, v_at);
         };
         auto put_keys = [&](int32_t x) { place_values(k_raw, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
-        auto put_values = [&](int32_t x) { place_values(v_raw, values_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
+        auto true_values = [&](int32_t x, const Step& e) { only_rows(v_raw, t, t.block0 + 4 * x + wave, e.bad >> wave & 1, lane); };
+        auto put_values = [&](int32_t x, const Step& e) {
+            true_values(x, e);
+            place_values(v_raw, values_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane);
+        };
         // the x-th product's piece of the keys, or values, in a stage; what differs by constants is added by the reads
         struct Keys {
             uint32_t at[kTurn / 2];
@@ -284,9 +312,9 @@ struct AttendFp4 : AttendBase<DP, Half> {
             l += a + b;
             w[x >> 2][x & 3] = pack16<Half>(a, b);
         };
-        // A step whose keys every row sees: sc its scores, top their largest; the next step's into nx; e2, e3: the blocks of steps
-        // x + 2 and x + 3.
-        auto open_step = [&](int32_t x, const f32x16* sc, f32x16* nx, float& top, const Step& e2, const Step& e3) {
+        // A step whose keys every row sees: sc its scores, top their largest; the next step's into nx; e1, e2, e3: the blocks of the
+        // steps after it.
+        auto open_step = [&](int32_t x, const f32x16* sc, f32x16* nx, float& top, const Step& e1, const Step& e2, const Step& e3) {
             const float base = follow(top);
             const Keys ka = keys_in(keys_at(x + 1));
             constexpr int n = 2 * KS;
@@ -316,6 +344,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
             // whole prompts 1,251 -> 1,214 us)
             __builtin_amdgcn_s_setprio(1);
             const Values va = values_in(values_at(x));
+            true_values(x + 1, e1);
             u32x4 v[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
@@ -360,7 +389,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         issue_values(s, now);
         put_keys(s);
         issue_keys(s + 1, next);
-        put_values(s);
+        put_values(s, now);
         issue_values(s + 1, next);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) q[ks] = query_of(a, t, r, 2 * ks + hi);
@@ -374,10 +403,10 @@ struct AttendFp4 : AttendBase<DP, Half> {
         float top = highest(sa);
         while (s + 1 < s_open && !(now.bad | next.bad)) {
             arrive();
-            open_step(s, sa, sb, top, then, far);
+            open_step(s, sa, sb, top, next, then, far);
             advance();
             arrive();
-            open_step(s, sb, sa, top, then, far);
+            open_step(s, sb, sa, top, next, then, far);
             advance();
         }
         for (;;) {
@@ -447,7 +476,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
                 if (u + kAhead < 4 * DT) v[u % kAhead] = value_piece(vs, u + kAhead);
             }
             if (s + 1 >= t.s1) break;
-            put_values(s + 1);               // (not in the last step: then others write their results there)
+            put_values(s + 1, next);         // (not in the last step: then others write their results there)
             put_keys(s + 2);
             issue_values(s + 2, then);
             issue_keys(s + 3, far);
@@ -495,7 +524,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
             l[n] = 0.0f;
         }
         const int32_t n_blocks = a.a.n_blocks;
-        const Side k_side = side(a.kc, a.a.D, t.head), v_side = side(a.vc, a.a.D, t.head);
+        const Side k_side = side(a.kc, a, t.head), v_side = side(a.vc, a, t.head);
         const Places k_at = places(a.kc, a.a.D, col, g), v_at = places(a.vc, a.a.D, col, g);
         uint32_t v_read[kTurn / 2];
         {
@@ -510,21 +539,23 @@ struct AttendFp4 : AttendBase<DP, Half> {
         const int32_t first_block = t.block0 + (Solo ? 0 : NB * wave);
         int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kKeys - 1) / kKeys;
         s1 = s1 < t.s1 ? s1 : t.s1;
-        int32_t s = t.s0, id[NB], later[NB];
-        auto ids = [&](int32_t* to, int32_t x) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) to[b] = block_id(t, first_block + kBlocks * x + b);
-        };
+        int32_t s = t.s0, id[NB];
+        Numbers<NB> numbers(t, first_block, kBlocks, n_blocks, s, lane);
         uint32_t bad = 0, any_bad = 0, next_bad[kSets] = {};
         Codes k_raw[kSets][NB], v_raw[kSets][NB];
         auto issue_keys = [&](auto u, int32_t x) {
-            next_bad[u] = 0;
+            const int32_t place = numbers.turn_to(x, lane);
+            next_bad[u] = numbers.bad_at(place);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) next_bad[u] |= ((uint32_t)id[b] >= (uint32_t)n_blocks ? 1u : 0u) << b;
-            codes_of<NB>(k_raw[u], k_side, t, first_block + kBlocks * x, id, next_bad[u], k_at);
+            for (int b = 0; b < NB; ++b) id[b] = numbers.at(place + b);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) k_raw[u][b] = codes_of(k_side, id[b], k_at);
+            __builtin_amdgcn_sched_barrier(0);
         };
-        auto issue_values = [&](auto u, int32_t x) {
-            codes_of<NB>(v_raw[u], v_side, t, first_block + kBlocks * x, id, next_bad[u], v_at);
+        auto issue_values = [&](auto u) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) v_raw[u][b] = codes_of(v_side, id[b], v_at);
+            __builtin_amdgcn_sched_barrier(0);
         };
         auto scores = [&](auto u, f32x4 (*sc)[NB]) {
 #pragma unroll
@@ -579,34 +610,43 @@ struct AttendFp4 : AttendBase<DP, Half> {
             const u32x2 lo = lds_read_columns(x), up = lds_read_columns(x + 16 * kRow);
             return u32x4{lo.x, lo.y, up.x, up.y};
         };
-        auto keys_read = [&](auto u) {
-            bad = next_bad[u];
-            if (s + kSets < s1) {
+        // The second product; values are read from LDS kAhead products before the one that takes them.
+        auto product = [&](const u32x4 (*w)[NB / 2]) {
+            constexpr int N = DT * (NB / 2), kAhead = 4;
+            u32x4 v[kAhead];
 #pragma unroll
-                for (int b = 0; b < NB; ++b) id[b] = later[b];
-                issue_keys(u, s + kSets);
-                ids(later, s + kSets + 1);
+            for (int x = 0; x < kAhead; ++x) v[x] = values(x % DT, x / DT);
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) o[n][x % DT] = mfma16<Half>(v[x % kAhead], w[n][x / DT], o[n][x % DT]);
+                if (x + kAhead < N) v[x % kAhead] = values((x + kAhead) % DT, (x + kAhead) / DT);
             }
         };
-        auto put_values = [&](auto u) {
+        auto keys_read = [&](auto u) {
+            bad = next_bad[u];
+            if (s + kSets < s1) issue_keys(u, s + kSets);
+        };
+        auto put_values = [&](auto u, bool some_behind) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) place_values(v_raw[u][b], vals + b * (RK_BLOCK_TOKENS * kRow), lane);
-            if (s + kSets < s1) issue_values(u, s + kSets);
+            for (int b = 0; b < NB; ++b) {
+                if (some_behind) only_rows(v_raw[u][b], t, first_block + kBlocks * s + b, bad >> b & 1, lane);
+                place_values(v_raw[u][b], vals + b * (RK_BLOCK_TOKENS * kRow), lane);
+            }
+            if (s + kSets < s1) issue_values(u);
         };
         constexpr std::integral_constant<int, 0> first{};
         constexpr std::integral_constant<int, kSets - 1> second{};
         if constexpr (Solo) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the LDS is the last tile's until here
         else __syncthreads();
         if (s < s1) {
-            ids(id, s);
             issue_keys(first, s);
-            issue_values(first, s);
+            issue_values(first);
             if (kSets > 1 && s + 1 < s1) {
-                ids(id, s + 1);
                 issue_keys(second, s + 1);
-                issue_values(second, s + 1);
+                issue_values(second);
             }
-            ids(later, s + kSets);
         }
         const int32_t seen = all_see + 1 - first_block * RK_BLOCK_TOKENS - kNarrowKeys;       // the last step's first key that all see
         const int32_t open = seen < 0 ? 0 : seen / kKeys + 1, s_open = open < s1 ? open : s1;
@@ -616,15 +656,8 @@ struct AttendFp4 : AttendBase<DP, Half> {
             scores(u, sc);
             keys_read(u);
             weights(sc, w);
-            put_values(u);
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int c = 0; c < NB / 2; ++c) {
-                    const u32x4 v = values(d, c);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
-                }
+            put_values(u, false);
+            product(w);
         };
         auto any_step = [&](auto u) {
             const int32_t key0 = (first_block + kBlocks * s) * RK_BLOCK_TOKENS;
@@ -642,7 +675,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
                     for (int i = 0; i < 4; ++i)
                         if (key0 + 16 * kt + 4 * g + i > last[n] || ((bad >> kt) & 1)) sc[n][kt][i] = -INFINITY;
             weights(sc, w);
-            put_values(u);
+            put_values(u, true);
             if (masked && t.mask && t.tokens > 1) {                      // (as for wide tiles, of values of the wavefront's own)
                 u16x2 most = {0, 0};
 #pragma unroll 4
@@ -672,14 +705,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 }
             }
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int c = 0; c < NB / 2; ++c) {
-                    const u32x4 v = values(d, c);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][d] = mfma16<Half>(v, w[n][c], o[n][d]);
-                }
+            product(w);
         };
         if constexpr (kSets == 1) {
             for (; s < s_open && !next_bad[0]; ++s) open_step(first);
