@@ -110,6 +110,13 @@ struct AttendFp4 : AttendBase<DP, Half> {
         }
         return x;
     }
+    // A use of x's powers beside their loads, on a path that is hardly taken.  Without it they leave the loads in 16 bits and are extended
+    // to 32 as soon as there is time, long before they are used, which waits for the memory.
+    static __device__ __forceinline__ void keep_wide(const Codes& x)
+    {
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) asm volatile("" ::"v"(x.power[i]));
+    }
     // The least power in the place of those of rows (lane % 16) that block number b of the tile's sequence does not have: what weights of
     // 0 are multiplied with is a number then.
     static __device__ __forceinline__ void only_rows(Codes& x, const Tile& t, int32_t b, bool bad, uint32_t lane)
@@ -131,47 +138,58 @@ struct AttendFp4 : AttendBase<DP, Half> {
         for (int ks = 0; ks < kPieces; ++ks) place_piece(x, ks, lds, lane);
     }
 
-    // The numbers of the blocks that a tile's steps load, N of each step, 64 at a time in the lanes of a register, the next 64 under way.
-    // (Scalar loads of each step's would be waited for with the LDS operations beside them, the memory's whole time in every step:
-    // decoding batches.)
-    template <int N>
+    // The numbers of the blocks that a tile's steps load, N of each step, 64 of them in the lanes of each of M registers.
+    // (Scalar loads of each step's would be waited for with the LDS operations beside them, the memory's whole time in every
+    // step.  So would loads in the midst of a tile, so there are M registers to choose from: decoding batches read all at a tile's beginning.)
+    template <int N, int M>
     struct Numbers {
         static constexpr int kSteps = 64 / N;
         const __attribute__((address_space(4))) int32_t* row;
-        int32_t from, per, last, n_blocks, end;      // step x, below `end`, loads the entries from + per x .. + N - 1, of which `last` is the last there is
-        int32_t base, now, next;             // `now` has those of the steps from `base` on
-        uint64_t bad;                        // of `now`, those outside the cache (and 0 there)
-        __device__ __forceinline__ int32_t load(int32_t step, uint32_t lane) const
-        {
-            const int32_t b = from + per * (step + (int32_t)(lane / N)) + (int32_t)(lane % N);
-            return row[b < last ? b : last];
-        }
+        int32_t from, per, last, n_blocks;   // step x loads the entries from + per x .. + N - 1, of which `last` is the last there is
+        int32_t base, held[M];               // the steps' from `base` on; of a block outside the cache, kBad
+        bool odd;                            // there is one among them
+        static constexpr int32_t kBad = (int32_t)0x80000000u;
         __device__ __forceinline__ Numbers(const Tile& t, int32_t from_, int32_t per_, int32_t n, int32_t step, uint32_t lane)
-            : row(t.row), from(from_), per(per_), last((t.keys_end - 1) / RK_BLOCK_TOKENS), n_blocks(n), end(t.s1), base(step)
+            : row(t.row), from(from_), per(per_), last((t.keys_end - 1) / RK_BLOCK_TOKENS), n_blocks(n)
         {
-            now = load(step, lane);
-            next = load(step + kSteps, lane);
-            check();
+            load(step, lane);
         }
-        __device__ __forceinline__ void check()
+        __device__ __forceinline__ void load(int32_t step, uint32_t lane)
         {
-            const bool outside = (uint32_t)now >= (uint32_t)n_blocks;
-            bad = __ballot(outside);
-            now = outside ? 0 : now;
-        }
-        // Makes those of step x, no more than a step behind the last one asked for, readable; returns the place of its first.
-        __device__ __forceinline__ int32_t turn_to(int32_t x, uint32_t lane)
-        {
-            if (x - base >= kSteps) {
-                now = next;
-                base += kSteps;
-                check();
-                if (base + kSteps < end) next = load(base + kSteps, lane);
+            base = step;
+            odd = false;
+#pragma unroll
+            for (int k = 0; k < M; ++k) {
+                const int32_t b = from + per * (step + kSteps * k + (int32_t)(lane / N)) + (int32_t)(lane % N);
+                held[k] = row[b < last ? b : last];
             }
-            return (x - base) * N;
+#pragma unroll
+            for (int k = 0; k < M; ++k) {
+                const bool outside = (uint32_t)held[k] >= (uint32_t)n_blocks;
+                odd |= __any(outside);
+                held[k] = outside ? kBad : held[k];
+            }
         }
-        __device__ __forceinline__ int32_t at(int32_t place) const { return __builtin_amdgcn_readlane(now, place); }
-        __device__ __forceinline__ uint32_t bad_at(int32_t place) const { return (uint32_t)(bad >> place) & ((1u << N) - 1u); }
+        // Step x's (x grows): the numbers, 0 of a block outside the cache; a bit of each such.
+        __device__ __forceinline__ uint32_t of(int32_t x, int32_t (&id)[N], uint32_t lane)
+        {
+            if (x - base >= M * kSteps) load(x, lane);
+            const int32_t y = x - base, k = y / kSteps, place = (y % kSteps) * N;
+            int32_t here = held[0];
+#pragma unroll
+            for (int j = 1; j < M; ++j) here = k >= j ? held[j] : here;
+            uint32_t bad = 0;
+#pragma unroll
+            for (int b = 0; b < N; ++b) id[b] = __builtin_amdgcn_readlane(here, place + b);
+            if (odd) {
+#pragma unroll
+                for (int b = 0; b < N; ++b) {
+                    bad |= ((uint32_t)id[b] >> 31) << b;
+                    id[b] &= ~kBad;
+                }
+            }
+            return bad;
+        }
     };
 
     // ---------------------------------------------------------------- up to 128 rows, 32 a wavefront
@@ -215,10 +233,11 @@ struct AttendFp4 : AttendBase<DP, Half> {
             int32_t own;                             // this wavefront's block
             uint32_t bad;                            // of the four blocks, those outside the cache
         };
-        Numbers<4> numbers(t, t.block0, 4, n_blocks, t.s0, lane);
+        Numbers<4, 2> numbers(t, t.block0, 4, n_blocks, t.s0, lane);
         auto look = [&](int32_t x) {
-            const int32_t place = numbers.turn_to(x, lane);
-            return Step{numbers.at(place + wave), numbers.bad_at(place)};
+            int32_t id[4];
+            const uint32_t bad = numbers.of(x, id, lane);
+            return Step{wave < 2 ? (wave == 0 ? id[0] : id[1]) : (wave == 2 ? id[2] : id[3]), bad};
         };
         auto keys_at = [&](int32_t x) { return tile + ((x - t.s0) & 1) * kKeys; };
         auto values_at = [&](int32_t x) { return tile + 2 * kKeys + ((x - t.s0) & 1) * kKeys; };
@@ -227,9 +246,11 @@ struct AttendFp4 : AttendBase<DP, Half> {
         Codes k_raw, v_raw;
         auto issue_keys = [&](int32_t x, const Step& e) {
             k_raw = codes_of(k_side, e.own, k_at);
+            if (numbers.odd) keep_wide(k_raw);
         };
         auto issue_values = [&](int32_t x, const Step& e) {
             v_raw = codes_of(v_side, e.own, v_at);
+            if (numbers.odd) keep_wide(v_raw);
         };
         auto put_keys = [&](int32_t x) { place_values(k_raw, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
         auto true_values = [&](int32_t x, const Step& e) { only_rows(v_raw, t, t.block0 + 4 * x + wave, e.bad >> wave & 1, lane); };
@@ -524,7 +545,8 @@ struct AttendFp4 : AttendBase<DP, Half> {
             l[n] = 0.0f;
         }
         const int32_t n_blocks = a.a.n_blocks;
-        const Side k_side = side(a.kc, a, t.head), v_side = side(a.vc, a, t.head);
+        Side k_side = side(a.kc, a, t.head), v_side = side(a.vc, a, t.head);
+        const int32_t k_bytes = k_side.code_bytes, k_powers = k_side.power_bytes, v_bytes = v_side.code_bytes, v_powers = v_side.power_bytes;
         const Places k_at = places(a.kc, a.a.D, col, g), v_at = places(a.vc, a.a.D, col, g);
         uint32_t v_read[kTurn / 2];
         {
@@ -540,22 +562,37 @@ struct AttendFp4 : AttendBase<DP, Half> {
         int32_t s1 = (t.keys_end - first_block * RK_BLOCK_TOKENS + kKeys - 1) / kKeys;
         s1 = s1 < t.s1 ? s1 : t.s1;
         int32_t s = t.s0, id[NB];
-        Numbers<NB> numbers(t, first_block, kBlocks, n_blocks, s, lane);
+        Numbers<NB, 4> numbers(t, first_block, kBlocks, n_blocks, s, lane);
         uint32_t bad = 0, any_bad = 0, next_bad[kSets] = {};
         Codes k_raw[kSets][NB], v_raw[kSets][NB];
+        // (Loads are made in any case, of nothing behind the last step: of loads that may or may not have been made, all later ones are
+        // waited for with the earlier.)
+        auto for_step = [&](int32_t x) {
+            const bool some = x < s1;
+            k_side.code_bytes = some ? k_bytes : 0;
+            k_side.power_bytes = some ? k_powers : 0;
+            v_side.code_bytes = some ? v_bytes : 0;
+            v_side.power_bytes = some ? v_powers : 0;
+        };
         auto issue_keys = [&](auto u, int32_t x) {
-            const int32_t place = numbers.turn_to(x, lane);
-            next_bad[u] = numbers.bad_at(place);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) id[b] = numbers.at(place + b);
+            next_bad[u] = numbers.of(x, id, lane);
+            for_step(x);
 #pragma unroll
             for (int b = 0; b < NB; ++b) k_raw[u][b] = codes_of(k_side, id[b], k_at);
             __builtin_amdgcn_sched_barrier(0);
+            if (numbers.odd) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) keep_wide(k_raw[u][b]);
+            }
         };
         auto issue_values = [&](auto u) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) v_raw[u][b] = codes_of(v_side, id[b], v_at);
             __builtin_amdgcn_sched_barrier(0);
+            if (numbers.odd) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) keep_wide(v_raw[u][b]);
+            }
         };
         auto scores = [&](auto u, f32x4 (*sc)[NB]) {
 #pragma unroll
@@ -626,7 +663,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         };
         auto keys_read = [&](auto u) {
             bad = next_bad[u];
-            if (s + kSets < s1) issue_keys(u, s + kSets);
+            issue_keys(u, s + kSets);
         };
         auto put_values = [&](auto u, bool some_behind) {
 #pragma unroll
@@ -634,7 +671,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
                 if (some_behind) only_rows(v_raw[u][b], t, first_block + kBlocks * s + b, bad >> b & 1, lane);
                 place_values(v_raw[u][b], vals + b * (RK_BLOCK_TOKENS * kRow), lane);
             }
-            if (s + kSets < s1) issue_values(u);
+            issue_values(u);
         };
         constexpr std::integral_constant<int, 0> first{};
         constexpr std::integral_constant<int, kSets - 1> second{};
@@ -643,7 +680,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         if (s < s1) {
             issue_keys(first, s);
             issue_values(first);
-            if (kSets > 1 && s + 1 < s1) {
+            if (kSets > 1) {
                 issue_keys(second, s + 1);
                 issue_values(second);
             }
