@@ -39,14 +39,13 @@ constexpr int kSoloMost = 512;                       // a narrow tile of so few 
 
 // Kinds of tiles, each on a line of its own.
 enum Kind { kWide, kNarrow, kSolo };
-// What a step of a tile costs, and its beginning and end, relative to each other (a solo tile's to a wavefront, the others' to a
-// workgroup): a wide or narrow step takes about 2 us, what comes before a wide tile's first and after its last 12 (a prologue without
-// products, and results out).  Measured: ends of 4 for narrow and solo ones, 128 requests on one prefix 82 -> 87 us, of 8,
-// groups of 200 62 -> 70; of 10 or 16 for wide ones, 0-5% more.  A piece of a line has at least kLeast, a step or more, so that a tile's
+// What a step of a tile costs, and its beginning and end, is the class's of the tiles: kStepCost, kEndsCost, by kind, a solo tile's to a
+// wavefront, the others' to a workgroup.  A piece of a line has at least kLeast, a step or more, so that a tile's
 // parts follow each other without a gap.
-constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
 constexpr uint32_t kLeast = 4;
-static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
+// Blocks of a narrow step, by workgroup, for each 4 units of its cost.
+template <class A>
+constexpr int kPerBlock = A::kNarrowKeys / RK_BLOCK_TOKENS / (int)A::kStepCost[kNarrow];
 // Keys of a tile's step; A: the class of the tiles, whose kNarrowKeys are a wavefront's in a narrow step.
 template <class A>
 constexpr int kKeysOf[3] = {kWideKeys, kWaves * A::kNarrowKeys, A::kNarrowKeys};
@@ -200,9 +199,12 @@ __device__ __forceinline__ Memory memory(const uint8_t* from, int32_t bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, bytes, 0x00027000);
 }
-__device__ __forceinline__ u32x4 load16(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b128(m, at, 0, 0); }
-__device__ __forceinline__ u32x2 load8(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b64(m, at, 0, 0); }
-__device__ __forceinline__ uint8_t load1(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b8(m, at, 0, 0); }
+template <int Aux = 0>
+__device__ __forceinline__ u32x4 load16(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b128(m, at, 0, Aux); }
+template <int Aux = 0>
+__device__ __forceinline__ u32x2 load8(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b64(m, at, 0, Aux); }
+template <int Aux = 0>
+__device__ __forceinline__ uint8_t load1(Memory m, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b8(m, at, 0, Aux); }
 
 // x, in a way that what is computed from it stays where it is used: hoisted out of the loop over tiles, the
 // addresses of all three kinds of tile would be held (and spilled) at once.
@@ -574,17 +576,18 @@ __device__ __forceinline__ int32_t steps_for(int64_t keys, int kind)
 
 // A tile's extent along the line (its steps, one after the other, then its ends' cost), and the steps of it that begin in its first
 // `length`.  A solo tile is not cut: it belongs where it starts.
+template <class A>
 __device__ __forceinline__ uint64_t extent(int32_t steps, int kind)
 {
-    return kind == kWide ? kEndsCost[kWide] + (uint64_t)steps * kStepCost[kWide]
-         : kind == kNarrow ? kEndsCost[kNarrow] + (uint64_t)steps * kStepCost[kNarrow]
-                           : kEndsCost[kSolo] + (uint64_t)steps * kStepCost[kSolo];
+    return kind == kWide ? A::kEndsCost[kWide] + (uint64_t)steps * A::kStepCost[kWide]
+         : kind == kNarrow ? A::kEndsCost[kNarrow] + (uint64_t)steps * A::kStepCost[kNarrow]
+                           : A::kEndsCost[kSolo] + (uint64_t)steps * A::kStepCost[kSolo];
 }
-template <int K>
+template <class A, int K>
 __device__ __forceinline__ int32_t steps_before(uint64_t length, int32_t steps)
 {
     if (K == kSolo) return length == 0 ? 0 : steps;
-    const uint64_t n = quotient_up(length, kStepCost[K]);
+    const uint64_t n = quotient_up(length, A::kStepCost[K]);
     return n < (uint64_t)steps ? (int32_t)n : steps;
 }
 
@@ -601,12 +604,12 @@ __device__ __forceinline__ Segment own_segment(const Request& r, const AttendArg
     s.tiles = (s.tokens + s.per - 1) / s.per;
     if (s.tiles == 1) {
         s.steps0 = steps_for<A>(own, s.kind);
-        s.pair = s.cost = extent(s.steps0, s.kind);
+        s.pair = s.cost = extent<A>(s.steps0, s.kind);
     } else {
         s.grows = true;
         s.steps0 = steps_for<A>(own - s.tokens + s.per, kWide);
         const int32_t last = steps_for<A>(own - s.tokens + (int64_t)s.tiles * s.per, kWide);
-        s.pair = extent(s.steps0, kWide) + extent(last, kWide) + 2 * kStepCost[kWide];
+        s.pair = extent<A>(s.steps0, kWide) + extent<A>(last, kWide) + 2 * A::kStepCost[kWide];
         s.cost = s.pair * ((s.tiles + 1) / 2);
     }
     return s;
@@ -622,7 +625,7 @@ __device__ __forceinline__ Segment prefix_segment(int32_t tokens, int32_t blocks
     s.per = s.kind == kWide ? p.wide_tokens : s.tokens;
     s.tiles = (s.tokens + s.per - 1) / s.per;
     s.steps0 = steps_for<A>((int64_t)blocks * RK_BLOCK_TOKENS, s.kind);
-    s.pair = extent(s.steps0, s.kind);
+    s.pair = extent<A>(s.steps0, s.kind);
     s.cost = s.pair * s.tiles;
     return s;
 }
@@ -678,7 +681,7 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
                 return steps_for<A>((int64_t)r.kv - (int64_t)r.shared * RK_BLOCK_TOKENS - sg.tokens + seen, kWide);
             };
             const int32_t k = sg.tiles - 1 - j;
-            const uint64_t first = extent(steps_of(j), kWide);
+            const uint64_t first = extent<A>(steps_of(j), kWide);
             steps = steps_of(j);
             left = first;
             if (in >= first) {               // the pair's other tile
@@ -690,7 +693,7 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
             }
         }
         // the steps of the tile that begin in [from, to)
-        const int32_t s0 = steps_before<K>(in, steps), s1 = steps_before<K>(to - x + in, steps);
+        const int32_t s0 = steps_before<A, K>(in, steps), s1 = steps_before<A, K>(to - x + in, steps);
         if (!nothing && s0 < s1) {
             Tile t;
             t.token = r.q0 + j * sg.per;
@@ -723,7 +726,7 @@ __device__ __forceinline__ void walk(A& work, const Request* req, int32_t i, uin
             }
             if (s0 == 0 && (joined || !whole)) {
                 // workgroups that the tile's steps fall to, up to the one in whose piece the last begins
-                const uint64_t of_mine = x - in - from + (uint64_t)(steps - 1) * kStepCost[K];
+                const uint64_t of_mine = x - in - from + (uint64_t)(steps - 1) * A::kStepCost[K];
                 const int32_t n = (int32_t)quotient(of_mine, each) + 1;
                 if (joined) {
                     for (int32_t k = tid; k < t.tokens; k += crew)
@@ -885,8 +888,9 @@ __global__ __launch_bounds__(kThreads, A::kHead <= 128 ? 2 : 1) void attend_kern
             const int64_t n = m.end - f, tokens = req[m.end - 1].q0 + req[m.end - 1].tokens - req[f].q0, rows = tokens * G;
             if (rows == 0 || rows >= kWideRows * n) continue;
             const Segment sg = prefix_segment<A>((int32_t)tokens, m.lent, p);
-            const int64_t apart = n * m.lent * (rows > kNarrowRows * n ? 2 : 1), costs = sg.kind == kSolo ? 1 : 4;    // in quarters
-            if ((int64_t)sg.cost * costs + 4 * kJoinCost * n >= apart) continue;
+            const int64_t apart = n * m.lent * (rows > kNarrowRows * n ? A::kStepCost[kWide] * kPerBlock<A> : 1);        // (a block of a narrow step: 1)
+            const int64_t costs = (sg.kind == kSolo ? 1 : 4) * kPerBlock<A>;
+            if ((int64_t)sg.cost * costs + 4 * kPerBlock<A> * kJoinCost * n >= apart) continue;
             req[i].shared = m.lent;
             if (i == f) req[i].end = m.end;
         }
@@ -1132,7 +1136,8 @@ template <class A, int DP, bool Half>
 static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
 {
     const int64_t rows = p.a.T * p.G;
-    const int32_t chunks = rows <= 4 ? 1 : rows <= 32 ? 4 : 8;
+    const int64_t average = rows / p.a.B;        // of a request: a row a wavefront, of most tiles, and no more workgroups
+    const int32_t chunks = rows <= 4 ? 1 : average <= 8 ? 2 : average <= 16 || rows <= 32 ? 4 : 8;
     const int32_t shared_chunks = (p.G + kWaves - 1) / kWaves;       // a row a wavefront, of one new token
     for (p.b0 = 0; p.b0 < p.a.B; p.b0 += p.n) {
         p.n = launch_size(p.a.B - p.b0);

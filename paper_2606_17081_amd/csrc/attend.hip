@@ -11,6 +11,11 @@ struct Attend : AttendBase<DP, Half> {
     using Base::block_id, Base::rows_of, Base::bad_block, Base::report_bad, Base::token_of, Base::query, Base::strays, Base::divisor,
         Base::out_row, Base::put_lse;
     static constexpr int kNarrowKeys = 32;            // of a wavefront in a narrow step
+    // A wide or narrow step takes about 2 us, what comes before a wide tile's first and after its last 12 (a prologue without
+    // products, and results out).  Measured: ends of 4 for narrow and solo ones, 128 requests on one prefix 82 -> 87 us, of 8,
+    // groups of 200 62 -> 70; of 10 or 16 for wide ones, 0-5% more.
+    static constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
+    static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
 
     const uint32_t last_piece;                        // of a row: the bytes before it
     // the pieces of a block that the lane loads: whole rows a load, or not

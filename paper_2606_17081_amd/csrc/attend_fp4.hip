@@ -11,6 +11,10 @@ struct AttendFp4 : AttendBase<DP, Half> {
     using Base::block_id, Base::report_bad, Base::token_of, Base::strays, Base::divisor;
     // Keys of a wavefront in a narrow step: a key is a quarter of the bytes of a 16-bit one, and as many should be under way.
     static constexpr int kNarrowKeys = DP <= 128 ? 64 : 32;
+    // As of 16-bit caches, though a narrow step has a quarter of the bytes and twice the keys.  (96 requests of 500-12,000 tokens 113 us; ends of 2, 3, 4
+    // or 10 for narrow tiles 115-120, a wide step of 1: 119.  A shared prompt 74 us, with ends of 2 or 3 82-84.)
+    static constexpr uint32_t kStepCost[3] = {2, 2, 2}, kEndsCost[3] = {12, 6, 6};
+    static_assert(kLeast >= kStepCost[kWide] && kLeast >= kStepCost[kNarrow], "a step begins in every piece of a tile");
 
     using Base::Base;
 
@@ -93,6 +97,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
     }
     // The lane's part of block `id` of the cache.  All of the block is loaded: a key behind a sequence's end gets no weight, and
     // of values there only what is no number could show.
+    template <int Aux>
     static __device__ __forceinline__ Codes codes_of(const Side& from, int32_t id, const Places& at)
     {
         const Memory codes = memory(from.codes + (uint64_t)(uint32_t)id * from.code_block, from.code_bytes);
@@ -101,12 +106,12 @@ struct AttendFp4 : AttendBase<DP, Half> {
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
             if (kHalfRound && i == kRounds - 1) {
-                const u32x2 w = load8(codes, at.codes[i]);
+                const u32x2 w = load8<Aux>(codes, at.codes[i]);
                 x.w[i] = u32x4{w.x, w.y, 0u, 0u};
             } else {
-                x.w[i] = load16(codes, at.codes[i]);
+                x.w[i] = load16<Aux>(codes, at.codes[i]);
             }
-            x.power[i] = load1(powers, at.powers[i]);
+            x.power[i] = load1<Aux>(powers, at.powers[i]);
         }
         return x;
     }
@@ -245,11 +250,11 @@ struct AttendFp4 : AttendBase<DP, Half> {
         // converted into the stages of keys two steps ahead and values one beside the second product, which leaves the vector units idle.
         Codes k_raw, v_raw;
         auto issue_keys = [&](int32_t x, const Step& e) {
-            k_raw = codes_of(k_side, e.own, k_at);
+            k_raw = codes_of<0>(k_side, e.own, k_at);
             if (numbers.odd) keep_wide(k_raw);
         };
         auto issue_values = [&](int32_t x, const Step& e) {
-            v_raw = codes_of(v_side, e.own, v_at);
+            v_raw = codes_of<0>(v_side, e.own, v_at);
             if (numbers.odd) keep_wide(v_raw);
         };
         auto put_keys = [&](int32_t x) { place_values(k_raw, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
@@ -516,6 +521,18 @@ struct AttendFp4 : AttendBase<DP, Half> {
     template <int NQ, bool Solo>
     __device__ void narrow(const Tile& t)
     {
+        // Where a head's rows of a block lie side by side, what is read is read once, by whole lines, and need not stay in caches.  Calls on
+        // inputs that change, 64 requests of 5,504 tokens on 8 heads: 101 us so, 110 without the hint; rows of all heads of a token
+        // side by side, which share lines with other tiles': 167 us with it, 138 without.  Solo tiles are few keys of small caches.
+        Args& a = args();
+        const int32_t row = (a.a.D + 31) / 32 * 16;
+        if (!Solo && a.kc.cs.token == row && a.vc.cs.token == row) narrow_of<NQ, Solo, 2>(t);
+        else narrow_of<NQ, Solo, 0>(t);
+    }
+    // kStream: how loads treat the caches (2: as of a stream).
+    template <int NQ, bool Solo, int kStream>
+    __device__ __forceinline__ void narrow_of(const Tile& t)
+    {
         constexpr int KS = DP / 32, DT = DP / 16, NB = kNarrowKeys / RK_BLOCK_TOKENS;     // blocks of a step
         constexpr int kSets = NQ == 1 || DP < 128 ? 2 : 1;      // steps whose codes are under way or in registers
         const int lane = afresh(threadIdx.x & 63);
@@ -578,7 +595,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
             next_bad[u] = numbers.of(x, id, lane);
             for_step(x);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) k_raw[u][b] = codes_of(k_side, id[b], k_at);
+            for (int b = 0; b < NB; ++b) k_raw[u][b] = codes_of<kStream>(k_side, id[b], k_at);
             __builtin_amdgcn_sched_barrier(0);
             if (numbers.odd) {
 #pragma unroll
@@ -587,7 +604,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         };
         auto issue_values = [&](auto u) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) v_raw[u][b] = codes_of(v_side, id[b], v_at);
+            for (int b = 0; b < NB; ++b) v_raw[u][b] = codes_of<kStream>(v_side, id[b], v_at);
             __builtin_amdgcn_sched_barrier(0);
             if (numbers.odd) {
 #pragma unroll
