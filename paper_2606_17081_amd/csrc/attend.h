@@ -82,7 +82,6 @@ struct AttendArgs {
     // then [2][Hkv][shared rows], the whole tiles of rows that share a prefix.
     float *part, *part_ml;
     int32_t shared_rows, shared_tokens;      // of a head
-    rk_fp4_cache kc, vc;                     // the caches, where they are held in 4 bits (a.k_cache, a.v_cache elsewhere)
 };
 
 // The first row of the whole tiles of a kind (prefixes: 0, requests' own keys: 1) and key head.
@@ -762,7 +761,7 @@ __device__ __forceinline__ bool spread(uint32_t& at, uint32_t n, uint32_t of)
 // that a workgroup keeps to one kind's code; workgroups of different kinds lie side by side on a CU, where one waits for memory while the other
 // computes (128 requests on one prefix 86 -> 83 us, groups of 200 64 -> 62 us against kind after kind).
 template <class A>
-__global__ __launch_bounds__(kThreads, A::kHead <= 128 ? 2 : 1) void attend_kernel(AttendArgs p)
+__global__ __launch_bounds__(kThreads, A::kHead <= 128 ? 2 : 1) void attend_kernel(typename A::Args p)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
     __shared__ float s_join[2 * kWaves * kNarrowRows];
@@ -1133,7 +1132,7 @@ inline AttendLayout attend_layout(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
 }
 
 template <class A, int DP, bool Half>
-static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
+static int launch(typename A::Args& p, int32_t grid, hipStream_t s)
 {
     const int64_t rows = p.a.T * p.G;
     const int64_t average = rows / p.a.B;        // of a request: a row a wavefront, of most tiles, and no more workgroups
@@ -1148,7 +1147,7 @@ static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
         int rc = hip_check(hipGetLastError(), "rk_prefix_attention launch");
         if (rc) return rc;
         const int64_t blocks = (int64_t)grid * chunks + (p.a.group_off ? (int64_t)p.n * p.a.Hkv * shared_chunks : 0);
-        hipLaunchKernelGGL((join_kernel<A, DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, p, grid, chunks,
+        hipLaunchKernelGGL((join_kernel<A, DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, (const AttendArgs&)p, grid, chunks,
                            shared_chunks);
         rc = hip_check(hipGetLastError(), "rk_prefix_attention join launch");
         if (rc) return rc;
@@ -1157,7 +1156,7 @@ static int launch(AttendArgs& p, int32_t grid, hipStream_t s)
 }
 
 template <template <int, bool> class Tiles, bool Half>
-static int launch_of(AttendArgs& p, int32_t grid, hipStream_t s)
+static int launch_of(typename Tiles<64, Half>::Args& p, int32_t grid, hipStream_t s)
 {
     switch (head_size(p.a.D)) {
     case 64: return launch<Tiles<64, Half>, 64, Half>(p, grid, s);
@@ -1204,22 +1203,16 @@ inline bool attention_arrays(const rk_attention& a)
     return a.q && a.out && a.kv_len && a.q_off && (a.table_stride == 0 || a.tables);
 }
 
-// The call whose arguments hold; Tiles: the class of its tiles; kc, vc: the caches, where they are held in 4 bits, or NULL.
-template <template <int, bool> class Tiles>
-static int attention_call(const rk_attention& a, const rk_fp4_cache* kc, const rk_fp4_cache* vc, void* workspace, size_t ws_bytes,
-                          void* stream, const char* name)
+// The call whose arguments hold; Tiles: the class of its tiles; p: what their kernels take, with what the caches alone need.
+template <template <int, bool> class Tiles, class Args>
+static int attention_call(const rk_attention& a, Args& p, void* workspace, size_t ws_bytes, void* stream, const char* name)
 {
     const AttendLayout L = attend_layout(a.group_off ? a.T : 0, a.B, a.Hq, a.Hkv, a.D);       // (no groups: no rows of such)
     if (!workspace || ws_bytes < L.bytes)
         return fail(RK_ENOMEM, "%s: workspace of %zu bytes, %zu needed", name, workspace ? ws_bytes : (size_t)0, L.bytes);
     if ((uintptr_t)workspace % 256) return fail(RK_EINVAL, "%s: workspace is not aligned to 256 bytes", name);
     uint8_t* ws = (uint8_t*)workspace;
-    AttendArgs p{};
     p.a = a;
-    if (kc) {
-        p.kc = *kc;
-        p.vc = *vc;
-    }
     p.status = status_word();
     if (!p.status) return fail(RK_EHIP, "%s: no status word", name);
     p.split = (Split*)(ws + L.split);

@@ -6,6 +6,7 @@ namespace rk {
 // Tiles over a 16-bit cache.
 template <int DP, bool Half>
 struct Attend : AttendBase<DP, Half> {
+    typedef AttendArgs Args;
     using Base = AttendBase<DP, Half>;
     using Base::NC, Base::NI, Base::kRow, Base::kTurn, Base::turn, Base::p, Base::tile, Base::join, Base::wave, Base::G, Base::c;
     using Base::block_id, Base::rows_of, Base::bad_block, Base::report_bad, Base::token_of, Base::query, Base::strays, Base::divisor,
@@ -659,7 +660,8 @@ int rk_prefix_attention(const rk_attention* a, void* workspace, size_t ws_bytes,
     if (!attention_arrays(*a) || (a->n_blocks > 0 && (!a->k_cache || !a->v_cache))) return fail(RK_EINVAL, "%s: NULL array", name);
     if (((uintptr_t)a->q | (uintptr_t)a->out | (uintptr_t)a->k_cache | (uintptr_t)a->v_cache) % 16)
         return fail(RK_EINVAL, "%s: an array is not aligned to 16 bytes", name);
-    return attention_call<Attend>(*a, nullptr, nullptr, workspace, ws_bytes, stream, name);
+    AttendArgs p{};
+    return attention_call<Attend>(*a, p, workspace, ws_bytes, stream, name);
 }
 
 }  // extern "C"

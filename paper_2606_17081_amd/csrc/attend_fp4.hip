@@ -3,9 +3,14 @@
 
 namespace rk {
 
+struct AttendFp4Args : AttendArgs {
+    rk_fp4_cache kc, vc;
+};
+
 // Tiles over a cache in 4 bits.
 template <int DP, bool Half>
 struct AttendFp4 : AttendBase<DP, Half> {
+    typedef AttendFp4Args Args;
     using Base = AttendBase<DP, Half>;
     using Base::NC, Base::kRow, Base::kTurn, Base::turn, Base::p, Base::tile, Base::join, Base::wave, Base::G, Base::c;
     using Base::block_id, Base::report_bad, Base::token_of, Base::strays, Base::divisor;
@@ -20,10 +25,10 @@ struct AttendFp4 : AttendBase<DP, Half> {
 
     // The kernel's arguments, to be read where they are used: what is read through `p` is read at the kernel's beginning and kept in
     // scalar registers through all tiles, more than there are.
-    typedef const __attribute__((address_space(4))) AttendArgs Args;
-    static __device__ __forceinline__ Args& args()
+    typedef const __attribute__((address_space(4))) AttendFp4Args Held;
+    static __device__ __forceinline__ Held& args()
     {
-        Args* a = (Args*)__builtin_amdgcn_kernarg_segment_ptr();
+        Held* a = (Held*)__builtin_amdgcn_kernarg_segment_ptr();
         asm volatile("" : "+s"(a));
         return *a;
     }
@@ -63,7 +68,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
     // Piece x of the row's query, its sign turned with the scale's; rows that are not there and pieces behind D are 0.  The load is made
     // in any case, from a place that is there: with a branch around each of a row's loads, values that two of them share were
     // computed for the lanes of one side alone (D = 256, 17 rows: results of no meaning).
-    __device__ __forceinline__ u32x4 query_of(Args& a, const Tile& t, int32_t r, int32_t piece) const
+    __device__ __forceinline__ u32x4 query_of(Held& a, const Tile& t, int32_t r, int32_t piece) const
     {
         const int32_t tok = token_of(r), head = r - tok * G;
         const bool there = tok < t.tokens && 8 * piece < a.a.D;
@@ -88,7 +93,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         uint32_t code_block, power_block;    // bytes from block to block (below 2^32)
         int32_t code_bytes, power_bytes;
     };
-    static __device__ __forceinline__ Side side(const Cache& c, Args& a, int32_t head)
+    static __device__ __forceinline__ Side side(const Cache& c, Held& a, int32_t head)
     {
         const int32_t shares = (a.a.D + 31) / 32, last = RK_BLOCK_TOKENS - 1;
         const bool some = a.a.n_blocks > 0;
@@ -230,7 +235,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         // scores run beside them (whole prompts 1,440 -> 1,360 us).  Pieces are read from LDS kAhead products before the one that
         // takes them: 3 are as good, 6 spill registers (whole prompts 1,230 -> 1,500 us).
         constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
-        Args& a = args();
+        Held& a = args();
         const int32_t n_blocks = a.a.n_blocks;
         const Side k_side = side(a.kc, a, t.head), v_side = side(a.vc, a, t.head);
         const Places k_at = places(a.kc, a.a.D, lane & 15, lane >> 4), v_at = places(a.vc, a.a.D, lane & 15, lane >> 4);
@@ -524,7 +529,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         // Where a head's rows of a block lie side by side, what is read is read once, by whole lines, and need not stay in caches.  Calls on
         // inputs that change, 64 requests of 5,504 tokens on 8 heads: 101 us so, 110 without the hint; rows of all heads of a token
         // side by side, which share lines with other tiles': 167 us with it, 138 without.  Solo tiles are few keys of small caches.
-        Args& a = args();
+        Held& a = args();
         const int32_t row = (a.a.D + 31) / 32 * 16;
         if (!Solo && a.kc.cs.token == row && a.vc.cs.token == row) narrow_of<NQ, Solo, 2>(t);
         else narrow_of<NQ, Solo, 0>(t);
@@ -537,7 +542,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         constexpr int kSets = NQ == 1 || DP < 128 ? 2 : 1;      // steps whose codes are under way or in registers
         const int lane = afresh(threadIdx.x & 63);
         const int g = lane >> 4, col = lane & 15;
-        Args& a = args();
+        Held& a = args();
         u32x4 q[NQ][KS];
         int32_t last[NQ];
 #pragma unroll
@@ -814,7 +819,10 @@ int rk_prefix_attention_fp4(const rk_attention_fp4* a4, void* workspace, size_t 
         return fail(RK_EINVAL, "%s: NULL array", name);
     if (((uintptr_t)a.q | (uintptr_t)a.out | (uintptr_t)a4->k.codes | (uintptr_t)a4->v.codes) % 16)
         return fail(RK_EINVAL, "%s: an array is not aligned to 16 bytes", name);
-    return attention_call<AttendFp4>(a, &a4->k, &a4->v, workspace, ws_bytes, stream, name);
+    AttendFp4Args p{};
+    p.kc = a4->k;
+    p.vc = a4->v;
+    return attention_call<AttendFp4>(a, p, workspace, ws_bytes, stream, name);
 }
 
 }  // extern "C"

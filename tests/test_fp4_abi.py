@@ -120,6 +120,9 @@ def test_attention_refusals(L):
         assert not _strides_refused(lambda c: rc(**{which: _cache(**c)}))
         for c in (dict(cs=S(1536, 32, 48)), dict(cs=S(1536, 1 << 26, 48)), dict(ss=S(96, 2, 3)), dict(ss=S(96, 1 << 26, 3))):
             assert rc(**{which: _cache(**c)}) == rk.RK_EINVAL and b"token stride" in L.rk_last_error()
+        for c in (dict(cs=S(1 << 32, 96, 48)), dict(ss=S(1 << 32, 6, 3))):
+            assert rc(**{which: _cache(**c)}) == rk.RK_EUNSUPPORTED and b"block stride" in L.rk_last_error()
+            assert rc(**{which: _cache(**c)}, n_blocks=1, q=None) == rk.RK_EINVAL       # of one block it does not matter
         for what in ("codes", "scales"):
             assert rc(**{which: _cache(**{what: None})}) == rk.RK_EINVAL and b"NULL" in L.rk_last_error()
         assert rc(**{which: _cache(codes=4104)}) == rk.RK_EINVAL and b"aligned" in L.rk_last_error()

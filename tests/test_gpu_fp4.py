@@ -579,6 +579,96 @@ def test_same_as_attention_over_what_is_read_back(gpu):
         b.check(out, lse, want=want)
 
 
+def test_attend_a_cache_of_no_blocks(gpu):
+    """Every block is outside it: results of 0, and no read."""
+    torch, rk = gpu
+    q = torch.randn((3, 8, 80), device="cuda", dtype=torch.float16)
+    codes, scales = (torch.empty((0, BLOCK, 2, n), dtype=torch.uint8, device="cuda") for n in (48, 3))
+    up = rk.to_device
+    for new, kv in (([1, 2], [40, 700]), ([3, 0], [3, 9])):
+        out, lse = rk.prefix_attention_fp4(q, codes, codes, scales, scales, torch.zeros((2, 50), dtype=torch.int32, device="cuda"),
+                                           up(np.array(kv, np.int32)), up(offsets(new)), want_lse=True)
+        assert (out == 0).all() and (lse == -np.inf).all() and rk.device_status(reset=True) == 0x80
+    slots = torch.tensor([-1, 5], device="cuda")
+    k, v = rk.kv_read_fp4(codes, codes, scales, scales, slots, D=80, dtype=torch.float16)
+    assert (k == 0).all() and (v == 0).all() and rk.device_status(reset=True) == 0x80
+    rk.kv_write_fp4(k, v, codes, codes, scales, scales, slots)
+    assert rk.device_status(reset=True) == 0x80
+
+
+@pytest.mark.parametrize("dtype,B,kv,new,Hq,Hkv,D,shared", [
+    ("bf16", 64, 20000, 1, 8, 8, 128, 0), ("fp16", 2, 9000, 9000, 16, 2, 128, 0), ("bf16", 3, 7000, 2500, 8, 1, 192, 0),
+    ("fp16", 40, 9000, 2, 40, 8, 64, 500), ("bf16", 20, 70000, 3, 16, 8, 40, 0)])
+def test_attend_at_size(gpu, dtype, B, kv, new, Hq, Hkv, D, shared):
+    """Tiles of more steps than a wavefront's block numbers are read for at once, narrow and wide: as attention over a 16-bit cache
+    that holds the same.  Each is off by at most half a step for the result and one for the weights, of the mean of |v| (from the same
+    attention over |v|), and by the fp32 sums' errors, with |score| <= scale sum |q| |k| <= scale D max |q| max |k|."""
+    torch, rk = gpu
+    rng = rng_of("size", B, kv, new)
+    ty, u = dtype_of(torch, dtype), STEP[dtype]
+    per = -(-kv // BLOCK)
+    own = per - shared
+    blocks = shared + B * own
+    caches = [fill(torch, rng, blocks, Hkv, D, heads_first=True, scales=(125, 128)) for _ in range(2)]
+    first = np.arange(shared)[None, :].repeat(B, 0)
+    tables = np.concatenate([first, shared + np.arange(B * own).reshape(B, own)], 1)
+    tables = torch.from_numpy(rng.permutation(blocks)[tables].astype(np.int32)).cuda()
+    lengths = np.full(B, kv) - (np.arange(B) % 13)          # fewer than its new tokens: that request is skipped
+    q = torch.randn((B * new, Hq, D), device="cuda", dtype=ty)
+    more = dict(group_off=torch.tensor([0] + [B] * B, device="cuda"),
+                shared=torch.tensor([shared] + [0] * (B - 1), dtype=torch.int32, device="cuda")) if shared else {}
+    rest = [tables, rk.to_device(lengths.astype(np.int32)), rk.to_device(offsets([new] * B))]
+
+    def results():
+        return dict(out=torch.full_like(q, 9), lse=torch.full((B * new, Hq), 7.0, device="cuda"))
+
+    out, lse = rk.prefix_attention_fp4(q, caches[0][0], caches[1][0], caches[0][1], caches[1][1], *rest, **more, **results())
+    k, v = (x.view(blocks, BLOCK, Hkv, D) for x in rk.kv_read_fp4(
+        caches[0][0], caches[1][0], caches[0][1], caches[1][1], torch.arange(BLOCK * blocks, device="cuda"), D=D, dtype=ty))
+    want, want_lse = rk.prefix_attention(q, k, v, *rest, **more, **results())
+    mean = rk.prefix_attention(q, k, v.abs(), *rest, **more, **results())[0].float() * (1 + 4 * u)
+    most = D ** -0.5 * D * float(q.abs().max()) * float(k.abs().max())
+    weight = (2 * (D + 2) * most + 2 * kv + 64) * 2.0 ** -24
+    bound = 2 * (u * want.float().abs() * (1 + u) + (1 + u) * (u + weight) * mean)
+    assert ((out.float() - want.float()).abs() <= bound).all()
+    assert ((lse - want_lse).abs() <= 2 * (weight + 4 * 2.0 ** -24 * want_lse.abs())).all()
+    skipped = torch.from_numpy(np.repeat(lengths < new, new)).cuda()
+    assert (out[skipped] == 9).all() and (lse[skipped] == 7).all() and bool(skipped.any()) == (kv == new)
+    assert rk.device_status(reset=True) == (0x01 if kv == new else 0)
+
+
+def test_read_of_many_tokens(gpu):
+    """More tokens than workgroups, outputs past 2^32 bytes, on a stream of the caller's."""
+    torch, rk = gpu
+    rng = rng_of("many tokens")
+    T, Hkv, D = (1 << 20) + 77, 128, 64
+    c, v = (fill(torch, rng, 3, Hkv, D, scales=(120, 130)) for _ in range(2))
+    slots = torch.randint(-1, 3 * BLOCK, (T,), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    k, w = rk.kv_read_fp4(c[0], v[0], c[1], v[1], slots, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    for at in (slice(0, 500), slice(1 << 19, (1 << 19) + 500), slice(T - 500, T)):
+        kk, ww = rk.kv_read_fp4(c[0], v[0], c[1], v[1], slots[at].contiguous())
+        assert torch.equal(k[at], kk) and torch.equal(w[at], ww)
+    where = (slots == 7).nonzero()[:, 0]
+    assert torch.equal(k[where], k[where[:1]].expand(len(where), -1, -1))
+    del w
+    # and written to a cache of as many blocks, of which every other token's rows stay
+    blocks = T // BLOCK + 1
+    codes = torch.full((blocks, BLOCK, Hkv, 32), 17, dtype=torch.uint8, device="cuda")
+    scales = torch.full((blocks, BLOCK, Hkv, 2), 99, dtype=torch.uint8, device="cuda")
+    other = codes[:1].expand(1, -1, -1, -1).clone(), scales[:1].clone()
+    to = torch.arange(T, device="cuda")
+    to = torch.where(to % 2 == 0, to, -1)
+    rk.kv_write_fp4(k, k, codes, codes.clone(), scales, scales.clone(), to)
+    back = rk.kv_read_fp4(codes, codes, scales, scales, to)[0]
+    assert torch.equal(back[::2], k[::2]) and not back[1::2].any()
+    flat = codes.view(-1, Hkv, 32)
+    assert (flat[1:T:2] == 17).all() and (flat[T:] == 17).all() and (scales.view(-1, Hkv, 2)[1:T:2] == 99).all()
+    assert torch.equal(other[0][0, 1], codes[0, 1]) and rk.device_status(reset=True) == 0
+
+
 # ------------------------------------------------------------------ together
 
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 72)])
