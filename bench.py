@@ -666,6 +666,8 @@ def worker_bench(torch, rk, wl, stream, steps, requests=768, Hq=16, Hkv=2, D=128
     n_blocks = int((kv // 16 + 2).sum())
     caches = [torch.randn((n_blocks, 16, Hkv, D), device="cuda", dtype=torch.bfloat16) for _ in range(2)]
     tables = torch.zeros((B, stride), dtype=torch.int32, device="cuda")
+    codes, scales = ([torch.randint(lo, hi, (n_blocks, Hkv, 16, n), dtype=torch.uint8, device="cuda").transpose(1, 2) for _ in range(2)]
+                     for lo, hi, n in ((0, 256, D // 2), (124, 128, D // 32)))      # the same cache in 4 bits
     free = torch.randperm(n_blocks, device="cuda").to(torch.int32)
     i32 = lambda a: up(np.ascontiguousarray(a, np.int32))  # noqa: E731
     out = {"workload": f"{B} of {requests} 1P/5D-shaped requests routed to one of {W} workers, {Hq} query and {Hkv} key heads of {D}",
@@ -679,7 +681,10 @@ def worker_bench(torch, rk, wl, stream, steps, requests=768, Hq=16, Hkv=2, D=128
         calls = {"block_tables": lambda: rk.block_tables(*args, group_off=group_off, shared=shared),
                  "kv_write": lambda: rk.kv_write(k, v, *caches, slots),
                  "prefix_attention": lambda: rk.prefix_attention(q, *caches, tables, args[1], q_off, group_off, shared),
-                 "attention_without_groups": lambda: rk.prefix_attention(q, *caches, tables, args[1], q_off)}
+                 "attention_without_groups": lambda: rk.prefix_attention(q, *caches, tables, args[1], q_off),
+                 "kv_write_fp4": lambda: rk.kv_write_fp4(k, v, *codes, *scales, slots),
+                 "kv_read_fp4": lambda: rk.kv_read_fp4(*codes, *scales, slots),
+                 "prefix_attention_fp4": lambda: rk.prefix_attention_fp4(q, *codes, *scales, tables, args[1], q_off, group_off, shared)}
         out[name] = {"tokens": T, **{c + "_ms": round(burst_ms(torch, stream, f, max(steps, 10)), 5) for c, f in calls.items()}}
         free = free[int(taken):].contiguous()
     assert rk.device_status(reset=True) == 0

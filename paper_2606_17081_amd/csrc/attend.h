@@ -1,4 +1,4 @@
-// attend.h -- attention of a step's new tokens over the block cache.
+// attend.h -- attention of a step's new tokens over the block cache: what caches of 16 and of 4 bits have alike.
 //
 // out_t = sum_j w_j v_j / sum_j w_j, w_j = exp(scale q_t . k_j), in one pass over the keys: with m at least near the largest
 // score so far, o = sum 2^(s_j - m) v_j and l = sum 2^(s_j - m) (scores in units of log2) are rescaled when m moves, and

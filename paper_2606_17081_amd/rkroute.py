@@ -709,7 +709,7 @@ def kv_write_fp4(k, v, k_cache, v_cache, k_scales, v_scales, slots, stream=None)
 
 def kv_read_fp4(k_cache, v_cache, k_scales, v_scales, slots, D=None, dtype=None, k=None, v=None, stream=None):
     """Tokens of a cache in 4 bits as 16-bit values (rk_kv_read_fp4): (k, v), [tokens, Hkv, D] each.  D defaults to the k that is
-    given, or to 2 bytes' worth of a row of codes each (32 C); dtype to the k that is given, or to bfloat16."""
+    given, or to all values of a row of codes (32 C); dtype to the k that is given, or to bfloat16."""
     dev = _where("k_cache", k_cache)
     torch = _found_torch or _torch()
     _no_gradient("kv_read_fp4", k, v)
