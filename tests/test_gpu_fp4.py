@@ -596,13 +596,15 @@ def test_attend_a_cache_of_no_blocks(gpu):
     assert rk.device_status(reset=True) == 0x80
 
 
-@pytest.mark.parametrize("dtype,B,kv,new,Hq,Hkv,D,shared", [
-    ("bf16", 64, 20000, 1, 8, 8, 128, 0), ("fp16", 2, 9000, 9000, 16, 2, 128, 0), ("bf16", 3, 7000, 2500, 8, 1, 192, 0),
-    ("fp16", 40, 9000, 2, 40, 8, 64, 500), ("bf16", 20, 70000, 3, 16, 8, 40, 0)])
-def test_attend_at_size(gpu, dtype, B, kv, new, Hq, Hkv, D, shared):
-    """Tiles of more steps than a wavefront's block numbers are read for at once, narrow and wide: as attention over a 16-bit cache
-    that holds the same.  Each is off by at most half a step for the result and one for the weights, of the mean of |v| (from the same
-    attention over |v|), and by the fp32 sums' errors, with |score| <= scale sum |q| |k| <= scale D max |q| max |k|."""
+@pytest.mark.parametrize("dtype,B,kv,new,Hq,Hkv,D,shared,bad", [
+    ("bf16", 64, 20000, 1, 8, 8, 128, 0, 0), ("fp16", 2, 9000, 9000, 16, 2, 128, 0, 0), ("bf16", 3, 7000, 2500, 8, 1, 192, 0, 0),
+    ("fp16", 40, 9000, 2, 40, 8, 64, 500, 0), ("bf16", 20, 70000, 3, 16, 8, 40, 0, 0), ("fp16", 64, 20000, 1, 8, 8, 128, 0, 1100),
+    ("bf16", 2, 9000, 4000, 16, 2, 128, 0, 300), ("bf16", 20, 70000, 3, 16, 8, 64, 0, 4200)])
+def test_attend_at_size(gpu, dtype, B, kv, new, Hq, Hkv, D, shared, bad):
+    """Tiles of more steps than a wavefront's block numbers are read for at once, narrow and wide, with blocks outside the cache or
+    without: as attention over a 16-bit cache that holds the same.  Each is off by at most half a step for the result and one for the
+    weights, of the mean of |v| (from the same attention over |v|), and by the fp32 sums' errors, with |score| <= scale sum |q| |k|
+    <= scale D max |q| max |k|."""
     torch, rk = gpu
     rng = rng_of("size", B, kv, new)
     ty, u = dtype_of(torch, dtype), STEP[dtype]
@@ -617,6 +619,11 @@ def test_attend_at_size(gpu, dtype, B, kv, new, Hq, Hkv, D, shared):
     q = torch.randn((B * new, Hq, D), device="cuda", dtype=ty)
     more = dict(group_off=torch.tensor([0] + [B] * B, device="cuda"),
                 shared=torch.tensor([shared] + [0] * (B - 1), dtype=torch.int32, device="cuda")) if shared else {}
+    if bad:                                                 # blocks outside the cache, from entry `bad` on
+        outside = rng.random(tables.shape) < 0.03
+        outside[:, :bad] = False
+        tables = torch.where(torch.from_numpy(outside).cuda(), torch.tensor([-1, blocks] * tables.shape[1], dtype=torch.int32, device="cuda")
+                             [:tables.shape[1]], tables)
     rest = [tables, rk.to_device(lengths.astype(np.int32)), rk.to_device(offsets([new] * B))]
 
     def results():
@@ -634,7 +641,7 @@ def test_attend_at_size(gpu, dtype, B, kv, new, Hq, Hkv, D, shared):
     assert ((lse - want_lse).abs() <= 2 * (weight + 4 * 2.0 ** -24 * want_lse.abs())).all()
     skipped = torch.from_numpy(np.repeat(lengths < new, new)).cuda()
     assert (out[skipped] == 9).all() and (lse[skipped] == 7).all() and bool(skipped.any()) == (kv == new)
-    assert rk.device_status(reset=True) == (0x01 if kv == new else 0)
+    assert rk.device_status(reset=True) == (0x01 if kv == new else 0x80 if bad else 0)
 
 
 def test_read_of_many_tokens(gpu):
