@@ -97,6 +97,15 @@ struct AttendFp4 : AttendBase<DP, Half> {
             return fp4_values<Half>(w[ks / 4][ks % 4], __uint_as_float(power[ks / 4] << 23));
         }
     };
+    // 0 for a key's codes behind D, beside values of the same power of two before it: the type may not hold what they stand for, and the
+    // query's zeros do not make 0 of an infinity.  (Values there are in products of their own, which go nowhere.)  A D that its class
+    // takes ends in a row's last round, and behind a lane's first piece there if rounds are whole.
+    static __device__ __forceinline__ void end_at(Codes& x, int32_t D, uint32_t j)
+    {
+        constexpr int r = kRounds - 1;
+#pragma unroll
+        for (int e = kHalfRound ? 0 : 1; e < (kHalfRound ? 2 : 4); ++e) x.w[r][e] = 8 * piece_of(4 * r + e, j) < D ? x.w[r][e] : 0u;
+    }
     // A key head's keys or values: where they begin, and how many bytes a block of them spans (0: there is none).
     struct Side {
         const uint8_t *codes, *powers;
@@ -250,7 +259,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         // takes them: 3 are as good, 6 spill registers (whole prompts 1,230 -> 1,500 us).
         constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
         Held& a = args();
-        const int32_t n_blocks = a.a.n_blocks;
+        const int32_t n_blocks = a.a.n_blocks, D = a.a.D;
         const Side k_side = side(a.kc, a, t.head), v_side = side(a.vc, a, t.head);
         const Places k_at = places(a.kc, a.a.D, lane & 15, lane >> 4), v_at = places(a.vc, a.a.D, lane & 15, lane >> 4);
         struct Step {
@@ -276,7 +285,10 @@ struct AttendFp4 : AttendBase<DP, Half> {
             v_raw = codes_of<0>(v_side, e.own, v_at);
             if (numbers.odd) keep_wide(v_raw);
         };
-        auto put_keys = [&](int32_t x) { place_values(k_raw, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane); };
+        auto put_keys = [&](int32_t x) {
+            end_at(k_raw, D, lane >> 4);
+            place_values(k_raw, keys_at(x) + wave * (RK_BLOCK_TOKENS * kRow), lane);
+        };
         auto true_values = [&](int32_t x, const Step& e) { only_rows(v_raw, t, t.block0 + 4 * x + wave, e.bad >> wave & 1, lane); };
         auto put_values = [&](int32_t x, const Step& e) {
             true_values(x, e);
@@ -390,6 +402,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
             __builtin_amdgcn_s_setprio(1);
             const Values va = values_in(values_at(x));
             true_values(x + 1, e1);
+            end_at(k_raw, D, lane >> 4);
             u32x4 v[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) v[u] = value_piece(va, u);
@@ -580,7 +593,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
             m[n] = -INFINITY;
             l[n] = 0.0f;
         }
-        const int32_t n_blocks = a.a.n_blocks;
+        const int32_t n_blocks = a.a.n_blocks, D = a.a.D;
         Side k_side = side(a.kc, a, t.head), v_side = side(a.vc, a, t.head);
         const int32_t k_bytes = k_side.code_bytes, k_powers = k_side.power_bytes, v_bytes = v_side.code_bytes, v_powers = v_side.power_bytes;
         const Places k_at = places(a.kc, a.a.D, col, g), v_at = places(a.vc, a.a.D, col, g);
@@ -633,6 +646,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         auto scores = [&](auto u, f32x4 (*sc)[NB]) {
 #pragma unroll
             for (int kt = 0; kt < NB; ++kt) {
+                end_at(k_raw[u][kt], D, g);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) sc[n][kt] = f32x4{};
 #pragma unroll

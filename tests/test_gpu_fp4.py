@@ -379,6 +379,38 @@ def test_attend_not_finite(gpu, Hq, new, D, dtype):
     assert rk.device_status(reset=True) == 0
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("D", [8, 16, 40, 56, 72, 80, 120, 136, 152, 184, 200, 240, 248])
+@pytest.mark.parametrize("kv,new,Hq,Hkv", [([40] * 300, [1] * 300, 1, 1), ([3000, 90], [1, 3], 4, 2), ([700, 40], [3, 2], 8, 1),
+                                           ([500, 129], [300, 129], 4, 1)])
+def test_attend_codes_behind_the_head(gpu, kv, new, Hq, Hkv, D, dtype):
+    """Codes behind D beside a scale with which the largest of them are past the type's range, while what lies before D is not: they
+    have no effect.  (Keys before D up to 3 * 2^14 or 3 * 2^126, with queries and a scale that make usual scores of them.)"""
+    torch, rk = gpu
+    b = Batch4(torch, rng_of("behind D", D, kv[0]), kv, new, Hq, Hkv, D, dtype)
+    if dtype == "bf16":
+        b.q = (b.q.float() * 2.0 ** -110).to(b.q.dtype)
+    large = 141 if dtype == "fp16" else 253
+    owned = ~torch.from_numpy((host(b.held[0][1]) == 255).any(-1)).cuda()
+    C, left = shares(D), D % 32 // 2                                    # (the last share's bytes before D)
+    for i, (codes, scales) in enumerate(b.held):
+        last = codes[..., 16 * C - 16:]
+        if i == 0:
+            nibble = torch.randint(0, 6, (2, *last.shape), device="cuda") + 8 * torch.randint(0, 2, (2, *last.shape), device="cuda")
+            last.copy_((nibble[0] | nibble[1] << 4).to(torch.uint8))
+        else:
+            last.zero_()
+        last[..., left:] = torch.tensor([0x77, 0x7f, 0xf7, 0x6e], dtype=torch.uint8, device="cuda").repeat(4)[:16 - left]
+        scales[..., C - 1][owned] = large
+        b.caches[i] = torch.from_numpy(ow.fp4_decode(host(codes), host(scales), D)).cuda().to(b.q.dtype)
+    slots = torch.arange(BLOCK * len(b.caches[0]), device="cuda")
+    read = rk.kv_read_fp4(b.held[0][0], b.held[1][0], b.held[0][1], b.held[1][1], slots, D=D, dtype=b.q.dtype)
+    for x, want in zip(read, b.caches):
+        assert equal(host(x), host(want).reshape(x.shape)) and torch.isfinite(want[owned]).all()
+    attend(gpu, b, scale=2.0 ** (-15 if dtype == "fp16" else -17))
+    assert rk.device_status(reset=True) == 0
+
+
 @pytest.mark.parametrize("kv,new,Hq", [(60, 1, 2), (9000, 1, 4), (700, 300, 8), (9000, 2, 64)])
 def test_attend_queries_that_are_no_numbers(gpu, kv, new, Hq):
     """A query with a NaN gives NaN, also where its parts are joined; and one with an infinity where its scores are none."""
