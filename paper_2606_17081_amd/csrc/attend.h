@@ -989,7 +989,7 @@ __global__ __launch_bounds__(kThreads, A::kHead <= 128 ? 2 : 1) void attend_kern
 // loads is all that bounds it (4 us with nothing to join, 8-10 us for decoding batches), but of the rows of whole prompts'
 // 500 cut tiles (30 us for 100 MB).
 template <class A, int DP, bool Half>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks, int32_t shared_chunks)
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t grid, int32_t chunks, int32_t soon, int32_t shared_chunks)
 {
     const rk_attention& a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1057,11 +1057,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p, int32_t gr
     auto cut = [&](int32_t wg, int32_t r, int32_t k) { return (2 * (int64_t)(wg + k) + (k == 0 ? 1 : 0)) * kWideRows + r; };
     const int32_t of_shared = a.group_off ? p.n * a.Hkv * shared_chunks : 0;
     if ((int32_t)blockIdx.x >= of_shared) {
-        const int32_t b = (int32_t)blockIdx.x - of_shared;
-        const Split t = p.split[b / chunks];
+        // each tile's first `soon` workgroups, then the others
+        const int32_t b = (int32_t)blockIdx.x - of_shared, late = b - grid * soon;
+        const int32_t tile = late < 0 ? b / soon : late / (chunks - soon), chunk = late < 0 ? b % soon : soon + late % (chunks - soon);
+        const Split t = p.split[tile];
         const int32_t rows = t.tokens * G;
         if (t.n == 0) return;
-        for (int32_t r = b % chunks * kWaves + wave; r < rows; r += chunks * kWaves)
+        for (int32_t r = chunk * kWaves + wave; r < rows; r += chunks * kWaves)
             join(t.n, [&](int32_t k) { return cut(t.wg, r, k); }, t.token + (int64_t)(r / G), t.head * G + r % G);
         return;
     }
@@ -1135,8 +1137,13 @@ template <class A, int DP, bool Half>
 static int launch(typename A::Args& p, int32_t grid, hipStream_t s)
 {
     const int64_t rows = p.a.T * p.G;
-    const int64_t average = rows / p.a.B;        // of a request: a row a wavefront, of most tiles, and no more workgroups
-    const int32_t chunks = rows <= 4 ? 1 : average <= 8 ? 2 : average <= 16 || rows <= 32 ? 4 : 8;
+    // A row a wavefront, so eight workgroups join a tile of 32 rows or more.  Most tiles of a batch have its average request's rows, and
+    // need fewer: those are launched first, for all tiles, and the others, which most tiles have nothing for, behind them.  (All
+    // eight of a tile side by side: 96 requests of 500-12,000 tokens, 64 / 8 heads, 145 us, so 140.  Only as many as the average asks
+    // for: 40 requests of a token and a piece of 128 on 20,000 tokens, 4 / 2 heads, 172 us over 4 bits and 148 over 16, so 72 and 63.)
+    const int64_t average = rows / p.a.B;
+    const int32_t chunks = rows <= 4 ? 1 : rows <= 32 ? 4 : 8;
+    const int32_t near = average <= 8 ? 2 : average <= 16 ? 4 : 8, soon = near < chunks ? near : chunks;
     const int32_t shared_chunks = (p.G + kWaves - 1) / kWaves;       // a row a wavefront, of one new token
     for (p.b0 = 0; p.b0 < p.a.B; p.b0 += p.n) {
         p.n = launch_size(p.a.B - p.b0);
@@ -1148,7 +1155,7 @@ static int launch(typename A::Args& p, int32_t grid, hipStream_t s)
         if (rc) return rc;
         const int64_t blocks = (int64_t)grid * chunks + (p.a.group_off ? (int64_t)p.n * p.a.Hkv * shared_chunks : 0);
         hipLaunchKernelGGL((join_kernel<A, DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, (const AttendArgs&)p, grid, chunks,
-                           shared_chunks);
+                           soon, shared_chunks);
         rc = hip_check(hipGetLastError(), "rk_prefix_attention join launch");
         if (rc) return rc;
     }

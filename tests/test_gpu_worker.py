@@ -325,6 +325,19 @@ def test_attend_single_token(gpu, kv):
     assert gpu[1].device_status(reset=True) == 0
 
 
+@pytest.mark.parametrize("singles,pieces,Hq,Hkv,D,dtype", [
+    (40, [(6000, 128)], 2, 2, 128, "bf16"), (60, [(5000, 64), (300, 300)], 4, 2, 64, "fp16"), (30, [(4000, 128)], 8, 1, 72, "bf16"),
+    (5, [(6000, 1)], 1, 1, 128, "fp16"), (0, [(7000, 4)], 4, 1, 64, "bf16"), (2, [(5000, 20)], 1, 1, 192, "bf16"), (9, [(3000, 40)], 3, 1, 256, "fp16")])
+def test_attend_pieces_beside_single_tokens(gpu, singles, pieces, Hq, Hkv, D, dtype):
+    """Tiles of many rows, cut over workgroups, in batches whose average request has few."""
+    rng = rng_of("beside", singles, pieces, Hq)
+    kv = np.concatenate([rng.integers(1, 1500, singles), [k for k, _ in pieces]])
+    new = np.concatenate([np.ones(singles, np.int64), [n for _, n in pieces]])
+    order = rng.permutation(len(kv))
+    attend(gpu, Batch(gpu[0], rng, kv[order], new[order], Hq, Hkv, D, dtype, rows_behind=2))
+    assert gpu[1].device_status(reset=True) == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("Hq,Hkv,D", [(1, 1, 8), (2, 1, 64), (8, 1, 128), (12, 1, 192), (16, 2, 256), (7, 1, 80), (5, 5, 96),
                                       (40, 8, 128), (128, 1, 64), (34, 1, 128), (10, 2, 136), (33, 11, 72), (17, 1, 248),
