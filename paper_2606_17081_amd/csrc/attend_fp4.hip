@@ -34,7 +34,8 @@ struct AttendFp4 : AttendBase<DP, Half> {
     using Base::Base;
 
     // The kernel's arguments, to be read where they are used: what is read through `p` is read at the kernel's beginning and kept in
-    // scalar registers through all tiles, more than there are.
+    // scalar registers through all tiles, more than there are.  (The address is the kernel's own: in a function that it calls the compiler
+    // has none, and takes 0.  So all that asks for it is inlined.)
     typedef const __attribute__((address_space(4))) AttendFp4Args Held;
     static __device__ __forceinline__ Held& args()
     {
@@ -229,7 +230,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
     // product with the values takes them.  All that differs is how keys and values come to LDS: by registers, a wavefront a block of
     // each step, converted once for the four of them.  Matrix instructions bound it (D = 128: 32 products of 32 cycles
     // a step and wavefront; 32 conversions and 32 exponentials a lane lie beside them).
-    __device__ void wide(const Tile& t)
+    __device__ __forceinline__ void wide(const Tile& t)
     {
         constexpr int KS = DP / 16, DT = DP / 32;
         const int lane = afresh(threadIdx.x & 63);
@@ -551,7 +552,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
     // kSets steps are under way to registers, keys in the order in which the product takes them, so that they are converted
     // there; values pass LDS once they are 16 bits, since the second product takes them by columns.
     template <int NQ, bool Solo>
-    __device__ void narrow(const Tile& t)
+    __device__ __forceinline__ void narrow(const Tile& t)
     {
         // Where a head's rows of a block lie side by side, what is read is read once, by whole lines, and need not stay in caches.  Calls on
         // inputs that change, 64 requests of 5,504 tokens on 8 heads: 101 us so, 110 without the hint; rows of all heads of a token

@@ -8,6 +8,7 @@ import subprocess
 
 import pytest
 
+from paper_2606_17081_amd import build
 from paper_2606_17081_amd import rkroute as rk
 
 WAIT_M0 = 1            # between a scalar write of m0 and a load to LDS, which reads it
@@ -87,3 +88,28 @@ def test_loads_to_lds_wait_for_what_they_read(tmp_path):
         loads += sum(op.startswith("buffer_load") and args[-1].split()[-1] == "lds" for op, args in code if args)
         wrong += faults(code)
     assert loads > 0 and not wrong, (loads, len(wrong), wrong[:5])
+
+
+def test_only_kernels_ask_for_their_arguments_address(tmp_path):
+    """Where a function that a kernel calls asks for the address of the kernel's arguments, it gets 0.  Without optimization all is
+    called that need not be inlined."""
+    try:
+        cc = build.hipcc()
+    except RuntimeError:
+        pytest.skip("no hipcc")
+    flags = [f for f in build.HIPCC_FLAGS if f != "-O3"]
+    asked, outside = 0, []
+    for src in build.SOURCES:
+        text = open(os.path.join(build.CSRC, src)).read()
+        if "kernarg_segment_ptr" not in text:
+            continue
+        to = str(tmp_path / "out.ll")
+        subprocess.run([cc, *flags, "-O0", "--offload-device-only", "-emit-llvm", "-S", os.path.join(build.CSRC, src), "-o", to],
+                       check=True, capture_output=True)
+        for line in open(to):
+            if line.startswith("define"):
+                where = line
+            elif "llvm.amdgcn.kernarg.segment.ptr" in line and " call " in line:
+                asked += 1
+                outside += [] if "amdgpu_kernel" in where else [re.search(r"@(\w+)", where)[1]]
+    assert asked > 0 and not outside, (asked, sorted(set(outside))[:5])
