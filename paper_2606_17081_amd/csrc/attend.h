@@ -321,17 +321,19 @@ struct AttendBase {
 
     __device__ __forceinline__ int32_t token_of(int32_t r) const { return (int32_t)((uint32_t)r * g_inverse >> 16); }
 
-    // piece x of the row's query, its sign turned with the scale's
-    __device__ __forceinline__ u32x4 query(const Tile& t, int32_t r, int32_t piece) const
+    // A piece of the row's query, its sign turned with the scale's; rows that are not there and pieces behind D are 0.  The load is made in
+    // any case, from a place that is there.  With a branch around each load, values that all lanes need later (the second 16 rows' token
+    // number and a 0, with heads of 256) were moved to other registers between the ends of two such branches, so for
+    // the lanes alone whose rows are there, and their old registers used again at once.
+    template <class R>
+    __device__ __forceinline__ u32x4 query_of(R& a, const Tile& t, int32_t r, int32_t piece) const
     {
-        u32x4 q = {0u, 0u, 0u, 0u};
-        const int32_t tok = token_of(r);
-        if (tok < t.tokens && 8 * piece < p.a.D) {
-            q = *reinterpret_cast<const u32x4*>((const uint16_t*)p.a.q + (t.token + (int64_t)tok) * p.a.q_token +
-                                                (t.head * G + r - tok * G) * p.a.q_head + 8 * piece);
-            if (p.a.scale < 0.0f) q ^= 0x80008000u;
-        }
-        return q;
+        const int32_t tok = token_of(r), head = r - tok * G;
+        const bool there = tok < t.tokens && 8 * piece < a.D;
+        const uint32_t mask = there ? 0xffffffffu : 0u, sign = a.scale < 0.0f ? 0x80008000u & mask : 0u;
+        const u32x4 q = *reinterpret_cast<const u32x4*>((const uint16_t*)a.q + (t.token + (int64_t)(there ? tok : 0)) * a.q_token +
+                                                        (t.head * G + (there ? head : 0)) * a.q_head + (there ? 8 * piece : 0));
+        return (q & mask) ^ sign;
     }
 
     // Whether a step whose largest score is `top` asks for another divisor than 2^m of its weights.  bf16 has fp32's range: the divisor

@@ -9,7 +9,7 @@ struct Attend : AttendBase<DP, Half> {
     typedef AttendArgs Args;
     using Base = AttendBase<DP, Half>;
     using Base::NC, Base::NI, Base::kRow, Base::kTurn, Base::turn, Base::p, Base::tile, Base::join, Base::wave, Base::G, Base::c;
-    using Base::block_id, Base::rows_of, Base::bad_block, Base::report_bad, Base::token_of, Base::query, Base::strays, Base::divisor,
+    using Base::block_id, Base::rows_of, Base::bad_block, Base::report_bad, Base::token_of, Base::query_of, Base::strays, Base::divisor,
         Base::out_row, Base::put_lse;
     static constexpr int kNarrowKeys = 32;            // of a wavefront in a narrow step
     // A wide or narrow step takes about 2 us, what comes before a wide tile's first and after its last 12 (a prologue without
@@ -313,7 +313,7 @@ struct Attend : AttendBase<DP, Half> {
         issue_values(s, now);
         if (s + 1 < t.s1) issue_keys(s + 1, next);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = query(t, r, 2 * ks + hi);
+        for (int ks = 0; ks < KS; ++ks) q[ks] = query_of(p.a, t, r, 2 * ks + hi);
         __builtin_amdgcn_s_waitcnt(0);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -423,7 +423,7 @@ struct Attend : AttendBase<DP, Half> {
         for (int n = 0; n < NQ; ++n) {
             const int32_t r = 16 * n + col;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query(t, r, 4 * ks + g);
+            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query_of(p.a, t, r, 4 * ks + g);
             last[n] = t.keys_end - 1;
             if (t.mask) {
                 const int32_t pos = t.pos + token_of(r);

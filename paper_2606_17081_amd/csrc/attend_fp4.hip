@@ -23,7 +23,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
     typedef AttendFp4Args Args;
     using Base = AttendBase<DP, Half>;
     using Base::NC, Base::kRow, Base::kTurn, Base::turn, Base::p, Base::tile, Base::join, Base::wave, Base::G, Base::c;
-    using Base::block_id, Base::report_bad, Base::token_of, Base::strays, Base::divisor;
+    using Base::block_id, Base::report_bad, Base::token_of, Base::query_of, Base::strays, Base::divisor;
     // Keys of a wavefront in a narrow step: a key is a quarter of the bytes of a 16-bit one, and as many should be under way.
     static constexpr int kNarrowKeys = DP <= 128 ? 64 : 32;
     // As of 16-bit caches, though a narrow step has a quarter of the bytes and twice the keys.  (96 requests of 500-12,000 tokens 113 us; ends of 2, 3, 4
@@ -74,19 +74,6 @@ struct AttendFp4 : AttendBase<DP, Half> {
             at.powers[i] = there ? r * (uint32_t)cache.ss.token + share : kNowhere;
         }
         return at;
-    }
-
-    // Piece x of the row's query, its sign turned with the scale's; rows that are not there and pieces behind D are 0.  The load is made
-    // in any case, from a place that is there: with a branch around each of a row's loads, values that two of them share were
-    // computed for the lanes of one side alone (D = 256, 17 rows: results of no meaning).
-    __device__ __forceinline__ u32x4 query_of(Held& a, const Tile& t, int32_t r, int32_t piece) const
-    {
-        const int32_t tok = token_of(r), head = r - tok * G;
-        const bool there = tok < t.tokens && 8 * piece < a.a.D;
-        const uint32_t mask = there ? 0xffffffffu : 0u, sign = a.a.scale < 0.0f ? 0x80008000u & mask : 0u;
-        const u32x4 q = *reinterpret_cast<const u32x4*>((const uint16_t*)a.a.q + (t.token + (int64_t)(there ? tok : 0)) * a.a.q_token +
-                                                        (t.head * G + (there ? head : 0)) * a.a.q_head + (there ? 8 * piece : 0));
-        return (q & mask) ^ sign;
     }
 
     struct Codes {
@@ -451,7 +438,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         put_values(s, now);
         issue_values(s + 1, next);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = query_of(a, t, r, 2 * ks + hi);
+        for (int ks = 0; ks < KS; ++ks) q[ks] = query_of(a.a, t, r, 2 * ks + hi);
         put_keys(s + 1);
         issue_keys(s + 2, then);
         arrive();
@@ -577,7 +564,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
         for (int n = 0; n < NQ; ++n) {
             const int32_t r = 16 * n + col;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query_of(a, t, r, piece_of(ks, g));
+            for (int ks = 0; ks < KS; ++ks) q[n][ks] = query_of(a.a, t, r, piece_of(ks, g));
             last[n] = t.keys_end - 1;
             if (t.mask) {
                 const int32_t pos = t.pos + token_of(r);

@@ -325,6 +325,19 @@ def test_attend_single_token(gpu, kv):
     assert gpu[1].device_status(reset=True) == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,new,D", [(17, 1, 256), (31, 1, 200), (10, 2, 256), (11, 2, 248), (9, 3, 136), (25, 1, 128), (6, 3, 64)])
+def test_attend_rows_that_are_not_there(gpu, Hq, new, D, dtype):
+    """17 to 31 rows of a key head, the others of 32 not there, with blocks in the cache and outside it."""
+    torch, rk = gpu
+    for bad in (False, True):
+        b = Batch(torch, rng_of("not there", Hq, D), [700, 50, 2000], [new, new, new], Hq, 1, D, dtype)
+        if bad:
+            b.tables[0, 3], b.tables[2, 100] = -5, 1 << 30
+        attend(gpu, b)
+        assert rk.device_status(reset=True) == (0x80 if bad else 0)
+
+
 @pytest.mark.parametrize("singles,pieces,Hq,Hkv,D,dtype", [
     (40, [(6000, 128)], 2, 2, 128, "bf16"), (60, [(5000, 64), (300, 300)], 4, 2, 64, "fp16"), (30, [(4000, 128)], 8, 1, 72, "bf16"),
     (5, [(6000, 1)], 1, 1, 128, "fp16"), (0, [(7000, 4)], 4, 1, 64, "bf16"), (2, [(5000, 20)], 1, 1, 192, "bf16"), (9, [(3000, 40)], 3, 1, 256, "fp16")])
