@@ -273,6 +273,20 @@ def test_attend_rows_that_are_not_there(gpu, Hq, new, D, dtype):
         assert rk.device_status(reset=True) == (0x80 if bad else 0)
 
 
+@pytest.mark.parametrize("Hq,kv,new", [(4, [700, 50], [1, 2]), (1, [30] * 300, [1] * 300), (8, [300, 90], [300, 33])])
+def test_attend_smallest_values(gpu, Hq, kv, new):
+    """fp16 keys and values below 2^-14, which the type holds with fewer bits."""
+    torch, rk = gpu
+    b = Batch4(torch, rng_of("small", Hq, len(kv)), kv, new, Hq, 1, 128, "fp16", garbage=0.0)
+    power = torch.tensor([2.0 ** -17, 2.0 ** -20], device="cuda").repeat(64)
+    for c in b.caches:
+        c.copy_((c.float() * power).half())
+    b.hold()
+    assert float(b.caches[0].abs().max()) < 2.0 ** -13 and float(b.caches[0].abs().max()) > 0
+    attend(gpu, b, scale=2.0 ** 14)
+    assert rk.device_status(reset=True) == 0
+
+
 @pytest.mark.parametrize("singles,pieces,Hq,Hkv,D,dtype", [
     (40, [(6000, 128)], 2, 2, 128, "bf16"), (60, [(5000, 64), (300, 300)], 4, 2, 64, "fp16"), (30, [(4000, 128)], 8, 1, 72, "bf16"),
     (5, [(6000, 1)], 1, 1, 128, "fp16"), (0, [(7000, 4)], 4, 1, 64, "bf16"), (2, [(5000, 20)], 1, 1, 192, "bf16"), (9, [(3000, 40)], 3, 1, 256, "fp16")])
@@ -351,6 +365,37 @@ def test_attend_many_requests_of_wide_heads(gpu, B, Hq, Hkv, D, dtype):
     new[rng.random(B) < 0.05] = 0
     kv[5] = new[5] = 300
     attend(gpu, Batch4(gpu[0], rng, kv, new, Hq, Hkv, D, dtype))
+    assert gpu[1].device_status(reset=True) == 0
+
+
+class Batch4As16(Batch4):
+    """Held to what attention over a 16-bit cache of the same values is held to."""
+    check = Batch.check
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("kv,new,Hq,Hkv,D", [
+    ([1], [1], 16, 2, 128), ([5000], [1], 16, 2, 128), ([300, 17, 2000], [1, 1, 4], 8, 1, 64), ([700, 64], [300, 64], 4, 1, 128),
+    ([40] * 270, [1] * 270, 4, 1, 128), ([900, 33], [5, 33], 6, 2, 192), ([2000, 300], [70, 1], 3, 1, 256), ([129, 1025], [3, 200], 7, 1, 80),
+    ([3000], [33], 2, 2, 40), ([20000, 9000], [1, 2], 4, 1, 64)])
+def test_attend_as_close_as_16_bits(gpu, kv, new, Hq, Hkv, D, dtype):
+    attend(gpu, Batch4As16(gpu[0], rng_of("as 16", kv[0], Hq, D), kv, new, Hq, Hkv, D, dtype, heads_first=Hq % 2 == 0))
+    assert gpu[1].device_status(reset=True) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("sizes,shared,tail,new,Hq,Hkv,D", [([40], [30], 50, 1, 8, 2, 128), ([70, 2], [9, 130], 40, 1, 8, 2, 128),
+                                                            ([6], [20], 300, 150, 8, 2, 128), ([20], [1000], 30, 1, 8, 1, 64)])
+def test_attend_groups_as_close_as_16_bits(gpu, sizes, shared, tail, new, Hq, Hkv, D, dtype):
+    rng = rng_of("groups as 16", sizes, shared, tail)
+    B = sum(sizes)
+    goff = np.concatenate([offsets(sizes), np.full(B + 1 - len(sizes) - 1, B)]).astype(np.int64)
+    sh = np.zeros(B, np.int32)
+    sh[:len(sizes)] = shared
+    own = rng.integers(1, tail + 1, B)
+    kv = BLOCK * np.repeat(shared, sizes) + own
+    n = np.minimum(rng.integers(1, new + 1, B), own)
+    attend(gpu, Batch4As16(gpu[0], rng, kv, n, Hq, Hkv, D, dtype, goff=goff, shared=sh))
     assert gpu[1].device_status(reset=True) == 0
 
 
@@ -584,6 +629,35 @@ def test_past_32_bits(gpu):
     assert torch.equal(k, x) and torch.equal(v, -x)
     for c, s in zip(codes, scales):
         assert int(scales[0][far - 1, 3].sum()) == 4 * 126 and int(s[0, 5].sum()) == 4 * 126
+    assert rk.device_status(reset=True) == 0
+
+
+def test_past_32_bits_of_each_cache(gpu):
+    """What is written past 2^32 bytes of codes and of scales lies there, in the keys' cache and in the values', and is read from there."""
+    torch, rk = gpu
+    far = 4_400_000                                      # blocks of 1,024 bytes of codes
+    codes = [torch.empty((far, BLOCK, 1, 64), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.empty((far, 1024), dtype=torch.uint8, device="cuda")[:, 960:].view(far, BLOCK, 1, 4) for _ in range(2)]
+    places = [(far - 1, 3), (0, 5), ((1 << 32) // 1024 - 1, 15), ((1 << 32) // 1024, 0)]
+    low = [(int(b * 1024 + t * 64) % (1 << 32)) // 64 for b, t in places]                # (where an address of 32 bits would lead)
+    assert len(set(low)) == len(low)
+    for x in (*codes, *scales):
+        x.fill_(9)
+    slots = torch.tensor([BLOCK * b + t for b, t in places], device="cuda")
+    x = torch.tensor([3.0, -1.5, 0.75, 12.0], dtype=torch.bfloat16, device="cuda").view(4, 1, 1).expand(4, 1, 128).contiguous()
+    rk.kv_write_fp4(x, -x, *codes, *scales, slots)
+    for c, s, sign in zip(codes, scales, (1, -1)):
+        for (b, t), value in zip(places, (3.0, -1.5, 0.75, 12.0)):
+            want = ow.fp4_encode(np.full((1, 128), sign * value), "bf16")
+            assert equal(host(c[b, t]), want[0]) and equal(host(s[b, t]), want[1])
+            c[b, t], s[b, t] = 9, 9
+        assert all(bool((x[k:k + 100_000] == 9).all()) for x in (c, s) for k in range(0, far, 100_000))
+    # and read: other bytes in each cache
+    for k, (c, s) in enumerate(zip(codes, scales)):
+        for n, (b, t) in enumerate(places):
+            c[b, t], s[b, t] = 0x22 + 0x11 * n, 127 + k
+    for k, got in enumerate(rk.kv_read_fp4(*codes, *scales, slots)):
+        assert equal(host(got), np.array([1.0, 1.5, 2.0, 3.0]).reshape(4, 1, 1) * 2 ** k * np.ones((4, 1, 128)))
     assert rk.device_status(reset=True) == 0
 
 

@@ -338,6 +338,19 @@ def test_attend_rows_that_are_not_there(gpu, Hq, new, D, dtype):
         assert rk.device_status(reset=True) == (0x80 if bad else 0)
 
 
+@pytest.mark.parametrize("Hq,kv,new", [(4, [700, 50], [1, 2]), (1, [30] * 300, [1] * 300), (8, [300, 90], [300, 33])])
+def test_attend_smallest_values(gpu, Hq, kv, new):
+    """fp16 keys and values below 2^-14, which the type holds with fewer bits."""
+    torch, rk = gpu
+    b = Batch(torch, rng_of("small", Hq, len(kv)), kv, new, Hq, 1, 128, "fp16", garbage=0.0)
+    power = torch.tensor([2.0 ** -17, 2.0 ** -20], device="cuda").repeat(64)
+    for c in b.caches:
+        c.copy_((c.float() * power).half())
+    assert float(b.caches[0].abs().max()) < 2.0 ** -13 and float(b.caches[0].abs().max()) > 0
+    attend(gpu, b, scale=2.0 ** 14)
+    assert rk.device_status(reset=True) == 0
+
+
 @pytest.mark.parametrize("singles,pieces,Hq,Hkv,D,dtype", [
     (40, [(6000, 128)], 2, 2, 128, "bf16"), (60, [(5000, 64), (300, 300)], 4, 2, 64, "fp16"), (30, [(4000, 128)], 8, 1, 72, "bf16"),
     (5, [(6000, 1)], 1, 1, 128, "fp16"), (0, [(7000, 4)], 4, 1, 64, "bf16"), (2, [(5000, 20)], 1, 1, 192, "bf16"), (9, [(3000, 40)], 3, 1, 256, "fp16")])
