@@ -632,9 +632,12 @@ struct AttendFp4 : AttendBase<DP, Half> {
             }
         };
         auto scores = [&](auto u, f32x4 (*sc)[NB]) {
+            if (D % 32 != 0) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) end_at(k_raw[u][b], D, g);
+            }
 #pragma unroll
             for (int kt = 0; kt < NB; ++kt) {
-                end_at(k_raw[u][kt], D, g);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) sc[n][kt] = f32x4{};
 #pragma unroll
