@@ -11,8 +11,8 @@
 // What bounds it: few rows (a decoding batch) the reading of keys and values, 4 D bytes a key and head for 4 D
 // operations a row; from some hundred rows a key head on (a prompt, or a group on its prefix) the matrix instructions.  So there are tiles of two
 // shapes, wide and narrow, and solo ones for what is short.  Kernels in a trace, the same inputs over and over: 128 requests on
-// one prefix of 8,192 tokens (64 / 8 heads of 128) 66 + 10 us; prompts of 2,500-6,000 tokens 1.15-1.26 ms, 860-940 TFLOP/s;
-// 5 requests of 60,000-131,072 tokens 193-199 us, 5.1 TB/s.
+// one prefix of 8,192 tokens (64 / 8 heads of 128) 63 + 10 us; prompts of 2,500-6,000 tokens 1.15-1.26 ms, 860-940 TFLOP/s;
+// 5 requests of 60,000-131,072 tokens 188-199 us, 5.1 TB/s.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -43,7 +43,7 @@ enum Kind { kWide, kNarrow, kSolo };
 // wavefront, the others' to a workgroup.  A piece of a line has at least kLeast, a step or more, so that a tile's
 // parts follow each other without a gap.
 constexpr uint32_t kLeast = 4;
-// Blocks of a narrow step, by workgroup, for each 4 units of its cost.
+// A workgroup's blocks in a quarter of a unit of a narrow step's cost.
 template <class A>
 constexpr int kPerBlock = A::kNarrowKeys / RK_BLOCK_TOKENS / (int)A::kStepCost[kNarrow];
 // Keys of a tile's step; A: the class of the tiles, whose kNarrowKeys are a wavefront's in a narrow step.
@@ -1136,7 +1136,7 @@ inline AttendLayout attend_layout(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
 }
 
 template <class A, int DP, bool Half>
-static int launch(typename A::Args& p, int32_t grid, hipStream_t s)
+static int launch(typename A::Args& p, int32_t grid, hipStream_t s, const char* name)
 {
     const int64_t rows = p.a.T * p.G;
     // A row a wavefront, so eight workgroups join a tile of 32 rows or more.  Most tiles of a batch have its average request's rows, and
@@ -1153,25 +1153,25 @@ static int launch(typename A::Args& p, int32_t grid, hipStream_t s)
         // on 2 key heads 25 us, 21 by workgroups; 64 of 128 on 8 22 us, 27 by workgroups).
         p.solo_most = (int64_t)p.n * p.a.Hkv > grid / 2 ? kSoloMost : 0;
         hipLaunchKernelGGL((attend_kernel<A>), dim3((unsigned)grid), dim3(kThreads), lds_bytes(DP, p.n), s, p);
-        int rc = hip_check(hipGetLastError(), "rk_prefix_attention launch");
+        int rc = hip_check(hipGetLastError(), name);
         if (rc) return rc;
         const int64_t blocks = (int64_t)grid * chunks + (p.a.group_off ? (int64_t)p.n * p.a.Hkv * shared_chunks : 0);
         hipLaunchKernelGGL((join_kernel<A, DP, Half>), dim3((unsigned)blocks), dim3(kThreads), 0, s, (const AttendArgs&)p, grid, chunks,
                            soon, shared_chunks);
-        rc = hip_check(hipGetLastError(), "rk_prefix_attention join launch");
+        rc = hip_check(hipGetLastError(), name);
         if (rc) return rc;
     }
     return RK_OK;
 }
 
 template <template <int, bool> class Tiles, bool Half>
-static int launch_of(typename Tiles<64, Half>::Args& p, int32_t grid, hipStream_t s)
+static int launch_of(typename Tiles<64, Half>::Args& p, int32_t grid, hipStream_t s, const char* name)
 {
     switch (head_size(p.a.D)) {
-    case 64: return launch<Tiles<64, Half>, 64, Half>(p, grid, s);
-    case 128: return launch<Tiles<128, Half>, 128, Half>(p, grid, s);
-    case 192: return launch<Tiles<192, Half>, 192, Half>(p, grid, s);
-    default: return launch<Tiles<256, Half>, 256, Half>(p, grid, s);
+    case 64: return launch<Tiles<64, Half>, 64, Half>(p, grid, s, name);
+    case 128: return launch<Tiles<128, Half>, 128, Half>(p, grid, s, name);
+    case 192: return launch<Tiles<192, Half>, 192, Half>(p, grid, s, name);
+    default: return launch<Tiles<256, Half>, 256, Half>(p, grid, s, name);
     }
 }
 
@@ -1234,7 +1234,8 @@ static int attention_call(const rk_attention& a, Args& p, void* workspace, size_
     p.g_inverse = (uint32_t)((65535 + p.G) / p.G);
     p.shared_rows = L.shared_rows;
     p.shared_tokens = L.shared_tokens;
-    return a.dtype == RK_F16 ? launch_of<Tiles, true>(p, L.grid, (hipStream_t)stream) : launch_of<Tiles, false>(p, L.grid, (hipStream_t)stream);
+    return a.dtype == RK_F16 ? launch_of<Tiles, true>(p, L.grid, (hipStream_t)stream, name)
+                             : launch_of<Tiles, false>(p, L.grid, (hipStream_t)stream, name);
 }
 
 }  // namespace rk

@@ -8,7 +8,7 @@
 // Kernels in a trace, the same inputs over and over: 96 requests of 500-12,000 tokens (64 / 8 heads of 128) 98 + 5 us, 3.9 TB/s, of
 // which 20-25 us are the beginning (lengths, pieces, block numbers, queries) and the ends of pieces (longer and shorter batches
 // differ by 5.7 TB/s); 5 requests of 60,000-200,000 tokens (16 / 4 heads) 88 + 6 us, 4.3 TB/s; 128 requests on one prefix of 8,192
-// tokens 67 + 10 us, as over 16 bits; whole prompts of 2,500-6,000 tokens 1.10-1.19 ms, 910-980 TFLOP/s.
+// tokens 67 + 10 us, as over 16 bits; whole prompts of 2,500-6,000 tokens 1.10-1.22 ms, 890-980 TFLOP/s.
 #include "attend.h"
 
 namespace rk {
@@ -243,8 +243,8 @@ struct AttendFp4 : AttendBase<DP, Half> {
         }
         constexpr uint32_t kKeys = kWideKeys * kRow;   // bytes of a step's keys; two of them, then two steps' values
         // Keys come two steps ahead, values one: while a step's weights are computed, the products of the next step's
-        // scores run beside them (whole prompts 1,440 -> 1,360 us).  Pieces are read from LDS kAhead products before the one that
-        // takes them: 3 are as good, 6 spill registers (whole prompts 1,230 -> 1,500 us).
+        // scores run beside them.  Pieces are read from LDS kAhead products before the one that takes them.  (Both as over 16 bits, where they
+        // were measured: 1,440 -> 1,360 us of whole prompts, and with 6 ahead, which spills, 1,230 -> 1,500.)
         constexpr int kAhead = 4, kPairs = 16;       // (a lane has 32 scores of a step: kPairs pairs)
         Held& a = args();
         const int32_t n_blocks = a.a.n_blocks, D = a.a.D;
@@ -386,7 +386,7 @@ struct AttendFp4 : AttendBase<DP, Half> {
                 }
             }
             // (a wavefront in this product goes first: the other on its SIMD has its weights to compute meanwhile;
-            // whole prompts 1,251 -> 1,214 us)
+            // whole prompts over 16 bits 1,251 -> 1,214 us)
             __builtin_amdgcn_s_setprio(1);
             const Values va = values_in(values_at(x));
             true_values(x + 1, e1);
